@@ -78,11 +78,15 @@ extern "C" {
 #define DSDE_ERR_SIGNAL 32u  /* non-finite KLD, SF, WVIR or SL_max, or SL_max < sl_min */
 #define DSDE_ERR_STATE 64u   /* ring head outside [0, W) or count outside [0, W] */
 
+#define DSDE_ERR_FILTER 128u /* top_p outside (0, 1] or min_p outside [0, 1] */
+
 /* Largest supported speculation length bound (one wavefront lane per drafted position). */
 #define DSDE_MAX_K 63
 /* Largest supported vocabulary (512 chunks of 8192 logits; the draw keeps one
  * cell per 2048 logits in the workspace). */
 #define DSDE_MAX_VOCAB 4194304
+/* Most entries per row of dsde_top_logits and of a teacher in dsde_distill_*. */
+#define DSDE_MAX_TOP 256
 
 /* The ABI version this library implements (DSDE_ABI_VERSION). */
 int32_t dsde_abi_version(void);
@@ -433,6 +437,125 @@ int32_t dsde_shard_draw_pick(int32_t G, int32_t g, const dsde_shard_mass *masses
                              int32_t B, int64_t N, int32_t k_max, const dsde_draw_job *jobs, int32_t pad_id,
                              int32_t *accepted, int32_t *tokens, int32_t *drawn, uint32_t *seq_err,
                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Operators on rows of logits around the step: drawing the draft model's tokens
+ * (and those of sequences that draft nothing), keeping the target's largest
+ * logits, and distilling the draft model from them.
+ *
+ * Common to them:
+ *   - rows [R, V] of fp32 or bf16 logits (dtype), row r at element r * row_stride
+ *     (row_stride >= V where R > 1: slices of wider rows are read in place); rows
+ *     of any width and alignment;
+ *   - a logit of -inf is a masked token: it has weight 0 and is never drawn or kept.
+ *     Finite masks (the type's lowest value, say) are ordinary logits;
+ *   - R = 0 is a call without work;
+ *   - row_err [R] uint32 holds DSDE_ERR_* bits per row, 0 when fine; DSDE_ERR_LOGIT:
+ *     a NaN or +inf in the row, or no finite logit at all;
+ *   - equal logits rank by token id, the smallest first (+0 and -0 are equal).
+ */
+
+/* Workspace bytes of dsde_sample and dsde_top_logits; 0 when the sizes are
+ * invalid.  It grows with R up to 192 MiB (more rows run in several passes). */
+size_t dsde_sample_workspace_bytes(int64_t R, int64_t V);
+
+/*
+ * One token per row from softmax(z / T) under filters, from given uniforms.
+ *
+ *   temperature [R]   float   T: in [2^-16, 2^16], or 0 for the row's argmax (its
+ *                             other settings are not read then)
+ *   top_k [R]         int32   optional (NULL: off): keep the top_k largest logits;
+ *                             <= 0 or >= V: off
+ *   top_p [R]         float   optional (NULL: off): of those, keep the smallest number
+ *                             of largest ones that holds top_p of their weight; in (0, 1], 1: off
+ *   min_p [R]         float   optional (NULL: off): of those, keep the ones whose
+ *                             probability is at least min_p times the largest; in [0, 1], 0: off
+ *   u [R]             float   uniforms in [0, 1)
+ *   pad_id                    token of flagged rows
+ * Outputs:
+ *   tokens [R]        int32   the smallest id whose cumulative weight over the kept
+ *                             tokens, in ascending id order, exceeds u times their total
+ *   logprob [R]       float   optional: log softmax(z / T) of that token over the whole row
+ *                             (T = 0: at T = 1)
+ *   kept [R]          int32   optional: how many tokens the filters kept (at least 1),
+ *                             masked ones left out; counting them takes a row without filters
+ *                             a second pass
+ *   row_err [R]       uint32  DSDE_ERR_LOGIT, DSDE_ERR_TEMP, DSDE_ERR_UNIFORM, DSDE_ERR_FILTER;
+ *                             a flagged row has pad_id, NaN and 0
+ * Drafts that dsde_verify will judge are drawn without filters, at the temperature given to it:
+ * its acceptance takes q to be the whole tempered softmax.
+ */
+int32_t dsde_sample(const void *logits, int64_t row_stride, int32_t dtype, int64_t V, int64_t R,
+                    const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                    const float *u, int32_t pad_id, int32_t *tokens, float *logprob, int32_t *kept,
+                    uint32_t *row_err, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The k largest logits of each row (1 <= k <= DSDE_MAX_TOP), largest first, with
+ * their ids, and the row's log-normaliser: what distillation needs of a teacher's row.
+ *
+ *   temperature        one T for every row, in [2^-16, 2^16]
+ * Outputs:
+ *   values [R, k]  float   the logits themselves (not divided by T); -inf in unused slots
+ *   ids [R, k]     int32   their tokens; -1 in unused slots (rows with fewer finite logits)
+ *   lse [R]        float   log sum_v exp(z_v / T)
+ *   row_err [R]    uint32  DSDE_ERR_LOGIT; a flagged row has NaN values and lse, ids -1
+ */
+int32_t dsde_top_logits(const void *logits, int64_t row_stride, int32_t dtype, int64_t V, int64_t R, int32_t k,
+                        float temperature, float *values, int32_t *ids, float *lse, uint32_t *row_err,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Distillation from a teacher's top logits.
+ *
+ *   logits [N, V]        the student's rows s
+ *   ids, teacher [N, K]  int32, float: the teacher's tokens i_k and logits t_k (1 <= K <=
+ *                        DSDE_MAX_TOP), in any order; id -1: unused, -inf: no weight
+ *   teacher_lse [N]      float, optional: log sum_v exp(t_v / T) of the teacher's whole row
+ *   temperature          T, in [2^-16, 2^16], of both models
+ * With teacher_lse: p_k = exp(t_k / T - lse), r = max(0, 1 - sum p_k) the teacher's
+ * mass on all other tokens, and with q = softmax(s / T), q_r = its sum over those
+ *   loss = sum_k p_k (log p_k - log q_{i_k}) + r (log r - log q_r)
+ *   T dloss/ds_v = q_v - p_k at v = i_k, and (q_v / q_r) (q_r - r) elsewhere;
+ * r counts as 0 where the student has no token outside the teacher's.  Without it (NULL) p is
+ * the softmax of t / T over the K entries and r = 0: T dloss/ds_v = q_v - p_k, and q_v
+ * elsewhere; a row without entries then has loss 0 and gradient 0.  The gradient is not
+ * multiplied by T^2; weights can be.
+ *
+ * dsde_distill_loss writes loss [N], and record [N], which dsde_distill_grad
+ * takes with weight [N] (the gradient with respect to the losses) for
+ *   grad [N, V], of the logits' type, row n at element n * grad_stride: weight[n] times
+ *   the gradient, rounded once.
+ * dsde_distill_step does both at once, where the weights are known beforehand; a row of
+ * weight 0 is left out (loss 0, gradient 0, nothing of it read or checked).  grad may be
+ * the logits' own memory (with the same stride).
+ * row_err [N]: DSDE_ERR_TOKEN (an id outside [-1, V), or one twice), DSDE_ERR_LOGIT (also a
+ * teacher logit of NaN or +inf, a teacher_lse that is not finite, or a student logit of -inf at a
+ * teacher's token with weight); a flagged row has loss NaN and gradient 0.
+ */
+typedef struct {
+  float rest_ref, rest_scale; /* gradient outside the entries: rest_scale 2^((s - rest_ref) c), c = log2(e) / T */
+  float ref, scale;           /* q at the entries: scale 2^((s - ref) c) */
+  float teacher_ref, teacher_scale; /* p: teacher_scale 2^((t - teacher_ref) c) */
+  int32_t empty;              /* 1: a row without gradient */
+  int32_t unused;
+} dsde_distill_row;           /* 32 bytes */
+
+/* Workspace bytes of dsde_distill_loss and dsde_distill_step; 0 when the sizes are invalid. */
+size_t dsde_distill_workspace_bytes(int64_t N, int64_t V);
+
+int32_t dsde_distill_loss(const void *logits, int64_t row_stride, int32_t dtype, int64_t V, int64_t N, int32_t K,
+                          const int32_t *ids, const float *teacher, const float *teacher_lse, float temperature,
+                          float *loss, dsde_distill_row *record, uint32_t *row_err, void *workspace,
+                          size_t workspace_bytes, void *stream);
+int32_t dsde_distill_grad(const void *logits, int64_t row_stride, int32_t dtype, int64_t V, int64_t N, int32_t K,
+                          const int32_t *ids, const float *teacher, float temperature,
+                          const dsde_distill_row *record, const float *weight, void *grad, int64_t grad_stride,
+                          void *stream);
+int32_t dsde_distill_step(const void *logits, int64_t row_stride, int32_t dtype, int64_t V, int64_t N, int32_t K,
+                          const int32_t *ids, const float *teacher, const float *teacher_lse, float temperature,
+                          const float *weight, float *loss, void *grad, int64_t grad_stride, uint32_t *row_err,
+                          void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Measurement utility, not part of the method: reads `bytes` bytes of device

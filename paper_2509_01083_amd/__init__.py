@@ -19,12 +19,17 @@ LIB_PATH = os.path.join(HERE, "libdsde.so")
 OK, INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE_ERROR = 0, 1, 2, 3
 FP32, BF16 = 0, 1
 ERR_LAYOUT, ERR_TOKEN, ERR_LOGIT, ERR_TEMP, ERR_UNIFORM, ERR_SIGNAL, ERR_STATE = 1, 2, 4, 8, 16, 32, 64
+ERR_FILTER = 128
 MAX_K = 63
+MAX_TOP = 256
+DISTILL_ROW_BYTES = 32
 STATIC_SCRATCH_BYTES = 16 << 20  # DSDE_STATIC_SCRATCH_BYTES: the scratch array of dsde_step_static
 EXPORTS = ("dsde_abi_version", "dsde_status_string", "dsde_verify_workspace_bytes", "dsde_verify",
            "dsde_step", "dsde_step_static", "dsde_kld_signal", "dsde_next_sl", "dsde_calibration_update", "dsde_calibrate_sl_max",
            "dsde_set_profile_events", "dsde_stream_read", "dsde_shard_workspace_bytes", "dsde_shard_stats",
-           "dsde_shard_accept", "dsde_shard_accept_step", "dsde_shard_draw_mass", "dsde_shard_draw_pick")
+           "dsde_shard_accept", "dsde_shard_accept_step", "dsde_shard_draw_mass", "dsde_shard_draw_pick",
+           "dsde_sample_workspace_bytes", "dsde_sample", "dsde_top_logits", "dsde_distill_workspace_bytes",
+           "dsde_distill_loss", "dsde_distill_grad", "dsde_distill_step")
 # sizes of the records the vocabulary-shard calls exchange (dsde_shard_partial,
 # dsde_draw_job, dsde_shard_mass); kept as raw bytes on the Python side
 SHARD_PARTIAL_BYTES, DRAW_JOB_BYTES, SHARD_MASS_BYTES = 64, 44, 32
@@ -90,6 +95,20 @@ def load(path: str = LIB_PATH):
     lib.dsde_shard_draw_pick.restype = i32
     lib.dsde_shard_draw_pick.argtypes = [i32, i32, P, P, P, i32, i64, i64, i32, i64, i32, P, i32, P, P, P, P, P,
                                          sz, P]
+    lib.dsde_sample_workspace_bytes.restype = sz
+    lib.dsde_sample_workspace_bytes.argtypes = [i64, i64]
+    lib.dsde_sample.restype = i32
+    lib.dsde_sample.argtypes = [P, i64, i32, i64, i64, P, P, P, P, P, i32, P, P, P, P, P, sz, P]
+    lib.dsde_top_logits.restype = i32
+    lib.dsde_top_logits.argtypes = [P, i64, i32, i64, i64, i32, f32, P, P, P, P, P, sz, P]
+    lib.dsde_distill_workspace_bytes.restype = sz
+    lib.dsde_distill_workspace_bytes.argtypes = [i64, i64]
+    lib.dsde_distill_loss.restype = i32
+    lib.dsde_distill_loss.argtypes = [P, i64, i32, i64, i64, i32, P, P, P, f32, P, P, P, P, sz, P]
+    lib.dsde_distill_grad.restype = i32
+    lib.dsde_distill_grad.argtypes = [P, i64, i32, i64, i64, i32, P, P, f32, P, P, P, i64, P]
+    lib.dsde_distill_step.restype = i32
+    lib.dsde_distill_step.argtypes = [P, i64, i32, i64, i64, i32, P, P, P, f32, P, P, P, i64, P, P, sz, P]
     _lib = lib
     return lib
 
@@ -337,6 +356,155 @@ def stream_read(buf, out):
         raise DsdeError("stream_read: out holds fewer than one word per 32 KiB")
     _check(lib.dsde_stream_read(ctypes.c_void_p(buf.data_ptr()), nbytes, ctypes.c_void_p(out.data_ptr()),
                                 ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)))
+
+
+# ---------------------------------------------------------------------------
+# operators on rows of logits: sampling, top logits, distillation
+# ---------------------------------------------------------------------------
+
+def _row_buffers(logits, name):
+    """Rows, vocabulary and device of the logits of a row operator."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise DsdeError(f"{name} must be [rows, vocabulary]")
+    return int(logits.shape[0]), int(logits.shape[1]), logits.device
+
+
+def new_sample_workspace(R, V, device="cuda"):
+    """The workspace of ``sample`` and ``top_logits`` for R rows of V logits; one made for
+    the largest sizes serves all smaller ones."""
+    n = int(load().dsde_sample_workspace_bytes(R, V))
+    if n == 0:
+        raise DsdeError("invalid sizes for the sampling workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def sample(logits, temperature, u, top_k=None, top_p=None, min_p=None, pad_id=-1, kept=False, out=None,
+           workspace=None, stream=None):
+    """``dsde_sample``: one token per row of ``logits`` [R, V] (bf16 or fp32, any row
+    stride) from softmax(logits / temperature) under top-k, top-p and min-p, by the
+    uniforms ``u`` [R].  temperature, top_p and min_p are [R] float32, top_k [R]
+    int32; None switches a filter off.  Returns a dict with tokens, logprob, row_err
+    (and kept, the number of tokens the filters left, when asked for); pass ``out``
+    to reuse its buffers (without logprob in it that is not computed)."""
+    native = _native or _bind()
+    if out is None or workspace is None:
+        R, V, dev = _row_buffers(logits, "logits")
+        with _on(stream):
+            if out is None:
+                i32 = torch.empty((3 if kept else 2, R), dtype=torch.int32, device=dev)
+                out = {"tokens": i32[0], "logprob": torch.empty(R, dtype=torch.float32, device=dev),
+                       "row_err": i32[1]}
+                if kept:
+                    out["kept"] = i32[2]
+            if workspace is None:
+                workspace = new_sample_workspace(R, V, device=dev)
+    native.sample(logits, temperature, top_k, top_p, min_p, u, int(pad_id), out, workspace, _handle(stream))
+    return out
+
+
+def top_logits(logits, k, temperature=1.0, out=None, workspace=None, stream=None):
+    """``dsde_top_logits``: the k largest logits of each row, largest first (equal ones
+    by id), and its log-normaliser at ``temperature`` (a number).  Returns a dict with
+    values [R, k] float32, ids [R, k] int32, lse [R] float32, row_err: the teacher's side
+    of ``distill``."""
+    native = _native or _bind()
+    k = int(k)
+    if out is None or workspace is None:
+        R, V, dev = _row_buffers(logits, "logits")
+        if not 1 <= k <= MAX_TOP:
+            raise DsdeError(f"k must be in 1..{MAX_TOP}")
+        with _on(stream):
+            if out is None:
+                out = {"values": torch.empty((R, k), dtype=torch.float32, device=dev),
+                       "ids": torch.empty((R, k), dtype=torch.int32, device=dev),
+                       "lse": torch.empty(R, dtype=torch.float32, device=dev),
+                       "row_err": torch.empty(R, dtype=torch.int32, device=dev)}
+            if workspace is None:
+                workspace = new_sample_workspace(R, V, device=dev)
+    native.top_logits(logits, k, float(temperature), out, workspace, _handle(stream))
+    return out
+
+
+def new_distill_workspace(N, V, device="cuda"):
+    """The workspace of ``distill_loss`` and ``distill_step`` for N rows of V logits."""
+    n = int(load().dsde_distill_workspace_bytes(N, V))
+    if n == 0:
+        raise DsdeError("invalid sizes for the distillation workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def distill_loss(logits, ids, teacher, teacher_lse=None, temperature=1.0, out=None, workspace=None, stream=None):
+    """``dsde_distill_loss``: per row of the student's ``logits`` [N, V] the divergence
+    from the teacher's top logits (``ids`` [N, K] int32, ``teacher`` [N, K] float32, and
+    ``teacher_lse`` [N] float32 for the mass it gives to all other tokens).  Returns a
+    dict with loss [N] float32, row_err, and record [N, 32] uint8 for ``distill_grad``."""
+    native = _native or _bind()
+    if out is None or workspace is None:
+        N, V, dev = _row_buffers(logits, "logits")
+        with _on(stream):
+            if out is None:
+                out = {"loss": torch.empty(N, dtype=torch.float32, device=dev),
+                       "record": torch.empty((N, DISTILL_ROW_BYTES), dtype=torch.uint8, device=dev),
+                       "row_err": torch.empty(N, dtype=torch.int32, device=dev)}
+            if workspace is None:
+                workspace = new_distill_workspace(N, V, device=dev)
+    native.distill_loss(logits, ids, teacher, teacher_lse, float(temperature), out, workspace, _handle(stream))
+    return out
+
+
+def distill_grad(logits, ids, teacher, record, weight, temperature=1.0, grad=None, stream=None):
+    """``dsde_distill_grad``: the gradient of sum(weight * loss) with respect to the
+    logits, from the record of ``distill_loss`` on the same inputs.  ``grad`` may be the logits themselves."""
+    native = _native or _bind()
+    if grad is None:
+        N, V, dev = _row_buffers(logits, "logits")
+        with _on(stream):
+            grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    native.distill_grad(logits, ids, teacher, float(temperature), record, weight, grad, _handle(stream))
+    return grad
+
+
+def distill_step(logits, ids, teacher, weight, teacher_lse=None, temperature=1.0, grad=None, out=None,
+                 workspace=None, stream=None):
+    """``dsde_distill_step``: loss and gradient in one call, for weights [N] known before
+    it (rows of weight 0 are left out).  ``grad`` may be the logits themselves.
+    Returns a dict with loss, grad, row_err."""
+    native = _native or _bind()
+    if out is None or grad is None or workspace is None:
+        N, V, dev = _row_buffers(logits, "logits")
+        with _on(stream):
+            if out is None:
+                out = {"loss": torch.empty(N, dtype=torch.float32, device=dev),
+                       "row_err": torch.empty(N, dtype=torch.int32, device=dev)}
+            if grad is None:
+                grad = out["grad"] if "grad" in out else torch.empty((N, V), dtype=logits.dtype, device=dev)
+            if workspace is None:
+                workspace = new_distill_workspace(N, V, device=dev)
+    native.distill_step(logits, ids, teacher, teacher_lse, float(temperature), weight, out["loss"], grad,
+                        out["row_err"], workspace, _handle(stream))
+    out["grad"] = grad
+    return out
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, teacher, teacher_lse, temperature):
+        o = distill_loss(logits, ids, teacher, teacher_lse, temperature)
+        ctx.save_for_backward(logits, ids, teacher, o["record"])
+        ctx.temperature = temperature
+        return o["loss"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, weight):
+        logits, ids, teacher, record = ctx.saved_tensors
+        return distill_grad(logits, ids, teacher, record, weight.contiguous(), ctx.temperature), None, None, None, None
+
+
+def distill(logits, ids, teacher, teacher_lse=None, temperature=1.0):
+    """``distill_loss`` [N] for autograd: differentiable with respect to the logits
+    (the teacher is taken as constant)."""
+    return _Distill.apply(logits, ids, teacher, teacher_lse, temperature)
 
 
 # ---------------------------------------------------------------------------

@@ -23,6 +23,7 @@ PyObject *g_error = nullptr;  // paper_2509_01083_amd.DsdeError
 #define DSDE_ENTRIES(X)                                                                                         \
   X(dsde_status_string)                                                                                         \
   X(dsde_verify) X(dsde_step) X(dsde_step_static) X(dsde_kld_signal) X(dsde_next_sl) X(dsde_calibration_update) \
+  X(dsde_sample) X(dsde_top_logits) X(dsde_distill_loss) X(dsde_distill_grad) X(dsde_distill_step)              \
   X(dsde_shard_stats) X(dsde_shard_accept) X(dsde_shard_accept_step) X(dsde_shard_draw_mass) X(dsde_shard_draw_pick)
 struct Library {
 #define X(name) decltype(&::name) name;
@@ -536,6 +537,159 @@ PyObject *py_shard_draw_pick(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
+// Strided rows [R, V] of logits: any row stride, each row dense.
+struct LogitRows {
+  void *data;
+  int64_t R, V, stride;
+  int32_t dtype;
+};
+LogitRows take_strided(Args &a, const char *name) {
+  PyObject *o = a.next();
+  size_of(o, 1, name);
+  const at::Tensor &t = THPVariable_Unpack(o);
+  LogitRows r;
+  r.dtype = logits_type(t);
+  if (t.dim() != 2) fail(std::string(name) + " must be [rows, vocabulary]");
+  if (!t.is_cuda()) fail(std::string(name) + " must be a GPU tensor");
+  r.R = t.size(0);
+  r.V = t.size(1);
+  r.stride = r.R > 1 ? t.stride(0) : r.V;
+  if (r.R > 0 && r.V > 1 && t.stride(1) != 1) fail(std::string(name) + " must have dense rows");
+  if (r.R > 1 && r.stride < r.V) fail(std::string(name) + " must have rows that do not overlap");
+  r.data = t.data_ptr();
+  return r;
+}
+
+// sample(logits, temperature, top_k, top_p, min_p, u, pad_id, out, workspace, stream); logprob and kept where out has them
+PyObject *py_sample(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    const LogitRows z = take_strided(a, "logits");
+    const auto *T = take<float>(a, kF32, z.R, "temperature");
+    const auto *k = take<int32_t>(a, kI32, z.R, "top_k");
+    const auto *p = take<float>(a, kF32, z.R, "top_p"), *m = take<float>(a, kF32, z.R, "min_p");
+    const auto *u = take<float>(a, kF32, z.R, "u");
+    const int32_t pad = a.int32();
+    PyObject *dict = a.next();
+    auto *tokens = out<int32_t>(dict, "tokens", kI32, z.R);
+    auto *lp = PyMapping_HasKeyString(dict, "logprob") ? out<float>(dict, "logprob", kF32, z.R) : nullptr;
+    auto *kept = PyMapping_HasKeyString(dict, "kept") ? out<int32_t>(dict, "kept", kI32, z.R) : nullptr;
+    auto *err = out<uint32_t>(dict, "row_err", kAny, z.R);
+    size_t bytes;
+    void *ws = take_workspace(a, &bytes), *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_sample(z.data, z.stride, z.dtype, z.V, z.R, T, k, p, m, u, pad, tokens, lp, kept, err, ws,
+                               bytes, stream);
+    });
+  });
+}
+
+// top_logits(logits, k, temperature, out, workspace, stream)
+PyObject *py_top_logits(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    const LogitRows z = take_strided(a, "logits");
+    const int32_t k = a.int32();
+    const float T = a.real();
+    PyObject *dict = a.next();
+    auto *values = out<float>(dict, "values", kF32, z.R * k);
+    auto *ids = out<int32_t>(dict, "ids", kI32, z.R * k);
+    auto *lse = out<float>(dict, "lse", kF32, z.R);
+    auto *err = out<uint32_t>(dict, "row_err", kAny, z.R);
+    size_t bytes;
+    void *ws = take_workspace(a, &bytes), *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_top_logits(z.data, z.stride, z.dtype, z.V, z.R, k, T, values, ids, lse, err, ws, bytes, stream);
+    });
+  });
+}
+
+// The teacher of a distillation: ids [N, K], teacher [N, K], teacher_lse [N] or None.
+struct Teacher {
+  int32_t K;
+  const int32_t *ids;
+  const float *logits;
+};
+Teacher take_teacher(Args &a, int64_t N) {
+  Teacher x;
+  PyObject *ids = a.next(), *logits = a.next();
+  const int64_t K = size_of(ids, 1, "ids");
+  for (PyObject *o : {ids, logits}) {
+    const char *name = o == ids ? "ids" : "teacher";
+    if (size_of(o, 0, name) != N || size_of(o, 1, name) != K || THPVariable_Unpack(o).dim() != 2)
+      fail("ids and teacher must be [N, K] for logits of N rows");
+  }
+  x.K = int32_t(K);
+  x.ids = static_cast<const int32_t *>(ptr(ids, kI32, N * K, "ids"));
+  x.logits = static_cast<const float *>(ptr(logits, kF32, N * K, "teacher"));
+  return x;
+}
+LogitRows take_gradient(Args &a, const LogitRows &z) {
+  const LogitRows g = take_strided(a, "grad");
+  if (g.R != z.R || g.V != z.V || g.dtype != z.dtype) fail("grad must have the logits' shape and type");
+  return g;
+}
+
+// distill_loss(logits, ids, teacher, teacher_lse, temperature, out, workspace, stream)
+PyObject *py_distill_loss(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    const LogitRows z = take_strided(a, "logits");
+    const Teacher x = take_teacher(a, z.R);
+    const auto *lse = take<float>(a, kF32, z.R, "teacher_lse");
+    const float T = a.real();
+    PyObject *dict = a.next();
+    auto *loss = out<float>(dict, "loss", kF32, z.R);
+    auto *record = out<dsde_distill_row>(dict, "record", kU8, z.R * int64_t(sizeof(dsde_distill_row)));
+    auto *err = out<uint32_t>(dict, "row_err", kAny, z.R);
+    size_t bytes;
+    void *ws = take_workspace(a, &bytes), *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_distill_loss(z.data, z.stride, z.dtype, z.V, z.R, x.K, x.ids, x.logits, lse, T, loss, record,
+                                     err, ws, bytes, stream);
+    });
+  });
+}
+
+// distill_grad(logits, ids, teacher, temperature, record, weight, grad, stream)
+PyObject *py_distill_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    const LogitRows z = take_strided(a, "logits");
+    const Teacher x = take_teacher(a, z.R);
+    const float T = a.real();
+    const auto *record = take<dsde_distill_row>(a, kU8, z.R * int64_t(sizeof(dsde_distill_row)), "record");
+    const auto *weight = take<float>(a, kF32, z.R, "weight");
+    const LogitRows g = take_gradient(a, z);
+    void *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_distill_grad(z.data, z.stride, z.dtype, z.V, z.R, x.K, x.ids, x.logits, T, record, weight,
+                                     g.data, g.stride, stream);
+    });
+  });
+}
+
+// distill_step(logits, ids, teacher, teacher_lse, temperature, weight, loss, grad, row_err, workspace, stream)
+PyObject *py_distill_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    const LogitRows z = take_strided(a, "logits");
+    const Teacher x = take_teacher(a, z.R);
+    const auto *lse = take<float>(a, kF32, z.R, "teacher_lse");
+    const float T = a.real();
+    const auto *weight = take<float>(a, kF32, z.R, "weight");
+    auto *loss = take<float>(a, kF32, z.R, "loss");
+    const LogitRows g = take_gradient(a, z);
+    auto *err = take<uint32_t>(a, kAny, z.R, "row_err");
+    size_t bytes;
+    void *ws = take_workspace(a, &bytes), *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_distill_step(z.data, z.stride, z.dtype, z.V, z.R, x.K, x.ids, x.logits, lse, T, weight, loss,
+                                     g.data, g.stride, err, ws, bytes, stream);
+    });
+  });
+}
+
 // set_error(type): the exception the checks raise
 PyObject *py_set_error(PyObject *, PyObject *type) {
   Py_INCREF(type);
@@ -576,6 +730,11 @@ PyMethodDef g_methods[] = {entry("verify", py_verify),
                            entry("shard_accept", py_shard_accept),
                            entry("shard_draw_mass", py_shard_draw_mass),
                            entry("shard_draw_pick", py_shard_draw_pick),
+                           entry("sample", py_sample),
+                           entry("top_logits", py_top_logits),
+                           entry("distill_loss", py_distill_loss),
+                           entry("distill_grad", py_distill_grad),
+                           entry("distill_step", py_distill_step),
                            {"set_error", py_set_error, METH_O, nullptr},
                            {"set_library", py_set_library, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};

@@ -39,10 +39,13 @@ __device__ __forceinline__ float dpp(float v) {
   return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
 }
 template <int CTRL>
+__device__ __forceinline__ uint64_t dpp(uint64_t v) {
+  const uint64_t lo = dpp<CTRL>(uint32_t(v)), hi = dpp<CTRL>(uint32_t(v >> 32));
+  return (hi << 32) | lo;
+}
+template <int CTRL>
 __device__ __forceinline__ double dpp(double v) {
-  const uint64_t b = uint64_t(__double_as_longlong(v));
-  const uint64_t lo = dpp<CTRL>(uint32_t(b)), hi = dpp<CTRL>(uint32_t(b >> 32));
-  return __longlong_as_double(int64_t((hi << 32) | lo));
+  return __longlong_as_double(int64_t(dpp<CTRL>(uint64_t(__double_as_longlong(v)))));
 }
 
 // The value of `lane` (wave-uniform) in every lane.
@@ -53,10 +56,12 @@ __device__ __forceinline__ int32_t readlane(int32_t v, int lane) { return __buil
 __device__ __forceinline__ float readlane(float v, int lane) {
   return __uint_as_float(readlane(__float_as_uint(v), lane));
 }
+__device__ __forceinline__ uint64_t readlane(uint64_t v, int lane) {
+  const uint64_t lo = readlane(uint32_t(v), lane), hi = readlane(uint32_t(v >> 32), lane);
+  return (hi << 32) | lo;
+}
 __device__ __forceinline__ double readlane(double v, int lane) {
-  const uint64_t b = uint64_t(__double_as_longlong(v));
-  const uint64_t lo = readlane(uint32_t(b), lane), hi = readlane(uint32_t(b >> 32), lane);
-  return __longlong_as_double(int64_t((hi << 32) | lo));
+  return __longlong_as_double(int64_t(readlane(uint64_t(__double_as_longlong(v)), lane)));
 }
 
 struct Add {

@@ -14,6 +14,9 @@ namespace dsde {
 // values stay finite, so padding adds exactly nothing to any sum.
 constexpr uint32_t kPadBf16x2 = 0xef80ef80u;
 constexpr float kPadF32 = -7.9228162514264337593543950336e28f;  // -2^96
+// Operators whose rows may hold -inf or the type's lowest value (masked tokens)
+// pad with -inf instead.
+constexpr uint32_t kInfBf16x2 = 0xff80ff80u;
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -124,9 +127,8 @@ __device__ __forceinline__ u32x4_t load_words(const char *row, uint32_t V, uint3
   return __builtin_nontemporal_load((const u32x4_a2_t *)(row + 2 * size_t(min(8 * w, V - 8))));
 }
 // What load_words returned, in place and padded past V.
-template <int ROW>
+template <int ROW, uint32_t P = kPadBf16x2>
 __device__ __forceinline__ void place_words(u32x4_t &v, uint32_t V, uint32_t w) {
-  constexpr uint32_t P = kPadBf16x2;
   if constexpr (ROW == kAlignedRows) {
     if (w > V / 8 - 1) v = u32x4_t{P, P, P, P};
   } else if (8 * w > V - 8) {
@@ -145,9 +147,9 @@ __device__ __forceinline__ f32x4_t load_quad(const char *row, uint32_t V, uint32
   if constexpr (ROW == kAlignedRows) return __builtin_nontemporal_load((const f32x4_t *)row + min(w, V / 4 - 1));
   return __builtin_nontemporal_load((const f32x4_a4_t *)(row + 4 * size_t(min(4 * w, V - 4))));
 }
-template <int ROW>
+template <int ROW, bool INF = false>
 __device__ __forceinline__ void place_quad(f32x4_t &v, uint32_t V, uint32_t w) {
-  constexpr float P = kPadF32;
+  constexpr float P = INF ? -__builtin_inff() : kPadF32;
   if constexpr (ROW == kAlignedRows) {
     if (w > V / 4 - 1) v = f32x4_t{P, P, P, P};
   } else if (4 * w > V - 4) {

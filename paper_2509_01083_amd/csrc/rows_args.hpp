@@ -1,0 +1,97 @@
+// Arguments, workspaces and launchers of the operators on single rows of logits.
+#pragma once
+
+#include "rows.hpp"
+
+namespace dsde {
+
+// Workspace of the rows that one pair of launches takes; larger calls run
+// their rows in several passes.  The cap also keeps a pass's keys (an eighth of
+// its logits) inside the last-level cache.
+constexpr size_t kSelectBytes = size_t(192) << 20;
+inline size_t select_row_bytes(int64_t V) {
+  return size_t(num_chunks(V)) * (sizeof(float) * (1 + kSegs) + sizeof(uint16_t) * kChunkGroups);
+}
+inline int64_t select_rows_per_pass(int64_t R, int64_t V) {
+  const int64_t n = int64_t(kSelectBytes / select_row_bytes(V));
+  return n < R ? n : R;
+}
+static_assert(kSelectBytes >= (DSDE_MAX_VOCAB / kChunk) * (4 * (1 + kSegs) + 2 * kChunkGroups), "one row fits");
+struct SelectLayout {
+  size_t max, seg, keys, total;
+};
+inline SelectLayout select_layout(int64_t R, int64_t V) {
+  const size_t n = size_t(select_rows_per_pass(R, V)) * size_t(num_chunks(V));
+  const size_t all = size_t(R) * select_row_bytes(V);
+  SelectLayout l;
+  l.max = 0;
+  l.seg = l.max + align_up(sizeof(float) * n);
+  l.keys = l.seg + align_up(sizeof(float) * kSegs * n);
+  l.total = (all < kSelectBytes ? align_up(all) : kSelectBytes) + 3 * 256;  // grows with R and with V
+  return l;
+}
+
+struct SelectArgs {
+  RowsView rows;
+  int32_t dtype;
+  int64_t V;
+  // per-row settings; a null pointer stands for one value or for no filter
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p, *u;
+  float one_temperature;
+  int32_t one_k;
+  bool keys_always;
+  struct {
+    float *max;      // [R, nc] largest logit of each chunk; NaN: a NaN in it
+    float *seg;      // [R, nc, 16] weights of its segments against that
+    uint16_t *keys;  // [R, nc, 1024] high halves of its groups' largest ordered keys
+  } scan;
+  void *workspace;
+  uint32_t *row_err;
+  // sample
+  int32_t pad_id;
+  int32_t *tokens;
+  float *logprob;  // may be null
+  int32_t *kept;   // may be null
+  // top logits
+  float *values;
+  int32_t *ids;
+  float *lse;
+};
+int launch_sample(const SelectArgs &a, int64_t R, hipStream_t stream);
+int launch_top_logits(const SelectArgs &a, int64_t R, hipStream_t stream);
+
+// Distillation: the teacher's entries and the row records that the loss leaves
+// for the gradient.
+struct DistillPartial {
+  float max;       // a chunk's largest logit outside the teacher's entries; NaN: a NaN in it
+  uint32_t bad;    // 1: a teacher's token twice in the chunk
+  double sum;      // sum of its weights against that
+};
+struct DistillArgs {
+  RowsView rows;
+  int32_t dtype;
+  int64_t V;
+  int32_t K;
+  const int32_t *ids;        // [N, K], -1: unused
+  const float *teacher;      // [N, K]
+  const float *teacher_lse;  // [N], may be null: the entries are the whole distribution
+  float temperature;
+  const float *weight;       // [N] gradient weights; null in the loss
+  bool skip_zero;            // rows of weight 0 are left out of the loss too
+  DistillPartial *part;      // [N, nc]
+  dsde_distill_row *record;  // [N]
+  float *loss;               // [N]
+  uint32_t *row_err;         // [N]
+  char *grad;                // [N, V], grad_stride bytes from row to row
+  int64_t grad_stride;
+};
+inline size_t distill_part_bytes(int64_t N, int64_t V) {
+  return align_up(sizeof(DistillPartial) * size_t(N) * size_t(num_chunks(V)));
+}
+int launch_distill_loss(const DistillArgs &a, int64_t N, hipStream_t stream);
+int launch_distill_grad(const DistillArgs &a, int64_t N, hipStream_t stream);
+int launch_distill_step(const DistillArgs &a, int64_t N, hipStream_t stream);
+
+}  // namespace dsde
