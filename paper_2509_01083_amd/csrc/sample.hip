@@ -14,10 +14,14 @@
 namespace dsde {
 namespace {
 
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
 constexpr int kCand = kSelThreads;  // candidates that the select kernel sorts, one per thread
-constexpr int kNeed = 512;          // groups that a row without a smaller top-k asks for
-constexpr int kBins = 4096;
+constexpr int kMostNeed = 256;      // groups asked for at most: about 1.4 times as many reach their threshold
+constexpr int kFirstNeed = 64;      // groups that a row without a top-k asks for
+constexpr int kBins = 2048;
+constexpr int kPerOctave = 64;  // bins per octave of a weight: 32 octaves below the largest
+constexpr int kList = 8192;     // groups in the list of the cuts over many tokens
+constexpr int kMostSegs = 4096;
 constexpr int32_t kUndecided = 0x7fffffff;
 
 // One row's settings, checked.  Greedy rows (T = 0) are rows with top_k = 1.
@@ -96,9 +100,10 @@ __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, 
   if (lane < 4) a.scan.seg[unit * kSegs + 4 * lane + wave] = total;
   if (t == 0) a.scan.max[unit] = bad ? NAN : M;
   if (a.keys_always || s.filtered) {
-    uint16_t *keys = a.scan.keys + unit * kChunkGroups + t;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) keys[256 * i] = uint16_t(order_key(gm[i]) >> 16);
+    // a thread's four keys together: group 256 i + t of the chunk at place 4 t + i (place_group)
+    const uint32_t lo = (order_key(gm[0]) >> 16) | (order_key(gm[1]) & 0xffff0000u);
+    const uint32_t hi = (order_key(gm[2]) >> 16) | (order_key(gm[3]) & 0xffff0000u);
+    reinterpret_cast<uint2 *>(a.scan.keys + unit * kChunkGroups)[t] = make_uint2(lo, hi);
   }
 }
 
@@ -106,91 +111,109 @@ __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, 
 // selection
 // ---------------------------------------------------------------------------
 
-// Everything the select kernel keeps in LDS.  The histogram's two arrays, the
-// candidates and the segment arrays are never needed at once.
+// The group whose key lies at this place of a row's keys.
+__device__ __forceinline__ uint32_t place_group(uint32_t q) {
+  return (q & ~uint32_t(kChunkGroups - 1)) + 256 * (q & 3) + ((q & (kChunkGroups - 1)) >> 2);
+}
+constexpr uint32_t kAll = (kKeyNegInf >> 16) + 1;  // the smallest key (high half) of a finite logit
+
+// Everything the select kernel keeps in LDS.  The histogram, the segments and
+// the arrays of the narrow search are never needed at once.
 struct SelectLds {
   union {
     struct {
       unsigned long long mass[kBins];
       uint32_t count[kBins];
     } hist;
+    unsigned long long segs[kMostSegs];
     struct {
-      uint64_t cand[kCand];
       uint32_t groups[kCand];
-    } list;
-    struct {
-      float weight[2 * kBins];
-      uint16_t ties[2 * kBins];
-    } segs;
+      uint32_t tmax[kSelThreads];
+    } narrow;
   };
-  double red64[kSelWaves];
+  uint64_t cand[kCand];
+  uint32_t list[kList];
+  uint64_t red64[kSelWaves];
   uint32_t red32[kSelWaves];
   float redf[kSelWaves];
   uint32_t n_groups, n_cand;
   int32_t found;
   uint32_t found_before, found_count;
   uint64_t mass_before, mass_count;
-  double mass, target;
+  double mass, rem;
   int32_t seg;
   uint32_t seg_ties;
+  uint64_t cut;
 };
 
-// Sorts one value per thread, descending over the first P threads (a power of
-// two; the others pass through).  Partners in one wavefront exchange by
-// shuffles, others through LDS.
-__device__ __forceinline__ uint64_t block_sort(uint64_t v, uint32_t P, uint64_t *lds) {
-  const uint32_t t = threadIdx.x;
-  for (uint32_t size = 2; size <= P; size *= 2) {
-    for (uint32_t stride = size / 2; stride > 0; stride /= 2) {
-      uint64_t o;
-      if (stride >= 64) {
-        lds[t] = v;
-        __syncthreads();
-        o = lds[t ^ stride];
-        __syncthreads();
-      } else {
-        o = __shfl_xor((unsigned long long)v, int(stride));
-      }
-      const bool first = (t & stride) == 0, desc = (t & size) == 0;
-      v = (first == desc) == (v < o) ? o : v;
-    }
-  }
-  return v;
+// The value of lane ^ STRIDE.
+template <int STRIDE>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
+  if constexpr (STRIDE == 1) return lanes::dpp<lanes::kQuadSwap1>(v);
+  if constexpr (STRIDE == 2) return lanes::dpp<lanes::kQuadSwap2>(v);
+  if constexpr (STRIDE == 4) return lanes::dpp<0x1B>(lanes::dpp<lanes::kRowHalfMirror>(v));  // i ^ 7, then i ^ 3
+  if constexpr (STRIDE == 8) return lanes::dpp<lanes::kRowRor8>(v);
+  return __shfl_xor((unsigned long long)v, STRIDE);
 }
-__device__ __forceinline__ uint32_t sort_width(uint32_t n) { return n <= 2 ? 2 : 1u << (32 - __builtin_clz(n - 1)); }
+template <int SIZE, int STRIDE>
+__device__ __forceinline__ void sort_steps(uint64_t &v, uint64_t *lds) {
+  const uint32_t t = threadIdx.x;
+  uint64_t o;
+  if constexpr (STRIDE >= 64) {
+    lds[t] = v;
+    __syncthreads();
+    o = lds[t ^ STRIDE];
+    __syncthreads();
+  } else {
+    o = lane_xor<STRIDE>(v);
+  }
+  const bool first = (t & STRIDE) == 0, desc = (t & SIZE) == 0;
+  v = (first == desc) == (v < o) ? o : v;
+  if constexpr (STRIDE > 1) sort_steps<SIZE, STRIDE / 2>(v, lds);
+}
+// Sorts one value per thread, descending over the first P threads (P the
+// smallest power of two >= n, at least 2; the others pass through): a
+// bitonic network whose partners inside one wavefront exchange by DPP moves
+// and shuffles, others through LDS.
+template <int SIZE = 2>
+__device__ __forceinline__ void block_sort(uint64_t &v, uint32_t n, uint64_t *lds) {
+  sort_steps<SIZE, SIZE / 2>(v, lds);
+  if constexpr (SIZE < kSelThreads) {
+    if (n > SIZE) block_sort<SIZE * 2>(v, n, lds);
+  }
+}
 
 // The bin of a descending histogram at which the running total (count, or mass
-// with MASS) reaches the target, given the total before its first bin.  Leaves
+// with MASS) reaches the target, given the totals before its first bin.  Leaves
 // found, found_before / found_count and mass_before / mass_count; found = -1
-// when the window does not reach it, with the totals over it in *_before.
+// when the window does not reach it, with the totals behind it in *_before.
 template <bool MASS>
 __device__ __forceinline__ void find_bin(SelectLds &L, uint64_t target, uint32_t count0, uint64_t mass0) {
+  constexpr int kPer = kBins / kSelThreads;
   const int t = threadIdx.x;
-  uint32_t c[4];
-  uint64_t m[4];
-  uint32_t cs = 0;
-  uint64_t ms = 0;
+  uint32_t c[kPer], cs = 0;
+  uint64_t m[kPer], ms = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c[i] = L.hist.count[4 * t + i];
-    m[i] = L.hist.mass[4 * t + i];
+  for (int i = 0; i < kPer; ++i) {
+    c[i] = L.hist.count[kPer * t + i];
+    m[i] = L.hist.mass[kPer * t + i];
     cs += c[i];
     ms += m[i];
   }
   if (t == 0) L.found = -1;
   const BlockScan<uint32_t> bc = block_scan<kSelWaves>(cs, L.red32);
-  const BlockScan<uint64_t> bm = block_scan<kSelWaves>(ms, reinterpret_cast<uint64_t *>(L.red64));
+  const BlockScan<uint64_t> bm = block_scan<kSelWaves>(ms, L.red64);
   uint32_t nc = count0 + bc.excl;
   uint64_t nm = mass0 + bm.excl;
   const uint64_t before = MASS ? nm : nc, after = MASS ? mass0 + bm.incl : count0 + bc.incl;
   if (before < target && target <= after) {
     bool done = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kPer; ++i) {
       const uint64_t next = MASS ? nm + m[i] : nc + c[i];
       if (!done && next >= target) {
         done = true;
-        L.found = 4 * t + i;
+        L.found = kPer * t + i;
         L.found_before = nc;
         L.found_count = c[i];
         L.mass_before = nm;
@@ -216,73 +239,379 @@ __device__ __forceinline__ void clear_hist(SelectLds &L) {
   __syncthreads();
 }
 
-// Tokens that a cut keeps: those with a larger key, and the first `ties` of
-// those with this key.
+// A token's place in its row's order: larger packed values come first.
+__device__ __forceinline__ uint64_t packed(uint32_t key, uint32_t id) { return (uint64_t(key) << 32) | uint32_t(~id); }
+constexpr uint64_t kEvery = uint64_t(kKeyNegInf + 1) << 32;  // below every token that is not masked
+
+// The last kept token of a row, and the weight of all kept ones.
 struct Cut {
-  uint32_t key, ties;
-  uint64_t mass;  // of what it keeps, in units of 2^-40 of the largest weight
+  uint64_t at;
+  uint64_t mass;  // in units of 2^-40 of the largest weight
 };
 constexpr float kFixed = 1099511627776.0f;  // 2^40: 2^22 weights of at most 1 stay below 2^63
+__device__ __forceinline__ unsigned long long fixed_weight(float w) { return (unsigned long long)(w * kFixed + 0.5f); }
+
+// Keys of a row that a thread holds: 5 x 8 consecutive places of each tile of
+// 20,480 groups (one tile up to V = 163,840), the first tile from the start on.
+constexpr int kKeyLoads = 5;
+constexpr uint32_t kTile = kKeyLoads * 8 * kSelThreads;
+struct KeyTile {
+  uint4 q[kKeyLoads];
+  // `places` keys of the row (a multiple of 1,024); missing ones are 0
+  __device__ __forceinline__ void load(const uint16_t *keys, uint32_t places, uint32_t base) {
+#pragma unroll
+    for (int j = 0; j < kKeyLoads; ++j) {
+      const uint32_t at = base + 8 * (uint32_t(j) * kSelThreads + threadIdx.x);
+      q[j] = *reinterpret_cast<const uint4 *>(keys + min(at, places - 8));
+      if (at >= places) q[j] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  // f(key, place) on every key
+  template <typename F>
+  __device__ __forceinline__ void each(uint32_t base, F f) const {
+#pragma unroll
+    for (int j = 0; j < kKeyLoads; ++j) {
+      // opaque to the compiler, which would otherwise keep all 40 unpacked keys and
+      // places of one use for the next (and spill)
+      uint32_t at = base + 8 * (uint32_t(j) * kSelThreads + threadIdx.x);
+      uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
+      asm volatile("" : "+v"(at), "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f((w[i / 2] >> (16 * (i & 1))) & 0xffffu, at + i);
+    }
+  }
+};
+
+static_assert(DSDE_MAX_VOCAB / kChunk <= kSelThreads, "one chunk per thread at most");
+static_assert(DSDE_MAX_VOCAB <= kMostSegs << 10, "segments of the cuts fit the LDS array");
 
 template <int DT, int ROW>
 struct Selector {
-  const SelectArgs &a;
   const char *row;
   const uint16_t *keys;
-  uint32_t V, ng;
+  uint32_t V, ng, places;
   float m, c;
   SelectLds &L;
+  KeyTile tile;          // the first tile's keys
+  bool listed = false;     // the groups to look at are in L.list
+  bool min_bound = false;  // they are those that min_p may keep
 
   __device__ __forceinline__ float weight(float z) const { return row_weight(z, m, c); }
 
-  // Calls f(key, weight) on every finite logit of the groups that reach the key `lo` (16 bits).
+  // f(tile, base) on every tile of keys
   template <typename F>
-  __device__ __forceinline__ void each(uint32_t lo, F f) {
-    for (uint32_t w = threadIdx.x; w < ng; w += kSelThreads) {
-      if (keys[w] < lo) continue;
+  __device__ __forceinline__ void tiles(F f) {
+    f(tile, 0u);
+    for (uint32_t base = kTile; base < places; base += kTile) {
+      KeyTile x;
+      x.load(keys, places, base);
+      f(x, base);
+    }
+  }
+
+  // Writes the groups whose key reaches kappa to `out` (as far as they fit) and
+  // returns how many there are, in every thread.
+  __device__ __forceinline__ uint32_t groups_reaching(uint32_t kappa, uint32_t *out, uint32_t most) {
+    if (threadIdx.x == 0) L.n_groups = 0;
+    __syncthreads();
+    tiles([&](const KeyTile &x, uint32_t base) {
+      uint32_t n = 0;
+      x.each(base, [&](uint32_t k, uint32_t) { n += k >= kappa; });
+      if (__ballot(n != 0) == 0) return;
+      const lanes::Scan<uint32_t> sc = lanes::wave_scan(n);
+      uint32_t at = 0;
+      if ((threadIdx.x & 63) == 63) at = atomicAdd(&L.n_groups, sc.incl);
+      at = lanes::readlane(at, 63) + sc.excl;
+      x.each(base, [&](uint32_t k, uint32_t q) {
+        if (k >= kappa) {
+          if (at < most) out[at] = place_group(q);
+          ++at;
+        }
+      });
+    });
+    __syncthreads();
+    return L.n_groups;
+  }
+
+  // A key that at least `need` groups reach: the need-th largest of the
+  // threads' largest keys.  (Of 512 threads, 64 with a key that reaches it hold about 69 such
+  // keys, and 256 about 355.)  kAll when fewer threads than that hold a finite one.
+  __device__ __forceinline__ uint32_t threshold(uint32_t need) {
+    uint32_t top = 0;
+    tiles([&](const KeyTile &x, uint32_t base) { x.each(base, [&](uint32_t k, uint32_t) { top = max(top, k); }); });
+    L.narrow.tmax[threadIdx.x] = top;
+    __syncthreads();
+    uint32_t v[kSelWaves];
+#pragma unroll
+    for (int j = 0; j < kSelWaves; ++j) v[j] = L.narrow.tmax[64 * j + (threadIdx.x & 63)];
+    uint32_t kappa = 0;
+    for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int j = 0; j < kSelWaves; ++j) n += __popcll(__ballot(v[j] >= (kappa | bit)));
+      if (n >= need) kappa |= bit;
+    }
+    return max(kappa, kAll);
+  }
+
+  // The largest key that at least `need` groups reach, or kAll.
+  __device__ __forceinline__ uint32_t exact_threshold(uint32_t need) {
+    uint32_t kappa = 0;
+    for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+      uint32_t n = 0;
+      tiles([&](const KeyTile &x, uint32_t base) { x.each(base, [&](uint32_t k, uint32_t) { n += k >= (kappa | bit); }); });
+      if (block_reduce<kSelWaves>(n, L.red32, lanes::Add{}) >= need) kappa |= bit;
+    }
+    return max(kappa, kAll);
+  }
+
+  // The logits that reach kappa, one per thread, in the row's order.  -1 when
+  // there are more groups or logits than threads.
+  __device__ __forceinline__ int32_t gather(uint32_t kappa, uint64_t *sorted) {
+    const int t = threadIdx.x;
+    const uint32_t n_groups = groups_reaching(kappa, L.narrow.groups, kCand);
+    if (n_groups > kCand) return -1;
+    uint32_t key[kGroup], n = 0, w = 0;
+    if (uint32_t(t) < n_groups) {
+      w = L.narrow.groups[t];
       Group<DT, ROW> g;
       g.get(row, V, w);
       g.place(V, w);
 #pragma unroll
-      for (int i = 0; i < kGroup; ++i) {
-        const uint32_t key = order_key(g.at(i));
-        if (key > kKeyNegInf) f(key, g.at(i));
+      for (int e = 0; e < kGroup; ++e) {
+        key[e] = order_key(g.at(e));
+        n += key[e] >> 16 >= kappa;
+      }
+    }
+    const BlockScan<uint32_t> sc = block_scan<kSelWaves>(n, L.red32);
+    if (sc.total > kCand) return -1;
+    if (n) {
+      uint32_t at = sc.excl;
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e)
+        if (key[e] >> 16 >= kappa) L.cand[at++] = (uint64_t(key[e]) << 32) | uint32_t(~(w * kGroup + e));
+    }
+    __syncthreads();
+    uint64_t v = uint32_t(t) < sc.total ? L.cand[t] : 0;
+    __syncthreads();
+    block_sort(v, sc.total, L.cand);
+    *sorted = v;
+    return int32_t(sc.total);
+  }
+
+  // Calls f(group, its number, whether it counts) on the listed groups, or on all:
+  // then the lanes of a wavefront hold the 64 consecutive groups of one segment.
+  template <typename F>
+  __device__ __forceinline__ void each_group(F f) {
+    const uint32_t n = listed ? L.n_groups : ng;
+    constexpr int kBatch = 4;
+    for (uint32_t i = threadIdx.x & ~63u; i < n; i += kBatch * kSelThreads) {
+      Group<DT, ROW> g[kBatch];
+      uint32_t w[kBatch];
+      const uint32_t j0 = i + (threadIdx.x & 63);
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const uint32_t j = min(j0 + uint32_t(b) * kSelThreads, n - 1);
+        w[b] = listed ? L.list[j] : j;
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) g[b].get(row, V, w[b]);
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        if (i + uint32_t(b) * kSelThreads >= n) break;
+        g[b].place(V, w[b]);
+        f(g[b], w[b], j0 + uint32_t(b) * kSelThreads < n);
       }
     }
   }
-
-  // Tokens that are not masked (this thread's share).
-  __device__ uint32_t unmasked() {
-    uint32_t n = 0;
-    for (uint32_t w = threadIdx.x; w < ng; w += kSelThreads) {
-      Group<DT, ROW> g;
-      g.get(row, V, w);
-      g.place(V, w);
+  // Calls f(key, logit, id) on every logit of those groups that is not masked.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) {
+    each_group([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
 #pragma unroll
-      for (int i = 0; i < kGroup; ++i) n += g.at(i) != -__builtin_inff();
-    }
-    return n;
+      for (int e = 0; e < kGroup; ++e) {
+        const uint32_t key = order_key(g.at(e));
+        if (in && key > kKeyNegInf) f(key, g.at(e), w * kGroup + e);
+      }
+    });
   }
 
-  // The cut at which the running count (or mass) over the whole row reaches the target.
-  // Windows of 4,096 values of the 16-bit key from the row's maximum down: 32
-  // octaves of a logit's size, at bf16's resolution, so that bf16 rows are done
-  // and few logits share a bin; fp32 rows look into the bin twice more.
-  // Integer masses add up to the same bits in any order.
+  // Lists the groups that reach `low`; where they are too many, all are looked at.
+  __device__ __forceinline__ void list_groups(uint32_t low) {
+    listed = groups_reaching(low, L.list, kList) <= uint32_t(kList);
+  }
+
+  // The bin of a logit on a scale of its weight: equal logits share one, and larger
+  // ones never come behind smaller ones.
+  __device__ __forceinline__ uint32_t weight_bin(float z) const {
+    return uint32_t(fminf((m - z) * c * float(kPerOctave), float(kBins)));
+  }
+
+  // Lists the groups that may hold a token above the cuts, from the groups'
+  // largest keys.  k groups whose largest lies in the first b bins bound a
+  // count of k; and the weight outside the first b bins is at most that of eight
+  // logits like the largest for each group that begins behind them and of
+  // seven at their edge for each other: where that is less than what top_p leaves out, the cut lies inside.
+  __device__ __forceinline__ void list_relevant(int32_t k, float p, float S, uint32_t min_key) {
+    constexpr int kPer = kBins / kSelThreads;
+    const int t = threadIdx.x;
+    clear_hist(L);
+    tiles([&](const KeyTile &x, uint32_t base) {
+      x.each(base, [&](uint32_t key, uint32_t) {
+        if (key < kAll) return;
+        const uint32_t b = weight_bin(fminf(key_logit((key << 16) | 0xffffu), m));
+        if (b < uint32_t(kBins)) atomicAdd(&L.hist.count[b], 1u);
+      });
+    });
+    if (t == 0) L.found = kBins;
+    __syncthreads();
+    uint32_t n[kPer], own = 0;
+    float mass = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      n[i] = L.hist.count[kPer * t + i];
+      own += n[i];
+      mass += float(n[i]) * fast_exp2(-float(kPer * t + i) / kPerOctave);
+    }
+    const BlockScan<uint32_t> sn = block_scan<kSelWaves>(own, L.red32);
+    const BlockScan<float> sm = block_scan<kSelWaves>(mass, L.redf);
+    uint32_t before = sn.excl;
+    float behind = sm.total - sm.excl + float(ng) * fast_exp2(-float(kBins) / kPerOctave);
+    const float spare = 0.99f * (1.f - p) * S;
+    int32_t best = kBins;
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i) {
+      // the first b = kPer t + i + 1 bins
+      uint32_t inside = before;
+      float rest = behind;
+      for (int j = 0; j <= i; ++j) {
+        inside += n[j];
+        rest -= float(n[j]) * fast_exp2(-float(kPer * t + j) / kPerOctave);
+      }
+      const float edge = fast_exp2(-float(kPer * t + i + 1) / kPerOctave);
+      const bool ok = k > 0 ? inside >= uint32_t(k) : p < 1.f && 8.f * fmaxf(rest, 0.f) + 7.f * float(inside) * edge +
+                                                                    1e-5f * S <= spare;
+      if (ok) best = kPer * t + i + 1;
+    }
+    if (best < kBins) atomicMin(&L.found, best);
+    __syncthreads();
+    const int32_t b = L.found;
+    uint32_t low = kAll;
+    if (b < kBins) {
+      const float d = float(b + 1) / (kPerOctave * c);  // a bin more than needed, for its rounding
+      low = max(low, order_key(m - d - 1e-5f * (fabsf(m) + d)) >> 16);
+    }
+    min_bound = min_key > low && !(k > 0 && p < 1.f);  // (top_p's share there is of all top_k's weight)
+    if (min_bound) low = min_key;
+    __syncthreads();
+    list_groups(low);
+  }
+
+  // Counts and weights of the listed logits by bin.  Integer weights add up to
+  // the same bits in any order.
+  __device__ __forceinline__ void histogram() {
+    clear_hist(L);
+    each([&](uint32_t, float z, uint32_t) {
+      const uint32_t b = weight_bin(z);
+      if (b < uint32_t(kBins)) {
+        atomicAdd(&L.hist.count[b], 1u);
+        atomicAdd(&L.hist.mass[b], fixed_weight(weight(z)));
+      }
+    });
+    __syncthreads();
+  }
+
+  // The cut at which the running count (or weight) reaches the target, from
+  // the histogram and the logits of one bin, sorted.  With `last`, the segments'
+  // weights of what it and min_p keep are left in LDS.
   template <bool MASS>
-  __device__ Cut find_cut(uint64_t target) {
+  __device__ __forceinline__ Cut weight_cut(uint64_t target, bool last, float min_p, int32_t *kept) {
+    const int t = threadIdx.x;
+    find_bin<MASS>(L, target, 0, 0);
+    const int32_t bin = L.found;
+    const uint32_t in_bin = L.found_count;
+    const uint64_t count0 = L.found_before, mass0 = L.mass_before;
+    __syncthreads();
+    Cut cut;
+    if (bin < 0 && min_bound) {  // min_p's tokens, which are listed, end before the cut
+      if (last) add_segments(kEvery, min_p, kept);
+      return Cut{kEvery, 0};
+    }
+    if (bin < 0 || in_bin > uint32_t(kCand)) {
+      // outside the histogram's range, or a long run of nearly equal logits
+      cut = key_cut<MASS>(target);
+      if (last)
+        add_segments(cut.at, min_p, kept);
+      else
+        histogram();
+      return cut;
+    }
+    if (t == 0) L.n_cand = 0;
+    if (last) clear_segments();
+    __syncthreads();
+    int32_t n = 0;
+    each_group([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
+      unsigned long long sum = 0;
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) {
+        const float z = g.at(e);
+        const uint32_t b = weight_bin(z);
+        if (in && b <= uint32_t(bin)) {
+          if (b == uint32_t(bin)) {
+            L.cand[atomicAdd(&L.n_cand, 1u)] = packed(order_key(z), w * kGroup + e);
+          } else if (last) {
+            const float x = weight(z);
+            if (x >= min_p) {
+              sum += fixed_weight(x);
+              ++n;
+            }
+          }
+        }
+      }
+      if (last) add_segment(w, sum);
+    });
+    __syncthreads();
+    uint64_t v = uint32_t(t) < in_bin ? L.cand[t] : 0;
+    __syncthreads();
+    block_sort(v, in_bin, L.cand);
+    const float x = uint32_t(t) < in_bin ? weight(key_logit(uint32_t(v >> 32))) : 0.f;
+    const uint64_t f = fixed_weight(x);
+    const BlockScan<uint64_t> sc = block_scan<kSelWaves>(uint32_t(t) < in_bin ? f : 0, L.red64);
+    const uint32_t end = MASS ? min(uint32_t(__syncthreads_count(uint32_t(t) < in_bin && mass0 + sc.incl < target)), in_bin - 1)
+                              : uint32_t(target - count0) - 1;
+    if (uint32_t(t) == end) {
+      L.cut = v;
+      L.mass_before = mass0 + sc.incl;
+    }
+    if (last && uint32_t(t) <= end && x >= min_p) {
+      const uint32_t id = ~uint32_t(v);
+      atomicAdd(&L.segs[id >> seg_shift], (unsigned long long)f);
+      ++n;
+    }
+    __syncthreads();
+    cut.at = L.cut;
+    cut.mass = L.mass_before;
+    __syncthreads();
+    if (last) *kept = n;
+    return cut;
+  }
+
+  // The same cut by the logits' keys, for any row, in windows of 2,048 values of the keys' upper
+  // halves from the maximum down (16 octaves of a logit's size, at bf16's
+  // resolution), then, in fp32, by the rest of the key; among equal logits by their ids.
+  template <bool MASS>
+  __device__ __forceinline__ Cut key_cut(uint64_t target) {
     const uint32_t km = order_key(m) >> 16;
     uint32_t count0 = 0, key = 0;
     uint64_t mass0 = 0;
     for (uint32_t off0 = 0;; off0 += kBins) {
-      if (off0 > km) return Cut{kKeyNegInf, 0, mass0};  // every finite logit
+      if (off0 > km) return Cut{kEvery, mass0};
       clear_hist(L);
-      const uint32_t end = off0 + kBins;
-      each(km >= end ? km - end + 1 : 0, [&](uint32_t k, float z) {
+      each([&](uint32_t k, float z, uint32_t) {
         const uint32_t b = km - (k >> 16) - off0;
-        if (b < kBins) {
+        if (b < uint32_t(kBins)) {
           atomicAdd(&L.hist.count[b], 1u);
-          atomicAdd(&L.hist.mass[b], (unsigned long long)(weight(z) * kFixed + 0.5f));
+          atomicAdd(&L.hist.mass[b], fixed_weight(weight(z)));
         }
       });
       __syncthreads();
@@ -297,225 +626,210 @@ struct Selector {
       }
     }
     if constexpr (DT == DSDE_FP32) {
-      // the next 12 bits, then the last 4
+      // the next 11 bits, then the last 5
       for (int last = 0; last < 2; ++last) {
-        const uint32_t prefix = key, below = last ? 4 : 16, shift = last ? 0 : 4, most = last ? 15 : kBins - 1;
+        const uint32_t prefix = key, below = last ? 5 : 16, shift = last ? 0 : 5, most = last ? 31 : kBins - 1;
         clear_hist(L);
-        each(last ? prefix >> 12 : prefix, [&](uint32_t k, float z) {
+        each([&](uint32_t k, float z, uint32_t) {
           if (k >> below == prefix) {
             const uint32_t b = most - ((k >> shift) & most);
             atomicAdd(&L.hist.count[b], 1u);
-            atomicAdd(&L.hist.mass[b], (unsigned long long)(weight(z) * kFixed + 0.5f));
+            atomicAdd(&L.hist.mass[b], fixed_weight(weight(z)));
           }
         });
         __syncthreads();
         find_bin<MASS>(L, target, count0, mass0);
         count0 = L.found_before;
         mass0 = L.mass_before;
-        key = (prefix << (last ? 4 : 12)) | (most - uint32_t(L.found));
+        key = (prefix << (last ? 5 : 11)) | (most - uint32_t(L.found));
         __syncthreads();
       }
     } else {
       key = (key << 16) | ((key & 0x8000u) ? 0u : 0xffffu);
     }
     const uint32_t in_bin = L.found_count;
-    const uint64_t unit = L.mass_count / in_bin;
+    const uint64_t unit = L.mass_count / in_bin;  // the bin's logits are equal
     uint64_t ties = target - (MASS ? mass0 : count0);
     if (MASS) ties = unit ? (ties + unit - 1) / unit : in_bin;
     if (ties > in_bin) ties = in_bin;
     __syncthreads();
-    return Cut{key, uint32_t(ties), mass0 + ties * unit};
+    return Cut{packed(key, tie_id(key, uint32_t(ties))), mass0 + ties * unit};
   }
 
-  // Ties (and, for a draw, weights above the cut) of every segment, into LDS.
-  // Returns how many tokens above the cut this thread kept.
-  template <bool WEIGHTS>
-  __device__ int32_t scan_segments(const Cut &cut, float min_p, int32_t nseg) {
-    const int t = threadIdx.x, lane = t & 63;
-    int32_t count = 0;
-    for (int32_t s = t >> 6; s < nseg; s += kSelWaves) {
-      const uint32_t w = uint32_t(s) * 64 + lane;
-      uint32_t ties = 0;
-      float sum = 0.f;
-      if (w < ng) {
+  // The id of the n-th token, in id order, whose key is this (there are as many).
+  __device__ __forceinline__ uint32_t tie_id(uint32_t key, uint32_t n) {
+    const int t = threadIdx.x;
+    clear_segments();
+    each([&](uint32_t k, float, uint32_t id) {
+      if (k == key) atomicAdd(&L.segs[id >> seg_shift], 1ull);
+    });
+    __syncthreads();
+    const int32_t per = (nseg + kSelThreads - 1) / kSelThreads, s0 = t * per, s1 = min(s0 + per, nseg);
+    uint32_t own = 0;
+    for (int32_t i = s0; i < s1; ++i) own += uint32_t(L.segs[i]);
+    uint32_t before = block_scan<kSelWaves>(own, L.red32).excl;
+    for (int32_t i = s0; i < s1; ++i) {
+      const uint32_t x = uint32_t(L.segs[i]);
+      if (before < n && n <= before + x) {
+        L.seg = i;
+        L.seg_ties = before;
+      }
+      before += x;
+    }
+    __syncthreads();
+    if (t < 64) {
+      uint32_t rank = L.seg_ties;
+      for (uint32_t b = 0; b < 1u << (seg_shift - 9); ++b) {
+        const uint32_t w = ((uint32_t(L.seg) << (seg_shift - 9)) + b) * 64 + t;
         Group<DT, ROW> g;
-        g.get(row, V, w);
-        g.place(V, w);
+        g.get(row, V, min(w, ng - 1));
+        g.place(V, min(w, ng - 1));
+        uint32_t here = 0;
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) {
-          const uint32_t key = order_key(g.at(i));
-          ties += key == cut.key;
-          if (WEIGHTS) {
-            const float e = weight(g.at(i));
-            const bool in = key > cut.key && e >= min_p;
-            sum += in ? e : 0.f;
-            count += in;
-          }
-        }
-      }
-      ties = lanes::wave_sum(ties);
-      if (WEIGHTS) sum = lanes::wave_sum(sum);
-      if (lane == 0) {
-        L.segs.ties[s] = uint16_t(ties);
-        if (WEIGHTS) L.segs.weight[s] = sum;
+        for (int e = 0; e < kGroup; ++e) here += w < ng && order_key(g.at(e)) == key;
+        const lanes::Scan<uint32_t> sc = lanes::wave_scan(here);
+        uint32_t at = rank + sc.excl;
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e)
+          if (w < ng && order_key(g.at(e)) == key && ++at == n) L.found_count = w * kGroup + e;
+        rank += lanes::readlane(sc.incl, 63);
       }
     }
     __syncthreads();
-    return count;
+    const uint32_t id = L.found_count;
+    __syncthreads();
+    return id;
   }
 
-  // The inverse-CDF draw over segment weights: the last segment of positive
-  // weight whose exclusive prefix is at most u times the total.  weight_of(s, ties
-  // before s) gives a segment's weight; ties_of(s) its ties.  Leaves the segment,
-  // the ties before it and the weight left in LDS.
-  template <typename WF, typename TF>
-  __device__ void draw_segment(int32_t nseg, float u, WF weight_of, TF ties_of) {
-    const int t = threadIdx.x;
-    const int32_t per = (nseg + kSelThreads - 1) / kSelThreads;  // consecutive segments of one thread
-    const int32_t s0 = t * per, s1 = min(s0 + per, nseg);
-    uint32_t ties = 0;
-    for (int32_t s = s0; s < s1; ++s) ties += ties_of(s);
-    const uint32_t ties0 = block_scan<kSelWaves>(ties, L.red32).excl;
-    double w = 0.0;
-    uint32_t before = ties0;
-    for (int32_t s = s0; s < s1; ++s) {
-      w += weight_of(s, before);
-      before += ties_of(s);
-    }
-    if (t == 0) L.seg = -1;
-    const BlockScan<double> bw = block_scan<kSelWaves>(w, L.red64);
-    const double target = double(u) * bw.total;
-    int32_t best = -1;
-    uint32_t best_ties = 0;
-    double best_rem = 0.0;
-    double at = bw.excl;
-    before = ties0;
-    for (int32_t s = s0; s < s1; ++s) {
-      const double x = weight_of(s, before);
-      if (x > 0.0 && at <= target) {
-        best = s;
-        best_ties = before;
-        best_rem = target - at;
-      }
-      at += x;
-      before += ties_of(s);
-    }
-    if (best >= 0) atomicMax(&L.seg, best);
-    __syncthreads();
-    if (best >= 0 && L.seg == best) {
-      L.seg_ties = best_ties;
-      L.target = best_rem;
-    }
+  // Segments of the cuts: 512 logits, or as many more as keep them within the LDS array.
+  __device__ __forceinline__ void clear_segments() {
+    seg_shift = V <= 512u * kMostSegs ? 9 : 10;
+    nseg = int32_t((V + (1u << seg_shift) - 1) >> seg_shift);
+    for (int32_t i = threadIdx.x; i < nseg; i += kSelThreads) L.segs[i] = 0;
     __syncthreads();
   }
-
-  // The token of the chosen segment, by wavefront 0: keep(key, weight, tie
-  // rank) says whether a logit belongs to the kept set.  Every lane returns (token, logit).
-  template <typename K>
-  __device__ void draw_token(K keep, uint32_t tie_key, int32_t *token, float *logit) {
-    const int lane = threadIdx.x & 63;
-    const uint32_t w = uint32_t(L.seg) * 64 + lane;
-    Group<DT, ROW> g;
-    g.get(row, V, min(w, ng - 1));
-    g.place(V, min(w, ng - 1));
-    uint32_t ties = 0;
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) ties += w < ng && order_key(g.at(i)) == tie_key;
-    uint32_t rank = L.seg_ties + lanes::wave_scan(ties).excl;
-    float e[kGroup];
-    double sum = 0.0;
-    int last = -1;
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) {
-      const uint32_t key = order_key(g.at(i));
-      const float x = weight(g.at(i));
-      e[i] = w < ng && key > kKeyNegInf && keep(key, x, rank) ? x : 0.f;
-      rank += key == tie_key;
-      sum += double(e[i]);
-      if (e[i] > 0.f) last = i;
+  // Adds a group's weight to its segment.  Where all groups are looked at, the
+  // wavefront's 64 lie in one segment and are added first.
+  __device__ __forceinline__ void add_segment(uint32_t w, unsigned long long sum) {
+    if (!listed) {
+      sum = lanes::wave_sum(uint64_t(sum));
+      if ((threadIdx.x & 63) != 0) return;
     }
-    const lanes::Scan<double> sc = lanes::wave_scan(sum);
-    const double rem = L.target;
-    const uint64_t can = __ballot(last >= 0 && sc.excl <= rem);
-    const int winner = can ? 63 - __builtin_clzll(can) : 0;
-    int pick = last >= 0 ? last : 0;
-    double acc = sc.excl;
-    bool done = false;
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) {
-      acc += double(e[i]);
-      if (!done && acc > rem) {
-        pick = i;
-        done = true;
-      }
-    }
-    float z = g.at(0);
-#pragma unroll
-    for (int i = 1; i < kGroup; ++i)
-      if (pick == i) z = g.at(i);
-    *token = lanes::readlane(int32_t(w * kGroup) + pick, winner);
-    *logit = lanes::readlane(z, winner);
+    if (sum) atomicAdd(&L.segs[w >> (seg_shift - 3)], sum);
   }
-
-  // The groups that reach a key, and from them the logits that do, sorted in
-  // the row's order.  -1 when there are more than one per thread.
-  __device__ int32_t gather(uint32_t kappa, uint64_t *sorted) {
-    const int t = threadIdx.x;
-    if (t == 0) L.n_groups = L.n_cand = 0;
-    __syncthreads();
-    for (uint32_t w = t; w < ng; w += kSelThreads)
-      if (keys[w] >= kappa) {
-        const uint32_t i = atomicAdd(&L.n_groups, 1u);
-        if (i < kCand) L.list.groups[i] = w;
-      }
-    __syncthreads();
-    if (L.n_groups > kCand) return -1;
-    if (uint32_t(t) < L.n_groups) {
-      const uint32_t w = L.list.groups[t];
-      Group<DT, ROW> g;
-      g.get(row, V, w);
-      g.place(V, w);
+  // Weights of every segment under a cut and min_p, and this thread's share of the kept tokens.
+  __device__ __forceinline__ void add_segments(uint64_t cut, float min_p, int32_t *kept) {
+    clear_segments();
+    int32_t n = 0;
+    each_group([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
+      unsigned long long sum = 0;
 #pragma unroll
       for (int e = 0; e < kGroup; ++e) {
-        const uint32_t key = order_key(g.at(e));
-        if (key >> 16 >= kappa) {
-          const uint32_t i = atomicAdd(&L.n_cand, 1u);
-          if (i < kCand) L.list.cand[i] = (uint64_t(key) << 32) | uint32_t(~(w * kGroup + e));
+        const float x = weight(g.at(e));
+        if (in && packed(order_key(g.at(e)), w * kGroup + e) >= cut && x >= min_p) {
+          sum += fixed_weight(x);
+          ++n;
         }
       }
-    }
+      add_segment(w, sum);
+    });
     __syncthreads();
-    const uint32_t n = L.n_cand;
-    if (n > kCand) return -1;
-    uint64_t v = uint32_t(t) < n ? L.list.cand[t] : 0;
-    __syncthreads();
-    *sorted = block_sort(v, sort_width(n), L.list.cand);
-    return int32_t(n);
+    *kept = n;
   }
 
-  // The largest 16-bit key that at least `need` groups reach (kAll when fewer
-  // than that lie in the histogram's window).
-  static constexpr uint32_t kAll = (kKeyNegInf >> 16) + 1;  // every finite logit
-  __device__ uint32_t threshold(uint32_t need) {
-    const uint32_t km = order_key(m) >> 16;
-    clear_hist(L);
-    for (uint32_t w = threadIdx.x; w < ng; w += kSelThreads) {
-      const uint32_t b = km - keys[w];
-      if (b < kBins) atomicAdd(&L.hist.count[b], 1u);
+  // The segment of the draw: the last one of positive weight whose exclusive
+  // prefix is at most u times the total.  Leaves it and the weight left in LDS.
+  template <typename WF>
+  __device__ __forceinline__ void draw_segment(int32_t n, float u, WF weight_of) {
+    const int t = threadIdx.x;
+    const int32_t per = (n + kSelThreads - 1) / kSelThreads;  // consecutive segments of one thread
+    const int32_t s0 = t * per, s1 = min(s0 + per, n);
+    double w = 0.0;
+    for (int32_t s = s0; s < s1; ++s) w += weight_of(s);
+    if (t == 0) L.seg = -1;
+    const BlockScan<double> bw = block_scan<kSelWaves>(w, reinterpret_cast<double *>(L.red64));
+    const double target = double(u) * bw.total;
+    int32_t best = -1;
+    double rem = 0.0, at = bw.excl;
+    if (w > 0.0 && at <= target)
+      for (int32_t s = s0; s < s1; ++s) {
+        const double x = weight_of(s);
+        if (x > 0.0 && at <= target) {
+          best = s;
+          rem = target - at;
+        }
+        at += x;
+      }
+    if (best >= 0) atomicMax(&L.seg, best);
+    __syncthreads();
+    if (best >= 0 && L.seg == best) L.rem = rem;
+    __syncthreads();
+  }
+
+  // The token of the drawn segment of `blocks` times 64 groups, by one
+  // wavefront, among those above the cut that min_p keeps.  Every lane returns (token, logit).
+  __device__ __forceinline__ void draw_token(int32_t blocks, uint64_t cut, float min_p, int32_t *token, float *logit) {
+    const int lane = threadIdx.x & 63;
+    double base = 0.0;
+    const double rem = L.rem;
+    *token = 0;
+    *logit = 0.f;
+    for (int32_t b = 0; b < blocks; ++b) {
+      const uint32_t w = uint32_t(L.seg * blocks + b) * 64 + lane;
+      if (w - lane >= ng) break;
+      Group<DT, ROW> g;
+      g.get(row, V, min(w, ng - 1));
+      g.place(V, min(w, ng - 1));
+      float e[kGroup];
+      double sum = 0.0;
+      int last = -1;
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) {
+        const float x = weight(g.at(i));
+        e[i] = w < ng && packed(order_key(g.at(i)), w * kGroup + i) >= cut && x >= min_p ? x : 0.f;
+        sum += double(e[i]);
+        if (e[i] > 0.f) last = i;
+      }
+      const lanes::Scan<double> sc = lanes::wave_scan(sum);
+      const uint64_t can = __ballot(last >= 0 && base + sc.excl <= rem);
+      if (can) {  // a later block takes over where it begins at or before the place
+        const int winner = 63 - __builtin_clzll(can);
+        int pick = last >= 0 ? last : 0;
+        double acc = base + sc.excl;
+        bool done = false;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+          acc += double(e[i]);
+          if (!done && acc > rem) {
+            pick = i;
+            done = true;
+          }
+        }
+        float z = g.at(0);
+#pragma unroll
+        for (int i = 1; i < kGroup; ++i)
+          if (pick == i) z = g.at(i);
+        *token = lanes::readlane(int32_t(w * kGroup) + pick, winner);
+        *logit = lanes::readlane(z, winner);
+      }
+      base += lanes::readlane(sc.incl, 63);
     }
-    __syncthreads();
-    find_bin<false>(L, need, 0, 0);
-    const int32_t f = L.found;
-    __syncthreads();
-    if (f < 0) return kAll;
-    const uint32_t k = km - uint32_t(f);
-    return k < kAll ? kAll : k;
+  }
+
+  int32_t nseg;
+  uint32_t seg_shift;
+
+  // Tokens that are not masked (this thread's share).
+  __device__ __forceinline__ uint32_t unmasked() {
+    uint32_t n = 0;
+    each([&](uint32_t, float, uint32_t) { ++n; });
+    return n;
   }
 };
 
 // One row per workgroup.
 template <int DT, int ROW, bool TOP>
-__global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
+__global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
   __shared__ SelectLds L;
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x, out = row0 + r;
@@ -523,14 +837,21 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a,
   const float *cmax = a.scan.max + r * nc;
   const float *seg = a.scan.seg + r * nc * kSegs;
   const int32_t nseg = nc * kSegs;
-
-  float mt = -INFINITY;
-  bool bad = false;
-  for (int32_t i = t; i < nc; i += kSelThreads) {
-    const float x = cmax[i];
-    bad |= !(x < INFINITY);
-    mt = fmaxf(mt, x);
+  const uint32_t V = uint32_t(a.V);
+  Selector<DT, ROW> sel{a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup,
+                        uint32_t(nc) * kChunkGroups, 0.f, s.c, L, {}, false, false, 0, 9};
+  // the loads that the kernel starts with, together
+  float first_max = -INFINITY, first_seg = 0.f, first_ref = -INFINITY;
+  if (t < nc) first_max = cmax[t];
+  if (t < nseg) {
+    first_seg = seg[t];
+    first_ref = cmax[t / kSegs];
   }
+  if (TOP || s.filtered) sel.tile.load(sel.keys, sel.places, 0);
+
+  float mt = first_max;
+  bool bad = !(mt < INFINITY);
+  // (a row has at most 512 chunks: one per thread)
   bad = __syncthreads_or(bad);
   const float m = block_reduce<kSelWaves>(mt, L.redf, lanes::Max{});
   const uint32_t err = s.err | (bad || m == -INFINITY ? DSDE_ERR_LOGIT : 0u);
@@ -549,12 +870,12 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a,
     }
     return;
   }
-  double part = 0.0;
-  for (int32_t i = t; i < nseg; i += kSelThreads) part += double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c));
-  const double S = block_reduce<kSelWaves>(part, L.red64, lanes::Add{});
-
-  const uint32_t V = uint32_t(a.V);
-  Selector<DT, ROW> sel{a, a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup, m, s.c, L};
+  sel.m = m;
+  const double part0 = double(first_seg) * double(row_weight(first_ref, m, s.c));
+  double part = part0;
+  for (int32_t i = t + kSelThreads; i < nseg; i += kSelThreads)
+    part += double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c));
+  const double S = block_reduce<kSelWaves>(part, reinterpret_cast<double *>(L.red64), lanes::Add{});
 
   auto emit = [&](int32_t token, float z, int32_t kept) {
     a.tokens[out] = token;
@@ -565,52 +886,26 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a,
   if constexpr (TOP) {
     if (t == 0) a.lse[out] = float(double(m) / double(s.T) + log(S));
     const int32_t k = a.one_k;
-    const uint32_t kappa = sel.threshold(uint32_t(k));
     uint64_t v = 0;
-    int32_t n = sel.gather(kappa, &v);
+    int32_t n = sel.gather(sel.threshold(uint32_t(k)), &v);
     if (n < 0) {
-      const Cut cut = sel.template find_cut<false>(uint64_t(k));
-      sel.template scan_segments<false>(cut, 0.f, nseg);
-      // ties before every segment, clamped (at most k <= 256 of them are taken)
-      const int32_t per = (nseg + kSelThreads - 1) / kSelThreads, s0 = t * per, s1 = min(s0 + per, nseg);
-      uint32_t ties = 0;
-      for (int32_t i = s0; i < s1; ++i) ties += L.segs.ties[i];
-      uint32_t before = block_scan<kSelWaves>(ties, L.red32).excl;
-      for (int32_t i = s0; i < s1; ++i) {
-        const uint32_t x = L.segs.ties[i];
-        L.segs.ties[i] = uint16_t(min(before, 65535u));
-        before += x;
-      }
+      // more logits than threads reach that threshold: long runs of equal or nearby ones
+      sel.list_groups(sel.exact_threshold(uint32_t(k)));
+      const uint64_t cut = sel.template key_cut<false>(uint64_t(k)).at;
       if (t == 0) L.n_cand = 0;
       __syncthreads();
-      uint64_t *picked = reinterpret_cast<uint64_t *>(L.segs.weight);  // not used here: 8 KB of its 32
-      for (int32_t i = t >> 6; i < nseg; i += kSelWaves) {
-        const uint32_t w = uint32_t(i) * 64 + (t & 63);
-        uint32_t key[kGroup], own = 0;
-        Group<DT, ROW> g;
-        g.get(sel.row, V, min(w, sel.ng - 1));
-        g.place(V, min(w, sel.ng - 1));
-#pragma unroll
-        for (int e = 0; e < kGroup; ++e) {
-          key[e] = w < sel.ng ? order_key(g.at(e)) : 0u;
-          own += key[e] == cut.key;
+      sel.each([&](uint32_t key, float, uint32_t id) {
+        const uint64_t x = packed(key, id);
+        if (x >= cut) {
+          const uint32_t i = atomicAdd(&L.n_cand, 1u);
+          if (i < kCand) L.cand[i] = x;
         }
-        uint32_t rank = L.segs.ties[i] + lanes::wave_scan(own).excl;
-#pragma unroll
-        for (int e = 0; e < kGroup; ++e) {
-          const bool tie = key[e] == cut.key;
-          if (key[e] > kKeyNegInf && (key[e] > cut.key || (tie && rank < cut.ties))) {
-            const uint32_t j = atomicAdd(&L.n_cand, 1u);
-            if (j < kCand) picked[j] = (uint64_t(key[e]) << 32) | uint32_t(~(w * kGroup + e));
-          }
-          rank += tie;
-        }
-      }
+      });
       __syncthreads();
       n = int32_t(min(L.n_cand, uint32_t(kCand)));
-      v = t < n ? picked[t] : 0;
+      v = t < n ? L.cand[t] : 0;
       __syncthreads();
-      v = block_sort(v, sort_width(uint32_t(n)), picked);
+      block_sort(v, uint32_t(n), L.cand);
     }
     if (t < k) {
       a.values[out * k + t] = t < n ? key_logit(uint32_t(v >> 32)) : -INFINITY;
@@ -622,97 +917,93 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a,
       const uint32_t n = a.kept ? block_reduce<kSelWaves>(sel.unmasked(), L.red32, lanes::Add{}) : 0u;
       sel.draw_segment(
           nseg, s.u,
-          [&](int32_t i, uint32_t) { return double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c)); },
-          [](int32_t) { return 0u; });
+          [&](int32_t i) {
+            return i == t ? part0 : double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c));
+          });
       if (t < 64) {
         int32_t token;
         float z;
-        sel.draw_token([](uint32_t, float, uint32_t) { return true; }, 0u, &token, &z);
+        sel.draw_token(1, kEvery, 0.f, &token, &z);
         if (t == 0) emit(token, z, int32_t(n));
       }
       return;
     }
 
-    // candidates: a prefix of the row's order
-    const uint32_t need = s.k > 0 && s.k < kNeed ? uint32_t(s.k) : uint32_t(kNeed);
-    uint32_t kappa = sel.threshold(need);
-    bool min_decided = false;
+    // A little below the smallest logit that min_p keeps, as a key.
+    uint32_t min_key = 0;
     if (s.m > 0.f) {
-      // a little below the smallest logit that min_p keeps
-      const float d = log2f(s.m) / s.c, z = m + d - 1e-5f * (1.f + fabsf(m) + fabsf(d));
-      const uint32_t low = order_key(z) >> 16;
-      if (low >= kappa) {
-        kappa = low;
-        min_decided = true;
-      }
+      const float d = log2f(s.m) / s.c;
+      min_key = order_key(m + d - 1e-5f * (1.f + fabsf(m) + fabsf(d))) >> 16;
     }
-    const bool all = kappa == sel.kAll;
-    uint64_t v = 0;
-    const int32_t n = sel.gather(kappa, &v);
-    int32_t kept = kUndecided;
-    if (n >= 0) {
-      const float e = t < n ? sel.weight(key_logit(uint32_t(v >> 32))) : 0.f;
-      const BlockScan<double> cs = block_scan<kSelWaves>(double(e), L.red64);
-      const bool k_in = s.k > 0 && s.k <= n;
-      if (k_in && t == s.k - 1) L.mass = cs.incl;
-      const int32_t n_min = __syncthreads_count(t < n && e >= s.m);
-      const double mass = k_in ? L.mass : all ? cs.total : S;
-      const int32_t n_below = __syncthreads_count(t < n && cs.incl < double(s.p) * mass);
-      int32_t lim = kUndecided;
-      if (k_in) lim = s.k;
-      if (all) lim = min(lim, n);
-      if (s.m > 0.f && (n_min < n || all || min_decided)) lim = min(lim, n_min);
-      bool known = true;
-      if (s.p < 1.f) {
-        known = k_in || all || s.k == 0;
-        if (n_below < n) lim = min(lim, n_below + 1);
+    // Few tokens kept: candidates, a prefix of the row's order, sorted.  Where its
+    // length does not settle every filter, four times as many, then the cuts below.
+    const bool small_k = s.k > 0 && s.k <= kMostNeed;
+    for (uint32_t need = small_k ? s.k : kFirstNeed;; need = kMostNeed) {
+      uint32_t kappa = sel.threshold(need);
+      const bool min_decided = min_key >= kappa;
+      if (min_decided) kappa = min_key;
+      const bool all = kappa == kAll;
+      uint64_t v = 0;
+      const int32_t n = sel.gather(kappa, &v);
+      int32_t kept = kUndecided;
+      if (n >= 0) {
+        const float e = t < n ? sel.weight(key_logit(uint32_t(v >> 32))) : 0.f;
+        const BlockScan<double> cs = block_scan<kSelWaves>(double(e), reinterpret_cast<double *>(L.red64));
+        const bool k_in = s.k > 0 && s.k <= n;
+        if (k_in && t == s.k - 1) L.mass = cs.incl;
+        const int32_t n_min = __syncthreads_count(t < n && e >= s.m);
+        const double mass = k_in ? L.mass : all ? cs.total : S;
+        const int32_t n_below = __syncthreads_count(t < n && cs.incl < double(s.p) * mass);
+        int32_t lim = kUndecided;
+        if (k_in) lim = s.k;
+        if (all) lim = min(lim, n);
+        if (s.m > 0.f && (n_min < n || all || min_decided)) lim = min(lim, n_min);
+        bool known = true;
+        if (s.p < 1.f) {
+          known = k_in || all || s.k == 0;  // else top_p's share is of a mass beyond the candidates
+          if (n_below < n) lim = min(lim, n_below + 1);
+        }
+        if (known && lim != kUndecided) kept = max(lim, 1);
       }
-      if (known && lim != kUndecided) kept = max(lim, 1);
-    }
-    if (kept != kUndecided) {
-      // the draw walks the kept tokens in the order of their ids
-      const uint32_t id = ~uint32_t(v);
-      const float e = t < kept ? sel.weight(key_logit(uint32_t(v >> 32))) : 0.f;
-      uint64_t x = t < kept ? (uint64_t(~id) << 32) | __float_as_uint(e) : 0;
-      if (kept > 1) x = block_sort(x, sort_width(uint32_t(kept)), L.list.cand);
-      const float ex = __uint_as_float(uint32_t(x));
-      const BlockScan<double> cs = block_scan<kSelWaves>(double(ex), L.red64);
-      const int32_t at = min(__syncthreads_count(t < kept && cs.incl <= double(s.u) * cs.total), kept - 1);
-      if (t == at) {
-        const int32_t token = int32_t(~uint32_t(x >> 32));
-        emit(token, load_logit(sel.row, DT, token), kept);
+      if (kept != kUndecided) {
+        // the draw walks the kept tokens in the order of their ids
+        const uint32_t id = ~uint32_t(v);
+        const float e = t < kept ? sel.weight(key_logit(uint32_t(v >> 32))) : 0.f;
+        uint64_t x = t < kept ? (uint64_t(~id) << 32) | __float_as_uint(e) : 0;
+        if (kept > 1) block_sort(x, uint32_t(kept), L.cand);
+        const BlockScan<double> cs =
+            block_scan<kSelWaves>(double(__uint_as_float(uint32_t(x))), reinterpret_cast<double *>(L.red64));
+        const int32_t at = min(__syncthreads_count(t < kept && cs.incl <= double(s.u) * cs.total), kept - 1);
+        if (t == at) {
+          const int32_t token = int32_t(~uint32_t(x >> 32));
+          emit(token, load_logit(sel.row, DT, token), kept);
+        }
+        return;
       }
-      return;
+      __syncthreads();
+      if (small_k || need == uint32_t(kMostNeed)) break;
     }
 
-    // more tokens than candidates: cuts over the whole row
-    __syncthreads();
-    Cut cut{kKeyNegInf, 0, uint64_t(S * double(kFixed))};
-    if (s.k > 0) cut = sel.template find_cut<false>(uint64_t(s.k));
-    if (s.p < 1.f) {
+    // More tokens: cuts by histograms over the groups that may hold them.
+    int32_t n_above = 0;
+    sel.list_relevant(s.k, s.p, float(S), min_key);
+    Cut cut{kEvery, uint64_t(S * double(kFixed))};
+    const bool by_p = s.p < 1.f;
+    sel.histogram();
+    if (s.k > 0) cut = sel.template weight_cut<false>(uint64_t(s.k), !by_p, s.m, &n_above);
+    if (by_p) {
       const uint64_t target = uint64_t(double(s.p) * double(cut.mass));
-      cut = sel.template find_cut<true>(target ? target : 1);
+      cut = sel.template weight_cut<true>(target ? target : 1, true, s.m, &n_above);
+    } else if (s.k == 0) {
+      sel.add_segments(kEvery, s.m, &n_above);
     }
-    const int32_t above = sel.template scan_segments<true>(cut, s.m, nseg);
-    const uint32_t count = block_reduce<kSelWaves>(uint32_t(above), L.red32, lanes::Add{});
-    const float tie_weight = sel.weight(key_logit(cut.key));
-    const uint32_t tie_limit = tie_weight >= s.m ? cut.ties : 0u;
-    auto ties_of = [&](int32_t i) { return uint32_t(L.segs.ties[i]); };
-    auto weight_of = [&](int32_t i, uint32_t before) {
-      const uint32_t left = before < tie_limit ? tie_limit - before : 0u, here = ties_of(i);
-      return double(L.segs.weight[i]) + double(tie_weight) * double(here < left ? here : left);
-    };
-    sel.draw_segment(nseg, s.u, weight_of, ties_of);
+    const uint32_t count = block_reduce<kSelWaves>(uint32_t(n_above), L.red32, lanes::Add{});
+    sel.draw_segment(sel.nseg, s.u, [&](int32_t i) { return double(L.segs[i]) * (1.0 / double(kFixed)); });
     if (t < 64) {
       int32_t token;
       float z;
-      const float min_p = s.m;
-      sel.draw_token(
-          [&](uint32_t key, float e, uint32_t rank) {
-            return e >= min_p && (key > cut.key || (key == cut.key && rank < tie_limit));
-          },
-          cut.key, &token, &z);
-      if (t == 0) emit(token, z, int32_t(count + tie_limit));
+      sel.draw_token(1 << (sel.seg_shift - 9), cut.at, s.m, &token, &z);
+      if (t == 0) emit(token, z, int32_t(count));
     }
   }
 }
