@@ -17,11 +17,11 @@ namespace {
 constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
 constexpr int kCand = kSelThreads;  // candidates that the select kernel sorts, one per thread
 constexpr int kMostNeed = 256;      // groups asked for at most: about 1.4 times as many reach their threshold
-constexpr int kFirstNeed = 64;      // groups that a row without a top-k asks for
+constexpr int kFirstNeed = 56;      // groups that a row without a top-k asks for: about 60 candidates, one wavefront's sort
 constexpr int kBins = 2048;
 constexpr int kPerOctave = 64;  // bins per octave of a weight: 32 octaves below the largest
-constexpr int kList = 8192;     // groups in the list of the cuts over many tokens
-constexpr int kMostSegs = 4096;
+constexpr uint32_t kListGroups = 4096;  // groups listed for the cuts over many tokens: about 4,700 logits reach their key
+constexpr int kMostSegs = 2048;
 constexpr int32_t kUndecided = 0x7fffffff;
 
 // One row's settings, checked.  Greedy rows (T = 0) are rows with top_k = 1.
@@ -117,26 +117,29 @@ __device__ __forceinline__ uint32_t place_group(uint32_t q) {
 }
 constexpr uint32_t kAll = (kKeyNegInf >> 16) + 1;  // the smallest key (high half) of a finite logit
 
-// Everything the select kernel keeps in LDS.  The histogram, the segments and
-// the arrays of the narrow search are never needed at once.
-struct SelectLds {
+// Everything the select kernel keeps in LDS, for two workgroups on a CU.  The
+// histogram, the segments, the list of groups and the arrays of the narrow search are never needed at once.
+template <int LIST>
+struct SelectLdsOf {
+  static constexpr uint32_t kList = LIST;
   union {
     struct {
       unsigned long long mass[kBins];
       uint32_t count[kBins];
     } hist;
     unsigned long long segs[kMostSegs];
+    uint32_t list[LIST];
     struct {
       uint32_t groups[kCand];
       uint32_t tmax[kSelThreads];
     } narrow;
   };
   uint64_t cand[kCand];
-  uint32_t list[kList];
+  uint64_t elems[LIST];
   uint64_t red64[kSelWaves];
   uint32_t red32[kSelWaves];
   float redf[kSelWaves];
-  uint32_t n_groups, n_cand;
+  uint32_t n_groups, n_cand, n_elems;
   int32_t found;
   uint32_t found_before, found_count;
   uint64_t mass_before, mass_count;
@@ -145,6 +148,9 @@ struct SelectLds {
   uint32_t seg_ties;
   uint64_t cut;
 };
+// Two workgroups of the draw fit on a CU, and three of the top logits, which hardly ever need the lists.
+template <bool TOP>
+using SelectLds = SelectLdsOf<TOP ? 2048 : 6144>;
 
 // The value of lane ^ STRIDE.
 template <int STRIDE>
@@ -187,8 +193,8 @@ __device__ __forceinline__ void block_sort(uint64_t &v, uint32_t n, uint64_t *ld
 // with MASS) reaches the target, given the totals before its first bin.  Leaves
 // found, found_before / found_count and mass_before / mass_count; found = -1
 // when the window does not reach it, with the totals behind it in *_before.
-template <bool MASS>
-__device__ __forceinline__ void find_bin(SelectLds &L, uint64_t target, uint32_t count0, uint64_t mass0) {
+template <bool MASS, typename LDS>
+__device__ __forceinline__ void find_bin(LDS &L, uint64_t target, uint32_t count0, uint64_t mass0) {
   constexpr int kPer = kBins / kSelThreads;
   const int t = threadIdx.x;
   uint32_t c[kPer], cs = 0;
@@ -231,7 +237,8 @@ __device__ __forceinline__ void find_bin(SelectLds &L, uint64_t target, uint32_t
   __syncthreads();
 }
 
-__device__ __forceinline__ void clear_hist(SelectLds &L) {
+template <typename LDS>
+__device__ __forceinline__ void clear_hist(LDS &L) {
   for (int i = threadIdx.x; i < kBins; i += kSelThreads) {
     L.hist.count[i] = 0;
     L.hist.mass[i] = 0;
@@ -266,6 +273,16 @@ struct KeyTile {
       if (at >= places) q[j] = make_uint4(0, 0, 0, 0);
     }
   }
+  __device__ __forceinline__ uint32_t largest() const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < kKeyLoads; ++j)
+#pragma unroll
+      for (uint32_t w : {q[j].x, q[j].y, q[j].z, q[j].w})
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w));
+    return m.x > m.y ? m.x : m.y;
+  }
   // f(key, place) on every key
   template <typename F>
   __device__ __forceinline__ void each(uint32_t base, F f) const {
@@ -283,17 +300,17 @@ struct KeyTile {
 };
 
 static_assert(DSDE_MAX_VOCAB / kChunk <= kSelThreads, "one chunk per thread at most");
-static_assert(DSDE_MAX_VOCAB <= kMostSegs << 10, "segments of the cuts fit the LDS array");
+static_assert(DSDE_MAX_VOCAB <= kMostSegs << 11, "segments of the cuts fit the LDS array");
 
-template <int DT, int ROW>
+template <int DT, int ROW, typename LDS>
 struct Selector {
   const char *row;
   const uint16_t *keys;
   uint32_t V, ng, places;
   float m, c;
-  SelectLds &L;
+  LDS &L;
   KeyTile tile;          // the first tile's keys
-  bool listed = false;     // the groups to look at are in L.list
+  bool listed = false;     // the logits to look at are in L.elems
   bool min_bound = false;  // they are those that min_p may keep
 
   __device__ __forceinline__ float weight(float z) const { return row_weight(z, m, c); }
@@ -338,7 +355,7 @@ struct Selector {
   // keys, and 256 about 355.)  kAll when fewer threads than that hold a finite one.
   __device__ __forceinline__ uint32_t threshold(uint32_t need) {
     uint32_t top = 0;
-    tiles([&](const KeyTile &x, uint32_t base) { x.each(base, [&](uint32_t k, uint32_t) { top = max(top, k); }); });
+    tiles([&](const KeyTile &x, uint32_t) { top = max(top, x.largest()); });
     L.narrow.tmax[threadIdx.x] = top;
     __syncthreads();
     uint32_t v[kSelWaves];
@@ -399,21 +416,17 @@ struct Selector {
     return int32_t(sc.total);
   }
 
-  // Calls f(group, its number, whether it counts) on the listed groups, or on all:
-  // then the lanes of a wavefront hold the 64 consecutive groups of one segment.
-  template <typename F>
-  __device__ __forceinline__ void each_group(F f) {
-    const uint32_t n = listed ? L.n_groups : ng;
+  // Calls f(group, its number, whether it counts) on the groups that list(i) names,
+  // or on all, in order: then the lanes of a wavefront hold the 64 groups of one segment.
+  template <typename F, typename I>
+  __device__ __forceinline__ void each_group(uint32_t n, I list, F f) {
     constexpr int kBatch = 4;
     for (uint32_t i = threadIdx.x & ~63u; i < n; i += kBatch * kSelThreads) {
       Group<DT, ROW> g[kBatch];
       uint32_t w[kBatch];
       const uint32_t j0 = i + (threadIdx.x & 63);
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const uint32_t j = min(j0 + uint32_t(b) * kSelThreads, n - 1);
-        w[b] = listed ? L.list[j] : j;
-      }
+      for (int b = 0; b < kBatch; ++b) w[b] = list(min(j0 + uint32_t(b) * kSelThreads, n - 1));
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) g[b].get(row, V, w[b]);
 #pragma unroll
@@ -424,21 +437,58 @@ struct Selector {
       }
     }
   }
-  // Calls f(key, logit, id) on every logit of those groups that is not masked.
+  template <typename F>
+  __device__ __forceinline__ void all_groups(F f) {
+    each_group(ng, [](uint32_t i) { return i; }, f);
+  }
+  // Calls f(key, logit, id) on the listed logits, or on all that are not masked.
   template <typename F>
   __device__ __forceinline__ void each(F f) {
-    each_group([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
-#pragma unroll
-      for (int e = 0; e < kGroup; ++e) {
-        const uint32_t key = order_key(g.at(e));
-        if (in && key > kKeyNegInf) f(key, g.at(e), w * kGroup + e);
+    if (listed) {
+      for (uint32_t i = threadIdx.x; i < L.n_elems; i += kSelThreads) {
+        const uint64_t x = L.elems[i];
+        f(uint32_t(x >> 32), key_logit(uint32_t(x >> 32)), ~uint32_t(x));
       }
-    });
+    } else {
+      all_groups([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) {
+          const uint32_t key = order_key(g.at(e));
+          if (in && key > kKeyNegInf) f(key, g.at(e), w * kGroup + e);
+        }
+      });
+    }
   }
 
-  // Lists the groups that reach `low`; where they are too many, all are looked at.
-  __device__ __forceinline__ void list_groups(uint32_t low) {
-    listed = groups_reaching(low, L.list, kList) <= uint32_t(kList);
+  // Lists the logits that reach `low` (a key's upper half); where they, or their
+  // groups, are too many, all logits are looked at.
+  __device__ __forceinline__ void list_logits(uint32_t low) {
+    const uint32_t n = groups_reaching(low, L.list, LDS::kList);
+    listed = n <= LDS::kList;
+    if (!listed) return;
+    if (threadIdx.x == 0) L.n_elems = 0;
+    __syncthreads();
+    const uint32_t least = low << 16;
+    each_group(n, [&](uint32_t i) { return L.list[i]; }, [&](const Group<DT, ROW> &g, uint32_t w, bool in) {
+      uint32_t key[kGroup], own = 0;
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) {
+        key[e] = order_key(g.at(e));
+        own += in && key[e] >= least;
+      }
+      const lanes::Scan<uint32_t> sc = lanes::wave_scan(own);
+      uint32_t at = 0;
+      if ((threadIdx.x & 63) == 63) at = atomicAdd(&L.n_elems, sc.incl);
+      at = lanes::readlane(at, 63) + sc.excl;
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e)
+        if (in && key[e] >= least) {
+          if (at < LDS::kList) L.elems[at] = packed(key[e], w * kGroup + e);
+          ++at;
+        }
+    });
+    __syncthreads();
+    listed = L.n_elems <= LDS::kList;
   }
 
   // The bin of a logit on a scale of its weight: equal logits share one, and larger
@@ -447,11 +497,11 @@ struct Selector {
     return uint32_t(fminf((m - z) * c * float(kPerOctave), float(kBins)));
   }
 
-  // Lists the groups that may hold a token above the cuts, from the groups'
-  // largest keys.  k groups whose largest lies in the first b bins bound a
-  // count of k; and the weight outside the first b bins is at most that of eight
-  // logits like the largest for each group that begins behind them and of
-  // seven at their edge for each other: where that is less than what top_p leaves out, the cut lies inside.
+  // Lists the logits from which the cuts are found, from the groups' largest
+  // keys.  Any key will do whose logits turn out to hold the cut (weight_cut
+  // looks): k groups whose largest lies in the first b bins do for a count of
+  // k; for a weight, the first bins whose groups' largest alone weigh enough, or else the most
+  // bins that the lists have room for.
   __device__ __forceinline__ void list_relevant(int32_t k, float p, float S, uint32_t min_key) {
     constexpr int kPer = kBins / kSelThreads;
     const int t = threadIdx.x;
@@ -471,27 +521,19 @@ struct Selector {
     for (int i = 0; i < kPer; ++i) {
       n[i] = L.hist.count[kPer * t + i];
       own += n[i];
-      mass += float(n[i]) * fast_exp2(-float(kPer * t + i) / kPerOctave);
+      mass += float(n[i]) * fast_exp2(-float(kPer * t + i + 1) / kPerOctave);
     }
     const BlockScan<uint32_t> sn = block_scan<kSelWaves>(own, L.red32);
     const BlockScan<float> sm = block_scan<kSelWaves>(mass, L.redf);
-    uint32_t before = sn.excl;
-    float behind = sm.total - sm.excl + float(ng) * fast_exp2(-float(kBins) / kPerOctave);
-    const float spare = 0.99f * (1.f - p) * S;
+    uint32_t inside = sn.excl;
+    float weighs = sm.excl;
     int32_t best = kBins;
 #pragma unroll
-    for (int i = kPer - 1; i >= 0; --i) {
-      // the first b = kPer t + i + 1 bins
-      uint32_t inside = before;
-      float rest = behind;
-      for (int j = 0; j <= i; ++j) {
-        inside += n[j];
-        rest -= float(n[j]) * fast_exp2(-float(kPer * t + j) / kPerOctave);
-      }
-      const float edge = fast_exp2(-float(kPer * t + i + 1) / kPerOctave);
-      const bool ok = k > 0 ? inside >= uint32_t(k) : p < 1.f && 8.f * fmaxf(rest, 0.f) + 7.f * float(inside) * edge +
-                                                                    1e-5f * S <= spare;
-      if (ok) best = kPer * t + i + 1;
+    for (int i = 0; i < kPer; ++i) {  // the first kPer t + i + 1 bins
+      inside += n[i];
+      weighs += float(n[i]) * fast_exp2(-float(kPer * t + i + 1) / kPerOctave);
+      const bool ok = k > 0 ? inside >= uint32_t(k) : (p < 1.f && weighs >= 1.00001f * p * S) || inside >= kListGroups;
+      if (ok && best == kBins) best = kPer * t + i + 1;
     }
     if (best < kBins) atomicMin(&L.found, best);
     __syncthreads();
@@ -501,23 +543,33 @@ struct Selector {
       const float d = float(b + 1) / (kPerOctave * c);  // a bin more than needed, for its rounding
       low = max(low, order_key(m - d - 1e-5f * (fabsf(m) + d)) >> 16);
     }
-    min_bound = min_key > low && !(k > 0 && p < 1.f);  // (top_p's share there is of all top_k's weight)
-    if (min_bound) low = min_key;
+    // (with both, top_p's share is of all top_k's weight; with neither, min_p alone decides)
+    min_bound = k > 0 ? min_key > low && p >= 1.f : min_key > low || p >= 1.f;
+    if (min_bound) low = max(min_key, kAll);
     __syncthreads();
-    list_groups(low);
+    list_logits(low);
   }
 
   // Counts and weights of the listed logits by bin.  Integer weights add up to
   // the same bits in any order.
   __device__ __forceinline__ void histogram() {
     clear_hist(L);
-    each([&](uint32_t, float z, uint32_t) {
-      const uint32_t b = weight_bin(z);
-      if (b < uint32_t(kBins)) {
+    auto add = [&](float z) {
+      const float d = (m - z) * c;
+      if (d < float(kBins / kPerOctave)) {
+        const uint32_t b = uint32_t(d * float(kPerOctave));
         atomicAdd(&L.hist.count[b], 1u);
-        atomicAdd(&L.hist.mass[b], fixed_weight(weight(z)));
+        atomicAdd(&L.hist.mass[b], fixed_weight(fast_exp2(-d)));
       }
-    });
+    };
+    if (listed)
+      each([&](uint32_t, float z, uint32_t) { add(z); });
+    else
+      all_groups([&](const Group<DT, ROW> &g, uint32_t, bool in) {
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e)
+          if (in) add(g.at(e));
+      });
     __syncthreads();
   }
 
@@ -528,6 +580,12 @@ struct Selector {
   __device__ __forceinline__ Cut weight_cut(uint64_t target, bool last, float min_p, int32_t *kept) {
     const int t = threadIdx.x;
     find_bin<MASS>(L, target, 0, 0);
+    if (L.found < 0 && listed && !min_bound) {  // the lists were too short
+      listed = false;
+      __syncthreads();
+      histogram();
+      find_bin<MASS>(L, target, 0, 0);
+    }
     const int32_t bin = L.found;
     const uint32_t in_bin = L.found_count;
     const uint64_t count0 = L.found_before, mass0 = L.mass_before;
@@ -550,25 +608,14 @@ struct Selector {
     if (last) clear_segments();
     __syncthreads();
     int32_t n = 0;
-    each_group([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
-      unsigned long long sum = 0;
-#pragma unroll
-      for (int e = 0; e < kGroup; ++e) {
-        const float z = g.at(e);
-        const uint32_t b = weight_bin(z);
-        if (in && b <= uint32_t(bin)) {
-          if (b == uint32_t(bin)) {
-            L.cand[atomicAdd(&L.n_cand, 1u)] = packed(order_key(z), w * kGroup + e);
-          } else if (last) {
-            const float x = weight(z);
-            if (x >= min_p) {
-              sum += fixed_weight(x);
-              ++n;
-            }
-          }
-        }
-      }
-      if (last) add_segment(w, sum);
+    pass([&](float z, uint32_t id, bool in) -> unsigned long long {
+      const uint32_t b = weight_bin(z);
+      if (in && b == uint32_t(bin)) L.cand[atomicAdd(&L.n_cand, 1u)] = packed(order_key(z), id);
+      if (!last) return 0;
+      const float x = weight(z);
+      const bool keep = in && b < uint32_t(bin) && x >= min_p;
+      n += keep;
+      return keep ? fixed_weight(x) : 0ull;
     });
     __syncthreads();
     uint64_t v = uint32_t(t) < in_bin ? L.cand[t] : 0;
@@ -703,35 +750,41 @@ struct Selector {
 
   // Segments of the cuts: 512 logits, or as many more as keep them within the LDS array.
   __device__ __forceinline__ void clear_segments() {
-    seg_shift = V <= 512u * kMostSegs ? 9 : 10;
+    seg_shift = V <= 512u * kMostSegs ? 9 : V <= 1024u * kMostSegs ? 10 : 11;
     nseg = int32_t((V + (1u << seg_shift) - 1) >> seg_shift);
     for (int32_t i = threadIdx.x; i < nseg; i += kSelThreads) L.segs[i] = 0;
     __syncthreads();
   }
-  // Adds a group's weight to its segment.  Where all groups are looked at, the
-  // wavefront's 64 lie in one segment and are added first.
-  __device__ __forceinline__ void add_segment(uint32_t w, unsigned long long sum) {
-    if (!listed) {
-      sum = lanes::wave_sum(uint64_t(sum));
-      if ((threadIdx.x & 63) != 0) return;
+  // Calls f(logit, id, whether it counts) on the listed logits, or on all, and adds the
+  // weights that it returns to their segments.  Where all are looked at, a
+  // wavefront's 64 groups lie in one segment and are added first.
+  template <typename F>
+  __device__ __forceinline__ void pass(F f) {
+    if (listed) {
+      for (uint32_t i = threadIdx.x; i < L.n_elems; i += kSelThreads) {
+        const uint64_t x = L.elems[i];
+        const unsigned long long sum = f(key_logit(uint32_t(x >> 32)), ~uint32_t(x), true);
+        if (sum) atomicAdd(&L.segs[~uint32_t(x) >> seg_shift], sum);
+      }
+    } else {
+      all_groups([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
+        unsigned long long sum = 0;
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) sum += f(g.at(e), w * kGroup + e, in);
+        sum = lanes::wave_sum(uint64_t(sum));
+        if (sum && (threadIdx.x & 63) == 0) atomicAdd(&L.segs[w >> (seg_shift - 3)], sum);
+      });
     }
-    if (sum) atomicAdd(&L.segs[w >> (seg_shift - 3)], sum);
   }
   // Weights of every segment under a cut and min_p, and this thread's share of the kept tokens.
   __device__ __forceinline__ void add_segments(uint64_t cut, float min_p, int32_t *kept) {
     clear_segments();
     int32_t n = 0;
-    each_group([&](const Group<DT, ROW> &g, uint32_t w, bool in) {
-      unsigned long long sum = 0;
-#pragma unroll
-      for (int e = 0; e < kGroup; ++e) {
-        const float x = weight(g.at(e));
-        if (in && packed(order_key(g.at(e)), w * kGroup + e) >= cut && x >= min_p) {
-          sum += fixed_weight(x);
-          ++n;
-        }
-      }
-      add_segment(w, sum);
+    pass([&](float z, uint32_t id, bool in) -> unsigned long long {
+      const float x = weight(z);
+      const bool keep = in && packed(order_key(z), id) >= cut && x >= min_p;
+      n += keep;
+      return keep ? fixed_weight(x) : 0ull;
     });
     __syncthreads();
     *kept = n;
@@ -830,7 +883,7 @@ struct Selector {
 // One row per workgroup.
 template <int DT, int ROW, bool TOP>
 __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
-  __shared__ SelectLds L;
+  __shared__ SelectLds<TOP> L;
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x, out = row0 + r;
   const Setting s = row_setting(a, out);
@@ -838,7 +891,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   const float *seg = a.scan.seg + r * nc * kSegs;
   const int32_t nseg = nc * kSegs;
   const uint32_t V = uint32_t(a.V);
-  Selector<DT, ROW> sel{a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup,
+  Selector<DT, ROW, SelectLds<TOP>> sel{a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup,
                         uint32_t(nc) * kChunkGroups, 0.f, s.c, L, {}, false, false, 0, 9};
   // the loads that the kernel starts with, together
   float first_max = -INFINITY, first_seg = 0.f, first_ref = -INFINITY;
@@ -890,7 +943,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
     int32_t n = sel.gather(sel.threshold(uint32_t(k)), &v);
     if (n < 0) {
       // more logits than threads reach that threshold: long runs of equal or nearby ones
-      sel.list_groups(sel.exact_threshold(uint32_t(k)));
+      sel.list_logits(sel.exact_threshold(uint32_t(k)));
       const uint64_t cut = sel.template key_cut<false>(uint64_t(k)).at;
       if (t == 0) L.n_cand = 0;
       __syncthreads();
@@ -936,10 +989,9 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
       min_key = order_key(m + d - 1e-5f * (1.f + fabsf(m) + fabsf(d))) >> 16;
     }
     // Few tokens kept: candidates, a prefix of the row's order, sorted.  Where its
-    // length does not settle every filter, four times as many, then the cuts below.
-    const bool small_k = s.k > 0 && s.k <= kMostNeed;
-    for (uint32_t need = small_k ? s.k : kFirstNeed;; need = kMostNeed) {
-      uint32_t kappa = sel.threshold(need);
+    // length does not settle every filter, the cuts below.
+    if (s.k <= kMostNeed) {
+      uint32_t kappa = sel.threshold(s.k > 0 ? s.k : kFirstNeed);
       const bool min_decided = min_key >= kappa;
       if (min_decided) kappa = min_key;
       const bool all = kappa == kAll;
@@ -966,22 +1018,28 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
         if (known && lim != kUndecided) kept = max(lim, 1);
       }
       if (kept != kUndecided) {
-        // the draw walks the kept tokens in the order of their ids
-        const uint32_t id = ~uint32_t(v);
-        const float e = t < kept ? sel.weight(key_logit(uint32_t(v >> 32))) : 0.f;
-        uint64_t x = t < kept ? (uint64_t(~id) << 32) | __float_as_uint(e) : 0;
-        if (kept > 1) block_sort(x, uint32_t(kept), L.cand);
-        const BlockScan<double> cs =
-            block_scan<kSelWaves>(double(__uint_as_float(uint32_t(x))), reinterpret_cast<double *>(L.red64));
-        const int32_t at = min(__syncthreads_count(t < kept && cs.incl <= double(s.u) * cs.total), kept - 1);
-        if (t == at) {
-          const int32_t token = int32_t(~uint32_t(x >> 32));
-          emit(token, load_logit(sel.row, DT, token), kept);
+        // the draw walks the kept tokens in the order of their ids; up to 64 of them lie in one wavefront
+        const bool one_wave = kept <= 64;
+        if (one_wave && t >= 64) return;
+        uint64_t x = t < kept ? (v << 32) | uint32_t(t) : 0;  // (~id, rank)
+        if (!one_wave) L.elems[t] = v;
+        block_sort(x, uint32_t(kept), L.cand);
+        const uint32_t key = one_wave ? __shfl(uint32_t(v >> 32), int(uint32_t(x)))
+                                      : uint32_t(L.elems[uint32_t(x)] >> 32);
+        const float z = key_logit(key);
+        const double e = t < kept ? double(sel.weight(z)) : 0.0;
+        int32_t at;
+        if (one_wave) {
+          const double incl = lanes::wave_scan(e).incl, total = lanes::readlane(incl, 63);
+          at = __popcll(__ballot(t < kept && incl <= double(s.u) * total));
+        } else {
+          const BlockScan<double> cs = block_scan<kSelWaves>(e, reinterpret_cast<double *>(L.red64));
+          at = __syncthreads_count(t < kept && cs.incl <= double(s.u) * cs.total);
         }
+        if (t == min(at, kept - 1)) emit(int32_t(~uint32_t(x >> 32)), z, kept);
         return;
       }
       __syncthreads();
-      if (small_k || need == uint32_t(kMostNeed)) break;
     }
 
     // More tokens: cuts by histograms over the groups that may hold them.
