@@ -9,16 +9,22 @@ namespace dsde {
 // their rows in several passes.  The cap also keeps a pass's keys (an eighth of
 // its logits) inside the last-level cache.
 constexpr size_t kSelectBytes = size_t(192) << 20;
+// A row left to the cuts over many tokens, with its maximum and the weight of all its logits.
+struct WideRow {
+  int32_t row;
+  float max;
+  double sum;
+};
 inline size_t select_row_bytes(int64_t V) {
-  return size_t(num_chunks(V)) * (sizeof(float) * (1 + kSegs) + sizeof(uint16_t) * kChunkGroups);
+  return size_t(num_chunks(V)) * (sizeof(float) * (1 + kSegs) + sizeof(uint16_t) * kChunkGroups) + sizeof(WideRow);
 }
 inline int64_t select_rows_per_pass(int64_t R, int64_t V) {
   const int64_t n = int64_t(kSelectBytes / select_row_bytes(V));
   return n < R ? n : R;
 }
-static_assert(kSelectBytes >= (DSDE_MAX_VOCAB / kChunk) * (4 * (1 + kSegs) + 2 * kChunkGroups), "one row fits");
+static_assert(kSelectBytes >= (DSDE_MAX_VOCAB / kChunk) * (4 * (1 + kSegs) + 2 * kChunkGroups) + sizeof(WideRow), "one row fits");
 struct SelectLayout {
-  size_t max, seg, keys, total;
+  size_t max, seg, keys, wide, n_wide, total;
 };
 inline SelectLayout select_layout(int64_t R, int64_t V) {
   const size_t n = size_t(select_rows_per_pass(R, V)) * size_t(num_chunks(V));
@@ -27,7 +33,9 @@ inline SelectLayout select_layout(int64_t R, int64_t V) {
   l.max = 0;
   l.seg = l.max + align_up(sizeof(float) * n);
   l.keys = l.seg + align_up(sizeof(float) * kSegs * n);
-  l.total = (all < kSelectBytes ? align_up(all) : kSelectBytes) + 3 * 256;  // grows with R and with V
+  l.wide = l.keys + align_up(sizeof(uint16_t) * kChunkGroups * n);
+  l.n_wide = l.wide + align_up(sizeof(WideRow) * size_t(select_rows_per_pass(R, V)));
+  l.total = (all < kSelectBytes ? align_up(all) : kSelectBytes) + 6 * 256;  // grows with R and with V
   return l;
 }
 
@@ -46,6 +54,8 @@ struct SelectArgs {
     float *max;      // [R, nc] largest logit of each chunk; NaN: a NaN in it
     float *seg;      // [R, nc, 16] weights of its segments against that
     uint16_t *keys;  // [R, nc, 1024] high halves of its groups' largest ordered keys
+    WideRow *wide;   // [*n_wide] rows left to wide_kernel
+    uint32_t *n_wide;
   } scan;
   void *workspace;
   uint32_t *row_err;

@@ -1,26 +1,27 @@
 // Sampling (temperature, top-k, top-p, min-p) and the k largest logits of rows.
 //
 // Both order a row by (logit descending, id ascending) and need its first
-// tokens: the kept set of every filter is a prefix of that order.  A scan kernel
-// reads each row once, at one workgroup per chunk of 8,192 logits, and leaves
-// per chunk its maximum, the weight of each of its 16 segments of 512 logits, and the
-// 16-bit ordered key of the maximum of each group of 8 logits: an eighth of the
-// row's length in keys.  A select kernel, one workgroup per row, finds from the keys alone a
-// threshold that at least `need` groups reach; the logits that reach it, a few
-// more than `need`, are all in those groups, which it reads again, sorts, and cuts.
+// tokens: the kept set of every filter is a prefix of that order.
+//   row_scan_kernel  reads each row once, one workgroup per chunk of 8,192 logits, and
+//                    leaves per chunk its maximum, the weight of each of its 16 segments
+//                    of 512 logits, and the 16-bit ordered key of the largest logit of each
+//                    group of 8: an eighth of the row's length in keys;
+//   select_kernel    one workgroup per row: draws without filters from the segments'
+//                    weights; else finds from the keys alone a threshold that enough groups
+//                    reach, reads those groups again, sorts the few logits that reach it too, and cuts;
+//   wide_kernel      rows whose filters keep more tokens than that: cuts by histograms.
 #include "rows.hpp"
 #include "rows_args.hpp"
 
 namespace dsde {
 namespace {
 
-constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
-constexpr int kCand = kSelThreads;  // candidates that the select kernel sorts, one per thread
+constexpr int kSelThreads = 512;    // threads per row of the select kernel,
+constexpr int kWideThreads = 1024;  // and of the cuts over many tokens
 constexpr int kMostNeed = 256;      // groups asked for at most: about 1.4 times as many reach their threshold
 constexpr int kFirstNeed = 56;      // groups that a row without a top-k asks for: about 60 candidates, one wavefront's sort
 constexpr int kBins = 2048;
 constexpr int kPerOctave = 64;  // bins per octave of a weight: 32 octaves below the largest
-constexpr uint32_t kListGroups = 4096;  // groups listed for the cuts over many tokens: about 4,700 logits reach their key
 constexpr int kMostSegs = 2048;
 constexpr int32_t kUndecided = 0x7fffffff;
 
@@ -99,6 +100,7 @@ __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, 
   // segment 4 i + wave of the chunk: groups 256 i + 64 wave ...
   if (lane < 4) a.scan.seg[unit * kSegs + 4 * lane + wave] = total;
   if (t == 0) a.scan.max[unit] = bad ? NAN : M;
+  if (t == 0 && unit == 0) *a.scan.n_wide = 0;
   if (a.keys_always || s.filtered) {
     // a thread's four keys together: group 256 i + t of the chunk at place 4 t + i (place_group)
     const uint32_t lo = (order_key(gm[0]) >> 16) | (order_key(gm[1]) & 0xffff0000u);
@@ -117,28 +119,26 @@ __device__ __forceinline__ uint32_t place_group(uint32_t q) {
 }
 constexpr uint32_t kAll = (kKeyNegInf >> 16) + 1;  // the smallest key (high half) of a finite logit
 
-// Everything the select kernel keeps in LDS, for two workgroups on a CU.  The
-// histogram, the segments, the list of groups and the arrays of the narrow search are never needed at once.
-template <int LIST>
+// What a workgroup of T threads keeps in LDS.  The histogram, the segments, the list of GROUPS
+// groups and the arrays of the search for few tokens are never needed at once.
+template <int T, int BINS, int GROUPS, int ELEMS>
 struct SelectLdsOf {
-  static constexpr uint32_t kList = LIST;
+  static constexpr int kThreads = T, kWaves = T / 64;
+  static constexpr uint32_t kGroups = GROUPS, kElems = ELEMS;
   union {
     struct {
-      unsigned long long mass[kBins];
-      uint32_t count[kBins];
+      unsigned long long mass[BINS];
+      uint32_t count[BINS];
     } hist;
-    unsigned long long segs[kMostSegs];
-    uint32_t list[LIST];
-    struct {
-      uint32_t groups[kCand];
-      uint32_t tmax[kSelThreads];
-    } narrow;
+    unsigned long long segs[BINS];
+    uint32_t list[GROUPS];
+    uint32_t tmax[T];
   };
-  uint64_t cand[kCand];
-  uint64_t elems[LIST];
-  uint64_t red64[kSelWaves];
-  uint32_t red32[kSelWaves];
-  float redf[kSelWaves];
+  uint64_t cand[T];  // what the workgroup sorts, one per thread
+  uint64_t elems[ELEMS];
+  uint64_t red64[kWaves];
+  uint32_t red32[kWaves];
+  float redf[kWaves];
   uint32_t n_groups, n_cand, n_elems;
   int32_t found;
   uint32_t found_before, found_count;
@@ -148,9 +148,13 @@ struct SelectLdsOf {
   uint32_t seg_ties;
   uint64_t cut;
 };
-// Two workgroups of the draw fit on a CU, and three of the top logits, which hardly ever need the lists.
-template <bool TOP>
-using SelectLds = SelectLdsOf<TOP ? 2048 : 6144>;
+// The draw's select kernel has no histogram; the top logits', whose rows hardly ever need one, keeps the
+// whole of it and short lists (45 KB: three workgroups per CU).  The cuts over many tokens take one CU.
+using DrawLds = SelectLdsOf<kSelThreads, 1, kSelThreads, kSelThreads>;
+using TopLds = SelectLdsOf<kSelThreads, kBins, 2048, 2048>;
+using WideLds = SelectLdsOf<kWideThreads, kBins, 8192, 12288>;
+static_assert(kBins == kMostSegs, "one array holds either");
+static_assert(sizeof(WideLds) <= 160 * 1024, "LDS of a CU");
 
 // The value of lane ^ STRIDE.
 template <int STRIDE>
@@ -181,11 +185,11 @@ __device__ __forceinline__ void sort_steps(uint64_t &v, uint64_t *lds) {
 // smallest power of two >= n, at least 2; the others pass through): a
 // bitonic network whose partners inside one wavefront exchange by DPP moves
 // and shuffles, others through LDS.
-template <int SIZE = 2>
+template <int T, int SIZE = 2>
 __device__ __forceinline__ void block_sort(uint64_t &v, uint32_t n, uint64_t *lds) {
   sort_steps<SIZE, SIZE / 2>(v, lds);
-  if constexpr (SIZE < kSelThreads) {
-    if (n > SIZE) block_sort<SIZE * 2>(v, n, lds);
+  if constexpr (SIZE < T) {
+    if (n > SIZE) block_sort<T, SIZE * 2>(v, n, lds);
   }
 }
 
@@ -195,7 +199,7 @@ __device__ __forceinline__ void block_sort(uint64_t &v, uint32_t n, uint64_t *ld
 // when the window does not reach it, with the totals behind it in *_before.
 template <bool MASS, typename LDS>
 __device__ __forceinline__ void find_bin(LDS &L, uint64_t target, uint32_t count0, uint64_t mass0) {
-  constexpr int kPer = kBins / kSelThreads;
+  constexpr int kPer = kBins / LDS::kThreads;
   const int t = threadIdx.x;
   uint32_t c[kPer], cs = 0;
   uint64_t m[kPer], ms = 0;
@@ -207,8 +211,8 @@ __device__ __forceinline__ void find_bin(LDS &L, uint64_t target, uint32_t count
     ms += m[i];
   }
   if (t == 0) L.found = -1;
-  const BlockScan<uint32_t> bc = block_scan<kSelWaves>(cs, L.red32);
-  const BlockScan<uint64_t> bm = block_scan<kSelWaves>(ms, L.red64);
+  const BlockScan<uint32_t> bc = block_scan<LDS::kWaves>(cs, L.red32);
+  const BlockScan<uint64_t> bm = block_scan<LDS::kWaves>(ms, L.red64);
   uint32_t nc = count0 + bc.excl;
   uint64_t nm = mass0 + bm.excl;
   const uint64_t before = MASS ? nm : nc, after = MASS ? mass0 + bm.incl : count0 + bc.incl;
@@ -239,7 +243,7 @@ __device__ __forceinline__ void find_bin(LDS &L, uint64_t target, uint32_t count
 
 template <typename LDS>
 __device__ __forceinline__ void clear_hist(LDS &L) {
-  for (int i = threadIdx.x; i < kBins; i += kSelThreads) {
+  for (int i = threadIdx.x; i < kBins; i += LDS::kThreads) {
     L.hist.count[i] = 0;
     L.hist.mass[i] = 0;
   }
@@ -258,17 +262,18 @@ struct Cut {
 constexpr float kFixed = 1099511627776.0f;  // 2^40: 2^22 weights of at most 1 stay below 2^63
 __device__ __forceinline__ unsigned long long fixed_weight(float w) { return (unsigned long long)(w * kFixed + 0.5f); }
 
-// Keys of a row that a thread holds: 5 x 8 consecutive places of each tile of
-// 20,480 groups (one tile up to V = 163,840), the first tile from the start on.
-constexpr int kKeyLoads = 5;
-constexpr uint32_t kTile = kKeyLoads * 8 * kSelThreads;
+// Keys of a row that a thread holds: 8 consecutive places in each load of a
+// tile (20,480 groups with 512 threads, one tile up to V = 163,840), the first tile from the start on.
+template <int T>
 struct KeyTile {
+  static constexpr int kKeyLoads = T == kSelThreads ? 5 : 3;
+  static constexpr uint32_t kTile = kKeyLoads * 8 * T;
   uint4 q[kKeyLoads];
   // `places` keys of the row (a multiple of 1,024); missing ones are 0
   __device__ __forceinline__ void load(const uint16_t *keys, uint32_t places, uint32_t base) {
 #pragma unroll
     for (int j = 0; j < kKeyLoads; ++j) {
-      const uint32_t at = base + 8 * (uint32_t(j) * kSelThreads + threadIdx.x);
+      const uint32_t at = base + 8 * (uint32_t(j) * T + threadIdx.x);
       q[j] = *reinterpret_cast<const uint4 *>(keys + min(at, places - 8));
       if (at >= places) q[j] = make_uint4(0, 0, 0, 0);
     }
@@ -288,9 +293,9 @@ struct KeyTile {
   __device__ __forceinline__ void each(uint32_t base, F f) const {
 #pragma unroll
     for (int j = 0; j < kKeyLoads; ++j) {
-      // opaque to the compiler, which would otherwise keep all 40 unpacked keys and
+      // opaque to the compiler, which would otherwise keep all unpacked keys and
       // places of one use for the next (and spill)
-      uint32_t at = base + 8 * (uint32_t(j) * kSelThreads + threadIdx.x);
+      uint32_t at = base + 8 * (uint32_t(j) * T + threadIdx.x);
       uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
       asm volatile("" : "+v"(at), "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
 #pragma unroll
@@ -304,12 +309,14 @@ static_assert(DSDE_MAX_VOCAB <= kMostSegs << 11, "segments of the cuts fit the L
 
 template <int DT, int ROW, typename LDS>
 struct Selector {
+  static constexpr int T = LDS::kThreads, W = LDS::kWaves;
+  using Tile = KeyTile<T>;
   const char *row;
   const uint16_t *keys;
   uint32_t V, ng, places;
   float m, c;
   LDS &L;
-  KeyTile tile;          // the first tile's keys
+  Tile tile;          // the first tile's keys
   bool listed = false;     // the logits to look at are in L.elems
   bool min_bound = false;  // they are those that min_p may keep
 
@@ -319,19 +326,18 @@ struct Selector {
   template <typename F>
   __device__ __forceinline__ void tiles(F f) {
     f(tile, 0u);
-    for (uint32_t base = kTile; base < places; base += kTile) {
-      KeyTile x;
+    for (uint32_t base = Tile::kTile; base < places; base += Tile::kTile) {
+      Tile x;
       x.load(keys, places, base);
       f(x, base);
     }
   }
 
-  // Writes the groups whose key reaches kappa to `out` (as far as they fit) and
-  // returns how many there are, in every thread.
-  __device__ __forceinline__ uint32_t groups_reaching(uint32_t kappa, uint32_t *out, uint32_t most) {
+  // Lists the groups whose key reaches kappa (as far as there is room) and returns how many there are, in every thread.
+  __device__ __forceinline__ uint32_t groups_reaching(uint32_t kappa) {
     if (threadIdx.x == 0) L.n_groups = 0;
     __syncthreads();
-    tiles([&](const KeyTile &x, uint32_t base) {
+    tiles([&](const Tile &x, uint32_t base) {
       uint32_t n = 0;
       x.each(base, [&](uint32_t k, uint32_t) { n += k >= kappa; });
       if (__ballot(n != 0) == 0) return;
@@ -341,7 +347,7 @@ struct Selector {
       at = lanes::readlane(at, 63) + sc.excl;
       x.each(base, [&](uint32_t k, uint32_t q) {
         if (k >= kappa) {
-          if (at < most) out[at] = place_group(q);
+          if (at < LDS::kGroups) L.list[at] = place_group(q);
           ++at;
         }
       });
@@ -355,17 +361,17 @@ struct Selector {
   // keys, and 256 about 355.)  kAll when fewer threads than that hold a finite one.
   __device__ __forceinline__ uint32_t threshold(uint32_t need) {
     uint32_t top = 0;
-    tiles([&](const KeyTile &x, uint32_t) { top = max(top, x.largest()); });
-    L.narrow.tmax[threadIdx.x] = top;
+    tiles([&](const Tile &x, uint32_t) { top = max(top, x.largest()); });
+    L.tmax[threadIdx.x] = top;
     __syncthreads();
-    uint32_t v[kSelWaves];
+    uint32_t v[W];
 #pragma unroll
-    for (int j = 0; j < kSelWaves; ++j) v[j] = L.narrow.tmax[64 * j + (threadIdx.x & 63)];
+    for (int j = 0; j < W; ++j) v[j] = L.tmax[64 * j + (threadIdx.x & 63)];
     uint32_t kappa = 0;
     for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
       uint32_t n = 0;
 #pragma unroll
-      for (int j = 0; j < kSelWaves; ++j) n += __popcll(__ballot(v[j] >= (kappa | bit)));
+      for (int j = 0; j < W; ++j) n += __popcll(__ballot(v[j] >= (kappa | bit)));
       if (n >= need) kappa |= bit;
     }
     return max(kappa, kAll);
@@ -376,8 +382,8 @@ struct Selector {
     uint32_t kappa = 0;
     for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
       uint32_t n = 0;
-      tiles([&](const KeyTile &x, uint32_t base) { x.each(base, [&](uint32_t k, uint32_t) { n += k >= (kappa | bit); }); });
-      if (block_reduce<kSelWaves>(n, L.red32, lanes::Add{}) >= need) kappa |= bit;
+      tiles([&](const Tile &x, uint32_t base) { x.each(base, [&](uint32_t k, uint32_t) { n += k >= (kappa | bit); }); });
+      if (block_reduce<W>(n, L.red32, lanes::Add{}) >= need) kappa |= bit;
     }
     return max(kappa, kAll);
   }
@@ -386,11 +392,11 @@ struct Selector {
   // there are more groups or logits than threads.
   __device__ __forceinline__ int32_t gather(uint32_t kappa, uint64_t *sorted) {
     const int t = threadIdx.x;
-    const uint32_t n_groups = groups_reaching(kappa, L.narrow.groups, kCand);
-    if (n_groups > kCand) return -1;
+    const uint32_t n_groups = groups_reaching(kappa);
+    if (n_groups > T) return -1;
     uint32_t key[kGroup], n = 0, w = 0;
     if (uint32_t(t) < n_groups) {
-      w = L.narrow.groups[t];
+      w = L.list[t];
       Group<DT, ROW> g;
       g.get(row, V, w);
       g.place(V, w);
@@ -400,8 +406,8 @@ struct Selector {
         n += key[e] >> 16 >= kappa;
       }
     }
-    const BlockScan<uint32_t> sc = block_scan<kSelWaves>(n, L.red32);
-    if (sc.total > kCand) return -1;
+    const BlockScan<uint32_t> sc = block_scan<W>(n, L.red32);
+    if (sc.total > T) return -1;
     if (n) {
       uint32_t at = sc.excl;
 #pragma unroll
@@ -411,7 +417,7 @@ struct Selector {
     __syncthreads();
     uint64_t v = uint32_t(t) < sc.total ? L.cand[t] : 0;
     __syncthreads();
-    block_sort(v, sc.total, L.cand);
+    block_sort<T>(v, sc.total, L.cand);
     *sorted = v;
     return int32_t(sc.total);
   }
@@ -421,19 +427,19 @@ struct Selector {
   template <typename F, typename I>
   __device__ __forceinline__ void each_group(uint32_t n, I list, F f) {
     constexpr int kBatch = 4;
-    for (uint32_t i = threadIdx.x & ~63u; i < n; i += kBatch * kSelThreads) {
+    for (uint32_t i = threadIdx.x & ~63u; i < n; i += kBatch * T) {
       Group<DT, ROW> g[kBatch];
       uint32_t w[kBatch];
       const uint32_t j0 = i + (threadIdx.x & 63);
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) w[b] = list(min(j0 + uint32_t(b) * kSelThreads, n - 1));
+      for (int b = 0; b < kBatch; ++b) w[b] = list(min(j0 + uint32_t(b) * T, n - 1));
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) g[b].get(row, V, w[b]);
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        if (i + uint32_t(b) * kSelThreads >= n) break;
+        if (i + uint32_t(b) * T >= n) break;
         g[b].place(V, w[b]);
-        f(g[b], w[b], j0 + uint32_t(b) * kSelThreads < n);
+        f(g[b], w[b], j0 + uint32_t(b) * T < n);
       }
     }
   }
@@ -445,7 +451,7 @@ struct Selector {
   template <typename F>
   __device__ __forceinline__ void each(F f) {
     if (listed) {
-      for (uint32_t i = threadIdx.x; i < L.n_elems; i += kSelThreads) {
+      for (uint32_t i = threadIdx.x; i < L.n_elems; i += T) {
         const uint64_t x = L.elems[i];
         f(uint32_t(x >> 32), key_logit(uint32_t(x >> 32)), ~uint32_t(x));
       }
@@ -463,8 +469,8 @@ struct Selector {
   // Lists the logits that reach `low` (a key's upper half); where they, or their
   // groups, are too many, all logits are looked at.
   __device__ __forceinline__ void list_logits(uint32_t low) {
-    const uint32_t n = groups_reaching(low, L.list, LDS::kList);
-    listed = n <= LDS::kList;
+    const uint32_t n = groups_reaching(low);
+    listed = n <= LDS::kGroups;
     if (!listed) return;
     if (threadIdx.x == 0) L.n_elems = 0;
     __syncthreads();
@@ -483,14 +489,18 @@ struct Selector {
 #pragma unroll
       for (int e = 0; e < kGroup; ++e)
         if (in && key[e] >= least) {
-          if (at < LDS::kList) L.elems[at] = packed(key[e], w * kGroup + e);
+          if (at < LDS::kElems) L.elems[at] = packed(key[e], w * kGroup + e);
           ++at;
         }
     });
     __syncthreads();
-    listed = L.n_elems <= LDS::kList;
+    listed = L.n_elems <= LDS::kElems;
   }
 
+  // The smallest logit with this upper half of a key (bf16 has no other).
+  __device__ __forceinline__ static float key_floor(uint32_t key) {
+    return key_logit((key << 16) | (DT == DSDE_BF16 && !(key & 0x8000u) ? 0xffffu : 0u));
+  }
   // The bin of a logit on a scale of its weight: equal logits share one, and larger
   // ones never come behind smaller ones.
   __device__ __forceinline__ uint32_t weight_bin(float z) const {
@@ -500,16 +510,16 @@ struct Selector {
   // Lists the logits from which the cuts are found, from the groups' largest
   // keys.  Any key will do whose logits turn out to hold the cut (weight_cut
   // looks): k groups whose largest lies in the first b bins do for a count of
-  // k; for a weight, the first bins whose groups' largest alone weigh enough, or else the most
-  // bins that the lists have room for.
+  // k; for a weight, the first bins whose groups' largest alone weigh enough, or as many bins as
+  // the list has room for.
   __device__ __forceinline__ void list_relevant(int32_t k, float p, float S, uint32_t min_key) {
-    constexpr int kPer = kBins / kSelThreads;
+    constexpr int kPer = kBins / T;
     const int t = threadIdx.x;
     clear_hist(L);
-    tiles([&](const KeyTile &x, uint32_t base) {
+    tiles([&](const Tile &x, uint32_t base) {
       x.each(base, [&](uint32_t key, uint32_t) {
         if (key < kAll) return;
-        const uint32_t b = weight_bin(fminf(key_logit((key << 16) | 0xffffu), m));
+        const uint32_t b = weight_bin(key_floor(key));
         if (b < uint32_t(kBins)) atomicAdd(&L.hist.count[b], 1u);
       });
     });
@@ -523,8 +533,11 @@ struct Selector {
       own += n[i];
       mass += float(n[i]) * fast_exp2(-float(kPer * t + i + 1) / kPerOctave);
     }
-    const BlockScan<uint32_t> sn = block_scan<kSelWaves>(own, L.red32);
-    const BlockScan<float> sm = block_scan<kSelWaves>(mass, L.redf);
+    const BlockScan<uint32_t> sn = block_scan<W>(own, L.red32);
+    const BlockScan<float> sm = block_scan<W>(mass, L.redf);
+    // about as many logits as there is room for reach the key that these groups reach, when the
+    // larger ones fall into the groups at random
+    const uint32_t room = min(LDS::kGroups, uint32_t(float(ng) * (1.f - __expf(-0.85f * LDS::kElems / float(ng)))));
     uint32_t inside = sn.excl;
     float weighs = sm.excl;
     int32_t best = kBins;
@@ -532,7 +545,8 @@ struct Selector {
     for (int i = 0; i < kPer; ++i) {  // the first kPer t + i + 1 bins
       inside += n[i];
       weighs += float(n[i]) * fast_exp2(-float(kPer * t + i + 1) / kPerOctave);
-      const bool ok = k > 0 ? inside >= uint32_t(k) : (p < 1.f && weighs >= 1.00001f * p * S) || inside >= kListGroups;
+      const uint32_t next = T * kPer > kPer * t + i + 1 ? L.hist.count[kPer * t + i + 1] : 0u;
+      const bool ok = k > 0 ? inside >= uint32_t(k) : weighs >= 1.00001f * p * S || inside + next > room;
       if (ok && best == kBins) best = kPer * t + i + 1;
     }
     if (best < kBins) atomicMin(&L.found, best);
@@ -595,13 +609,24 @@ struct Selector {
       if (last) add_segments(kEvery, min_p, kept);
       return Cut{kEvery, 0};
     }
-    if (bin < 0 || in_bin > uint32_t(kCand)) {
+    if (bin < 0 || in_bin > uint32_t(T)) {
       // outside the histogram's range, or a long run of nearly equal logits
-      cut = key_cut<MASS>(target);
-      if (last)
-        add_segments(cut.at, min_p, kept);
-      else
-        histogram();
+      if (bin >= 0 && !listed && in_bin <= LDS::kElems) {
+        if (t == 0) L.n_elems = 0;
+        __syncthreads();
+        pass([&](float z, uint32_t id, bool in) -> unsigned long long {
+          if (in && weight_bin(z) == uint32_t(bin)) L.elems[atomicAdd(&L.n_elems, 1u)] = packed(order_key(z), id);
+          return 0;
+        });
+        __syncthreads();
+        listed = true;
+        cut = key_cut<MASS>(target - (MASS ? mass0 : count0));
+        cut.mass += mass0;
+        listed = false;
+      } else {
+        cut = key_cut<MASS>(target);
+      }
+      if (last) add_segments(cut.at, min_p, kept);
       return cut;
     }
     if (t == 0) L.n_cand = 0;
@@ -620,10 +645,10 @@ struct Selector {
     __syncthreads();
     uint64_t v = uint32_t(t) < in_bin ? L.cand[t] : 0;
     __syncthreads();
-    block_sort(v, in_bin, L.cand);
+    block_sort<T>(v, in_bin, L.cand);
     const float x = uint32_t(t) < in_bin ? weight(key_logit(uint32_t(v >> 32))) : 0.f;
     const uint64_t f = fixed_weight(x);
-    const BlockScan<uint64_t> sc = block_scan<kSelWaves>(uint32_t(t) < in_bin ? f : 0, L.red64);
+    const BlockScan<uint64_t> sc = block_scan<W>(uint32_t(t) < in_bin ? f : 0, L.red64);
     const uint32_t end = MASS ? min(uint32_t(__syncthreads_count(uint32_t(t) < in_bin && mass0 + sc.incl < target)), in_bin - 1)
                               : uint32_t(target - count0) - 1;
     if (uint32_t(t) == end) {
@@ -711,10 +736,10 @@ struct Selector {
       if (k == key) atomicAdd(&L.segs[id >> seg_shift], 1ull);
     });
     __syncthreads();
-    const int32_t per = (nseg + kSelThreads - 1) / kSelThreads, s0 = t * per, s1 = min(s0 + per, nseg);
+    const int32_t per = (nseg + T - 1) / T, s0 = t * per, s1 = min(s0 + per, nseg);
     uint32_t own = 0;
     for (int32_t i = s0; i < s1; ++i) own += uint32_t(L.segs[i]);
-    uint32_t before = block_scan<kSelWaves>(own, L.red32).excl;
+    uint32_t before = block_scan<W>(own, L.red32).excl;
     for (int32_t i = s0; i < s1; ++i) {
       const uint32_t x = uint32_t(L.segs[i]);
       if (before < n && n <= before + x) {
@@ -752,7 +777,7 @@ struct Selector {
   __device__ __forceinline__ void clear_segments() {
     seg_shift = V <= 512u * kMostSegs ? 9 : V <= 1024u * kMostSegs ? 10 : 11;
     nseg = int32_t((V + (1u << seg_shift) - 1) >> seg_shift);
-    for (int32_t i = threadIdx.x; i < nseg; i += kSelThreads) L.segs[i] = 0;
+    for (int32_t i = threadIdx.x; i < nseg; i += T) L.segs[i] = 0;
     __syncthreads();
   }
   // Calls f(logit, id, whether it counts) on the listed logits, or on all, and adds the
@@ -761,7 +786,7 @@ struct Selector {
   template <typename F>
   __device__ __forceinline__ void pass(F f) {
     if (listed) {
-      for (uint32_t i = threadIdx.x; i < L.n_elems; i += kSelThreads) {
+      for (uint32_t i = threadIdx.x; i < L.n_elems; i += T) {
         const uint64_t x = L.elems[i];
         const unsigned long long sum = f(key_logit(uint32_t(x >> 32)), ~uint32_t(x), true);
         if (sum) atomicAdd(&L.segs[~uint32_t(x) >> seg_shift], sum);
@@ -795,12 +820,12 @@ struct Selector {
   template <typename WF>
   __device__ __forceinline__ void draw_segment(int32_t n, float u, WF weight_of) {
     const int t = threadIdx.x;
-    const int32_t per = (n + kSelThreads - 1) / kSelThreads;  // consecutive segments of one thread
+    const int32_t per = (n + T - 1) / T;  // consecutive segments of one thread
     const int32_t s0 = t * per, s1 = min(s0 + per, n);
     double w = 0.0;
     for (int32_t s = s0; s < s1; ++s) w += weight_of(s);
     if (t == 0) L.seg = -1;
-    const BlockScan<double> bw = block_scan<kSelWaves>(w, reinterpret_cast<double *>(L.red64));
+    const BlockScan<double> bw = block_scan<W>(w, reinterpret_cast<double *>(L.red64));
     const double target = double(u) * bw.total;
     int32_t best = -1;
     double rem = 0.0, at = bw.excl;
@@ -880,10 +905,23 @@ struct Selector {
   }
 };
 
+__device__ __forceinline__ float row_logprob(float z, float m, float T, double S) {
+  return float((double(z) - double(m)) / double(T) - log(S));
+}
+
+// A little below the smallest logit that min_p keeps, as the upper half of a key.
+__device__ __forceinline__ uint32_t min_p_key(const Setting &s, float m) {
+  if (!(s.m > 0.f)) return 0;
+  const float d = log2f(s.m) / s.c;
+  return order_key(m + d - 1e-5f * (1.f + fabsf(m) + fabsf(d))) >> 16;
+}
+
 // One row per workgroup.
 template <int DT, int ROW, bool TOP>
 __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
-  __shared__ SelectLds<TOP> L;
+  using LDS = std::conditional_t<TOP, TopLds, DrawLds>;
+  constexpr int W = LDS::kWaves;
+  __shared__ LDS L;
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x, out = row0 + r;
   const Setting s = row_setting(a, out);
@@ -891,7 +929,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   const float *seg = a.scan.seg + r * nc * kSegs;
   const int32_t nseg = nc * kSegs;
   const uint32_t V = uint32_t(a.V);
-  Selector<DT, ROW, SelectLds<TOP>> sel{a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup,
+  Selector<DT, ROW, LDS> sel{a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup,
                         uint32_t(nc) * kChunkGroups, 0.f, s.c, L, {}, false, false, 0, 9};
   // the loads that the kernel starts with, together
   float first_max = -INFINITY, first_seg = 0.f, first_ref = -INFINITY;
@@ -906,7 +944,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   bool bad = !(mt < INFINITY);
   // (a row has at most 512 chunks: one per thread)
   bad = __syncthreads_or(bad);
-  const float m = block_reduce<kSelWaves>(mt, L.redf, lanes::Max{});
+  const float m = block_reduce<W>(mt, L.redf, lanes::Max{});
   const uint32_t err = s.err | (bad || m == -INFINITY ? DSDE_ERR_LOGIT : 0u);
   if (t == 0) a.row_err[out] = err;
   if (err) {
@@ -928,11 +966,11 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   double part = part0;
   for (int32_t i = t + kSelThreads; i < nseg; i += kSelThreads)
     part += double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c));
-  const double S = block_reduce<kSelWaves>(part, reinterpret_cast<double *>(L.red64), lanes::Add{});
+  const double S = block_reduce<W>(part, reinterpret_cast<double *>(L.red64), lanes::Add{});
 
   auto emit = [&](int32_t token, float z, int32_t kept) {
     a.tokens[out] = token;
-    if (a.logprob) a.logprob[out] = float((double(z) - double(m)) / double(s.T) - log(S));
+    if (a.logprob) a.logprob[out] = row_logprob(z, m, s.T, S);
     if (a.kept) a.kept[out] = kept;
   };
 
@@ -951,14 +989,14 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
         const uint64_t x = packed(key, id);
         if (x >= cut) {
           const uint32_t i = atomicAdd(&L.n_cand, 1u);
-          if (i < kCand) L.cand[i] = x;
+          if (i < kSelThreads) L.cand[i] = x;
         }
       });
       __syncthreads();
-      n = int32_t(min(L.n_cand, uint32_t(kCand)));
+      n = int32_t(min(L.n_cand, uint32_t(kSelThreads)));
       v = t < n ? L.cand[t] : 0;
       __syncthreads();
-      block_sort(v, uint32_t(n), L.cand);
+      block_sort<kSelThreads>(v, uint32_t(n), L.cand);
     }
     if (t < k) {
       a.values[out * k + t] = t < n ? key_logit(uint32_t(v >> 32)) : -INFINITY;
@@ -967,7 +1005,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
     return;
   } else {
     if (!s.filtered) {
-      const uint32_t n = a.kept ? block_reduce<kSelWaves>(sel.unmasked(), L.red32, lanes::Add{}) : 0u;
+      const uint32_t n = a.kept ? block_reduce<W>(sel.unmasked(), L.red32, lanes::Add{}) : 0u;
       sel.draw_segment(
           nseg, s.u,
           [&](int32_t i) {
@@ -982,14 +1020,9 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
       return;
     }
 
-    // A little below the smallest logit that min_p keeps, as a key.
-    uint32_t min_key = 0;
-    if (s.m > 0.f) {
-      const float d = log2f(s.m) / s.c;
-      min_key = order_key(m + d - 1e-5f * (1.f + fabsf(m) + fabsf(d))) >> 16;
-    }
+    const uint32_t min_key = min_p_key(s, m);
     // Few tokens kept: candidates, a prefix of the row's order, sorted.  Where its
-    // length does not settle every filter, the cuts below.
+    // length does not settle every filter, the cuts of wide_kernel.
     if (s.k <= kMostNeed) {
       uint32_t kappa = sel.threshold(s.k > 0 ? s.k : kFirstNeed);
       const bool min_decided = min_key >= kappa;
@@ -1000,7 +1033,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
       int32_t kept = kUndecided;
       if (n >= 0) {
         const float e = t < n ? sel.weight(key_logit(uint32_t(v >> 32))) : 0.f;
-        const BlockScan<double> cs = block_scan<kSelWaves>(double(e), reinterpret_cast<double *>(L.red64));
+        const BlockScan<double> cs = block_scan<W>(double(e), reinterpret_cast<double *>(L.red64));
         const bool k_in = s.k > 0 && s.k <= n;
         if (k_in && t == s.k - 1) L.mass = cs.incl;
         const int32_t n_min = __syncthreads_count(t < n && e >= s.m);
@@ -1023,7 +1056,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
         if (one_wave && t >= 64) return;
         uint64_t x = t < kept ? (v << 32) | uint32_t(t) : 0;  // (~id, rank)
         if (!one_wave) L.elems[t] = v;
-        block_sort(x, uint32_t(kept), L.cand);
+        block_sort<kSelThreads>(x, uint32_t(kept), L.cand);
         const uint32_t key = one_wave ? __shfl(uint32_t(v >> 32), int(uint32_t(x)))
                                       : uint32_t(L.elems[uint32_t(x)] >> 32);
         const float z = key_logit(key);
@@ -1033,36 +1066,58 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
           const double incl = lanes::wave_scan(e).incl, total = lanes::readlane(incl, 63);
           at = __popcll(__ballot(t < kept && incl <= double(s.u) * total));
         } else {
-          const BlockScan<double> cs = block_scan<kSelWaves>(e, reinterpret_cast<double *>(L.red64));
+          const BlockScan<double> cs = block_scan<W>(e, reinterpret_cast<double *>(L.red64));
           at = __syncthreads_count(t < kept && cs.incl <= double(s.u) * cs.total);
         }
         if (t == min(at, kept - 1)) emit(int32_t(~uint32_t(x >> 32)), z, kept);
         return;
       }
-      __syncthreads();
     }
+    if (t == 0) a.scan.wide[atomicAdd(a.scan.n_wide, 1u)] = WideRow{int32_t(r), m, S};
+  }
+}
 
-    // More tokens: cuts by histograms over the groups that may hold them.
-    int32_t n_above = 0;
-    sel.list_relevant(s.k, s.p, float(S), min_key);
-    Cut cut{kEvery, uint64_t(S * double(kFixed))};
+// The rows that the select kernel has left: cuts by histograms over the logits
+// that may lie above them, then the draw over segments.
+template <int DT, int ROW>
+__global__ __launch_bounds__(kWideThreads) void wide_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
+  __shared__ WideLds L;
+  const int t = threadIdx.x;
+  const uint32_t n = *a.scan.n_wide, V = uint32_t(a.V);
+  for (uint32_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const WideRow w = a.scan.wide[i];
+    const int64_t out = row0 + w.row;
+    const Setting s = row_setting(a, out);
+    Selector<DT, ROW, WideLds> sel{a.rows.row(out), a.scan.keys + int64_t(w.row) * nc * kChunkGroups, V,
+                                   (V + kGroup - 1) / kGroup, uint32_t(nc) * kChunkGroups, w.max, s.c, L, {}, false,
+                                   false, 0, 9};
+    sel.tile.load(sel.keys, sel.places, 0);
+    int32_t kept = 0;
+    sel.list_relevant(s.k, s.p, float(w.sum), min_p_key(s, w.max));
+    Cut cut{kEvery, uint64_t(w.sum * double(kFixed))};
     const bool by_p = s.p < 1.f;
-    sel.histogram();
-    if (s.k > 0) cut = sel.template weight_cut<false>(uint64_t(s.k), !by_p, s.m, &n_above);
+    if (s.k > 0 || by_p) sel.histogram();
+    if (s.k > 0) cut = sel.template weight_cut<false>(uint64_t(s.k), !by_p, s.m, &kept);
     if (by_p) {
       const uint64_t target = uint64_t(double(s.p) * double(cut.mass));
-      cut = sel.template weight_cut<true>(target ? target : 1, true, s.m, &n_above);
+      if (s.k > 0) sel.histogram();
+      cut = sel.template weight_cut<true>(target ? target : 1, true, s.m, &kept);
     } else if (s.k == 0) {
-      sel.add_segments(kEvery, s.m, &n_above);
+      sel.add_segments(kEvery, s.m, &kept);
     }
-    const uint32_t count = block_reduce<kSelWaves>(uint32_t(n_above), L.red32, lanes::Add{});
-    sel.draw_segment(sel.nseg, s.u, [&](int32_t i) { return double(L.segs[i]) * (1.0 / double(kFixed)); });
+    const uint32_t count = block_reduce<WideLds::kWaves>(uint32_t(kept), L.red32, lanes::Add{});
+    sel.draw_segment(sel.nseg, s.u, [&](int32_t j) { return double(L.segs[j]) * (1.0 / double(kFixed)); });
     if (t < 64) {
       int32_t token;
       float z;
       sel.draw_token(1 << (sel.seg_shift - 9), cut.at, s.m, &token, &z);
-      if (t == 0) emit(token, z, int32_t(count));
+      if (t == 0) {
+        a.tokens[out] = token;
+        if (a.logprob) a.logprob[out] = row_logprob(z, w.max, s.T, w.sum);
+        if (a.kept) a.kept[out] = int32_t(count);
+      }
     }
+    __syncthreads();
   }
 }
 
@@ -1079,12 +1134,17 @@ int launch(const SelectArgs &a0, int64_t R, hipStream_t stream) {
   a.scan.max = reinterpret_cast<float *>(ws + l.max);
   a.scan.seg = reinterpret_cast<float *>(ws + l.seg);
   a.scan.keys = reinterpret_cast<uint16_t *>(ws + l.keys);
+  a.scan.wide = reinterpret_cast<WideRow *>(ws + l.wide);
+  a.scan.n_wide = reinterpret_cast<uint32_t *>(ws + l.n_wide);
   for (int64_t r0 = 0; r0 < R; r0 += per_pass) {
     const int64_t n = R - r0 < per_pass ? R - r0 : per_pass;
     by_rows(a.dtype, form, [&](auto dt, auto row) {
       constexpr int DT = decltype(dt)::value, ROW = decltype(row)::value;
       row_scan_kernel<DT, ROW><<<dim3(unsigned(n * nc)), dim3(kThreads), 0, stream>>>(a, r0, nc);
       select_kernel<DT, ROW, TOP><<<dim3(unsigned(n)), dim3(kSelThreads), 0, stream>>>(a, r0, nc);
+      if constexpr (!TOP)
+        if (a.top_k || a.top_p || a.min_p)
+          wide_kernel<DT, ROW><<<dim3(unsigned(n < 256 ? n : 256)), dim3(kWideThreads), 0, stream>>>(a, r0, nc);
     });
   }
   return hipGetLastError() == hipSuccess ? DSDE_OK : DSDE_DEVICE_ERROR;
