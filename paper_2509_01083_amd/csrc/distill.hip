@@ -16,6 +16,31 @@
 namespace dsde {
 namespace {
 
+// 2^(z c - ref c), one fused operation and an exponential.  ref c is rounded, but
+// to the same number for every token that is weighed against it.  Where it is
+// beyond 2^100 (rows masked with the type's lowest value throughout) the difference is taken first.
+struct Weigher {
+  float ref, c, scaled;
+  bool far;
+  __device__ __forceinline__ Weigher(float M, float c_) : ref(finite_ref(M)), c(c_) {
+    scaled = ref * c;
+    far = !(fabsf(scaled) < 0x1p100f);
+  }
+  template <bool FAR>
+  __device__ __forceinline__ float of(float z) const {
+    return FAR ? row_weight(z, ref, c) : fast_exp2(fmaf(z, c, -scaled));
+  }
+};
+// A group's weights: four pairs in fp32, added in fp32.
+template <bool FAR, typename G>
+__device__ __forceinline__ float group_weight(const G &g, const Weigher &w) {
+  const float a = w.template of<FAR>(g.at(0)) + w.template of<FAR>(g.at(1));
+  const float b = w.template of<FAR>(g.at(2)) + w.template of<FAR>(g.at(3));
+  const float d = w.template of<FAR>(g.at(4)) + w.template of<FAR>(g.at(5));
+  const float e = w.template of<FAR>(g.at(6)) + w.template of<FAR>(g.at(7));
+  return (a + b) + (d + e);
+}
+
 // The teacher's tokens in one chunk: a bit per logit, eight logits (a group) to
 // a byte, and for the gradient their list.
 struct ChunkTokens {
@@ -77,16 +102,145 @@ __global__ __launch_bounds__(kThreads) void distill_scan_kernel(const DistillArg
   }
   const bool bad = __syncthreads_or(tm != tm);
   const float M = block_max(tm, redf);
-  const float ref = finite_ref(M), c = kLog2e / a.temperature;
-  // pairs in fp32, their sums in fp64: the loss is a small difference of logarithms
+  const Weigher weigh(M, kLog2e / a.temperature);
+  // groups in fp32, their sums in fp64: the loss is a small difference of logarithms
   double sum = 0.0;
+  if (weigh.far) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) sum += double(group_weight<true>(g[i], weigh));
+  } else {
 #pragma unroll
-    for (int e = 0; e < kGroup; e += 2)
-      sum += double(row_weight(g[i].at(e), ref, c) + row_weight(g[i].at(e + 1), ref, c));
+    for (int i = 0; i < 4; ++i) sum += double(group_weight<false>(g[i], weigh));
+  }
   sum = block_reduce<kWaves>(sum, red, lanes::Add{});
   if (t == 0) a.part[unit] = DistillPartial{bad ? NAN : M, tokens.twice, sum};
+}
+
+// exp and log of a row's scalars in fp64, good to about 1e-7 of the value and of 1: the
+// hardware's fp32 functions on what is left of the argument after its power of
+// two.  The library's take some twenty constants each, which a loop over rows keeps
+// in registers.
+__device__ __forceinline__ double exp2_of(double x) {
+  const double y = fmax(x, -4096.0), n = rint(y);
+  return ldexp(double(fast_exp2(float(y - n))), int(n));
+}
+__device__ __forceinline__ double exp_of(double x) { return exp2_of(x * 1.4426950408889634); }
+__device__ __forceinline__ double log_of(double s) {
+  int e;
+  const double m = frexp(s, &e);
+  const float f = float(m), d = float(m - double(f));
+  return (double(e) + double(__builtin_amdgcn_logf(f)) + double(d * kLog2e * __builtin_amdgcn_rcpf(f))) * kLn2;
+}
+
+// The log2 of a reference's scale, ref c as Weigher rounds it, against that of m, and the factor that
+// takes sums against `ref` to sums against `to`.
+__device__ __forceinline__ double ref_log2(float ref, float m, float c) {
+  const Weigher w(ref, c);
+  return w.far ? (double(ref) - double(m)) * double(c) : double(w.scaled) - double(m) * double(c);
+}
+__device__ __forceinline__ double ref_factor(float ref, float to, float c) {
+  const Weigher x(ref, c), y(to, c);
+  return x.far || y.far ? double(row_weight(ref, to, c)) : exp2_of(double(x.scaled) - double(y.scaled));
+}
+
+// The teacher's side of one row and the student's logits at its tokens, by one
+// wavefront (entry k in lane k % 64), the same in every lane.
+constexpr int kPerLane = DSDE_MAX_TOP / 64;
+constexpr float kInf = __builtin_inff();
+struct TeacherRow {
+  uint32_t err;
+  bool nothing;      // no entry with weight, and no mass outside the entries either
+  float tmax, smax;  // largest logits of the teacher's entries and of the student's at them
+  double scale;      // p_k = scale 2^((t_k - tmax) c)
+  double sum;        // sum of p
+  double cross;      // sum of p_k (log p_k - (s_k - smax) / T)
+  double student;    // sum of exp((s_k - smax) / T)
+};
+__device__ __forceinline__ double entry_cross(float z, float tmax, float q, float smax, double iT) {
+  return ((double(z) - double(tmax)) - (double(q) - double(smax))) * iT;
+}
+__device__ __forceinline__ TeacherRow teacher_row(const DistillArgs &a, int64_t n) {
+  const int lane = threadIdx.x & 63;
+  const char *row = a.rows.row(n);
+  TeacherRow r;
+  r.err = 0;
+  float z[kPerLane], q[kPerLane];  // teacher and student logits
+  r.tmax = r.smax = -kInf;
+#pragma unroll
+  for (int j = 0; j < kPerLane; ++j) {
+    const int32_t k = lane + 64 * j;
+    const int32_t id = k < a.K ? a.ids[n * a.K + k] : -1;
+    if (id < -1 || id >= a.V) r.err |= DSDE_ERR_TOKEN;
+    const bool used = id >= 0 && id < a.V;
+    z[j] = used ? a.teacher[n * a.K + k] : -kInf;
+    q[j] = used ? load_logit(row, a.dtype, id) : -kInf;
+    if (!(z[j] < kInf) || !(q[j] < kInf) || (z[j] > -kInf && q[j] == -kInf)) r.err |= DSDE_ERR_LOGIT;
+    r.tmax = fmaxf(r.tmax, z[j]);
+    r.smax = fmaxf(r.smax, q[j]);
+  }
+  const bool tail = a.teacher_lse != nullptr;
+  const double L = tail ? double(a.teacher_lse[n]) : 0.0;
+  if (!(fabs(L) < double(kInf))) r.err |= DSDE_ERR_LOGIT;
+  r.err = lanes::wave_or(r.err);
+  r.tmax = lanes::wave_max(r.tmax);
+  r.smax = lanes::wave_max(r.smax);
+  r.nothing = !tail && r.tmax == -kInf;
+  const double iT = 1.0 / double(a.temperature);
+  const float c = kLog2e / a.temperature;
+  double e[kPerLane], esum = 0.0;
+  r.student = 0.0;
+#pragma unroll
+  for (int j = 0; j < kPerLane; ++j) {
+    e[j] = 0.0;
+    if (64 * j < a.K) {
+      if (z[j] > -kInf) e[j] = double(row_weight(z[j], r.tmax, c));
+      if (q[j] > -kInf) r.student += double(row_weight(q[j], r.smax, c));
+    }
+    esum += e[j];
+  }
+  r.student = lanes::wave_sum(r.student);
+  esum = lanes::wave_sum(esum);
+  // log p_k = (t_k - tmax) / T + log scale
+  const double logs = r.tmax == -kInf ? 0.0 : tail ? double(r.tmax) * iT - L : -log_of(esum);
+  r.scale = exp_of(logs);
+  r.sum = esum * r.scale;
+  double cross = 0.0;
+#pragma unroll
+  for (int j = 0; j < kPerLane; ++j)
+    if (e[j] > 0.0) cross += e[j] * entry_cross(z[j], r.tmax, q[j], r.smax, iT);
+  r.cross = lanes::wave_sum(cross) * r.scale + logs * r.sum;
+  return r;
+}
+
+// The loss and the record of one row, from its teacher's side and the sums
+// over the rest (the largest logit rmax there, and the sum of weights against
+// it), in every lane of a wavefront.
+struct RowLoss {
+  float loss;
+  uint32_t err;
+  dsde_distill_row record;
+};
+__device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const TeacherRow &r, uint32_t err, float rmax,
+                                            double rest) {
+  const float m = fmaxf(r.smax, rmax);
+  err |= r.err;
+  if (m == -kInf) err |= DSDE_ERR_LOGIT;
+  if (err || r.nothing)
+    return RowLoss{err ? __builtin_nanf("") : 0.f, err, dsde_distill_row{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1, 0}};
+  const float c = kLog2e / a.temperature;
+  const double ds = r.smax > -kInf ? (double(r.smax) - double(m)) * double(c) * kLn2 : 0.0;
+  const double dr = rmax > -kInf ? ref_log2(rmax, m, c) * kLn2 : 0.0;
+  const double es = exp_of(ds), er = rmax > -kInf ? exp_of(dr) : 0.0;
+  const double S = r.student * es + rest * er, logS = log_of(S);
+  const double tail = a.teacher_lse && r.sum < 1.0 ? 1.0 - r.sum : 0.0;
+  double loss = r.cross - r.sum * (ds - logS), share = 0.0;  // share: what the rest's gradient adds up to
+  if (rest > 0.0) {
+    if (tail > 0.0) loss += tail * (log_of(tail) - (dr + log_of(rest) - logS));
+    share = rest * er / S - tail;
+  }
+  return RowLoss{float(loss), 0,
+                 dsde_distill_row{finite_ref(rmax), rest > 0.0 ? float(share / rest) : 0.f, m, float(1.0 / S),
+                                  finite_ref(r.tmax), float(r.scale), 0, 0}};
 }
 
 // One wavefront per row: the loss, and the record that the gradient takes its
@@ -95,100 +249,33 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(const DistillA
   const int64_t n = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
   if (n >= N) return;
   const int lane = threadIdx.x & 63;
-  constexpr int kPer = DSDE_MAX_TOP / 64;
-  constexpr float kInf = __builtin_inff();
-  if (a.skip_zero && a.weight[n] == 0.0f) {
-    if (lane == 0) {
-      a.loss[n] = 0.f;
-      a.row_err[n] = 0;
-      a.record[n] = dsde_distill_row{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1, 0};
-    }
-    return;
-  }
-  uint32_t err = 0;
-  bool used[kPer];
-  float z[kPer], q[kPer];  // teacher and student logits
-  float tmax = -kInf, smax = -kInf;
-  const char *row = a.rows.row(n);
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const int32_t k = lane + 64 * j;
-    const int32_t id = k < a.K ? a.ids[n * a.K + k] : -1;
-    if (id < -1 || id >= a.V) err |= DSDE_ERR_TOKEN;
-    used[j] = id >= 0 && id < a.V;
-    z[j] = used[j] ? a.teacher[n * a.K + k] : -kInf;
-    q[j] = used[j] ? load_logit(row, a.dtype, id) : -kInf;
-    if (!(z[j] < kInf) || !(q[j] < kInf) || (z[j] > -kInf && q[j] == -kInf)) err |= DSDE_ERR_LOGIT;
-    tmax = fmaxf(tmax, z[j]);
-    smax = fmaxf(smax, q[j]);
-  }
-  float rmax = -kInf;
-  for (int32_t i = lane; i < nc; i += 64) {
-    const DistillPartial x = a.part[n * nc + i];
-    if (!(x.max < kInf)) err |= DSDE_ERR_LOGIT;
-    if (x.bad) err |= DSDE_ERR_TOKEN;
-    rmax = fmaxf(rmax, x.max);
-  }
-  const bool tail = a.teacher_lse != nullptr;
-  const double L = tail ? double(a.teacher_lse[n]) : 0.0;
-  if (!(fabs(L) < double(kInf))) err |= DSDE_ERR_LOGIT;
-  err = lanes::wave_or(err);
-  tmax = lanes::wave_max(tmax);
-  smax = lanes::wave_max(smax);
-  rmax = lanes::wave_max(rmax);
-  const float m = fmaxf(smax, rmax);
-  if (m == -kInf) err |= DSDE_ERR_LOGIT;
-  const bool nothing = !tail && tmax == -kInf;  // no teacher at all
-  if (err || nothing) {
-    if (lane == 0) {
-      a.loss[n] = err ? NAN : 0.f;
-      a.row_err[n] = err;
-      a.record[n] = dsde_distill_row{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1, 0};
-    }
-    return;
-  }
-  const double iT = 1.0 / double(a.temperature);
-  double rest = 0.0;  // against rmax
-  if (rmax > -kInf)
+  RowLoss out{0.f, 0, dsde_distill_row{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1, 0}};
+  if (!(a.skip_zero && a.weight[n] == 0.0f)) {
+    uint32_t err = 0;
+    float rmax = -kInf;
+    const float c = kLog2e / a.temperature;
+    const DistillPartial *part = a.part + n * nc;
     for (int32_t i = lane; i < nc; i += 64) {
-      const DistillPartial x = a.part[n * nc + i];
-      if (x.max > -kInf) rest += x.sum * exp((double(x.max) - double(rmax)) * iT);
+      const DistillPartial x = part[i];
+      if (!(x.max < kInf)) err |= DSDE_ERR_LOGIT;
+      if (x.bad) err |= DSDE_ERR_TOKEN;
+      rmax = fmaxf(rmax, x.max);
     }
-  rest = lanes::wave_sum(rest);
-  double top = 0.0, tsum = 0.0, e[kPer];
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    e[j] = z[j] > -kInf ? exp((double(z[j]) - double(tmax)) * iT) : 0.0;
-    tsum += e[j];
-    if (q[j] > -kInf) top += exp((double(q[j]) - double(m)) * iT);
-  }
-  top = lanes::wave_sum(top);
-  tsum = lanes::wave_sum(tsum);
-  const double rest_at = rmax > -kInf ? exp((double(rmax) - double(m)) * iT) : 0.0;
-  const double S = top + rest * rest_at, logS = log(S);
-  // log p_k = (z_k - tmax) / T + log t0, p_k = e_k t0
-  const double logt0 = tmax == -kInf ? 0.0 : tail ? double(tmax) * iT - L : -log(tsum), t0 = exp(logt0);
-  double loss = 0.0, psum = 0.0;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const double p = e[j] * t0;
-    psum += p;
-    if (p > 0.0)
-      loss += p * ((double(z[j]) - double(tmax)) * iT + logt0 - ((double(q[j]) - double(m)) * iT - logS));
-  }
-  loss = lanes::wave_sum(loss);
-  psum = lanes::wave_sum(psum);
-  double r = tail && psum < 1.0 ? 1.0 - psum : 0.0, share = 0.0;  // share: what the rest's gradient adds up to
-  if (rmax > -kInf) {
-    const double qr = rest * rest_at / S;
-    if (r > 0.0) loss += r * (log(r) - ((double(rmax) - double(m)) * iT + log(rest) - logS));
-    share = qr - r;
+    err = lanes::wave_or(err);
+    rmax = lanes::wave_max(rmax);
+    double rest = 0.0;  // against rmax
+    if (rmax > -kInf && rmax < kInf)
+      for (int32_t i = lane; i < nc; i += 64) {
+        const DistillPartial x = part[i];
+        if (x.max > -kInf) rest += x.sum * ref_factor(x.max, rmax, c);
+      }
+    rest = lanes::wave_sum(rest);
+    out = row_loss(a, teacher_row(a, n), err, rmax, rest);
   }
   if (lane == 0) {
-    a.loss[n] = float(loss);
-    a.row_err[n] = 0;
-    a.record[n] = dsde_distill_row{finite_ref(rmax), rest > 0.0 ? float(share / rest) : 0.f, m, float(1.0 / S),
-                                   finite_ref(tmax), float(t0), 0, 0};
+    a.loss[n] = out.loss;
+    a.row_err[n] = out.err;
+    a.record[n] = out.record;
   }
 }
 
@@ -224,6 +311,17 @@ __device__ __forceinline__ void put_group(char *row, uint32_t V, uint32_t w, con
   }
 }
 
+// The teacher's probability of an entry, and the gradient there; without contraction of the
+// products, so that every caller sees the same bits.
+__device__ __forceinline__ float teacher_p(float logit, const dsde_distill_row &r, float c) {
+#pragma clang fp contract(off)
+  return row_weight(logit, r.teacher_ref, c) * r.teacher_scale;
+}
+__device__ __forceinline__ float entry_gradient(float z, float p, const dsde_distill_row &r, float c, float scale) {
+#pragma clang fp contract(off)
+  return scale * (row_weight(z, r.ref, c) * r.scale - p);
+}
+
 // The gradient of one chunk of a row.  It may overwrite the logits: every
 // logit is read by the thread that writes its gradient.
 template <int DT, int ROW>
@@ -252,15 +350,21 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
   mark_tokens(tokens, a.ids + n * a.K, a.K, chunk, a.V, [&](ChunkTokens &s, int k, uint32_t local) {
     const uint32_t j = atomicAdd(&s.n, 1u);
     s.at[j] = uint16_t(local);
-    s.p[j] = row_weight(teacher[k], rec.teacher_ref, c) * rec.teacher_scale;
+    s.p[j] = teacher_p(teacher[k], rec, c);
   });
   const float coef = rec.rest_scale * scale;
+  const Weigher weigh(rec.rest_ref, c);
   const uint32_t listed = tokens.n;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     g[i].place(V, w0 + 256 * i);
+    if (weigh.far) {
 #pragma unroll
-    for (int e = 0; e < kGroup; ++e) x[e] = coef * row_weight(g[i].at(e), rec.rest_ref, c);
+      for (int e = 0; e < kGroup; ++e) x[e] = coef * weigh.of<true>(g[i].at(e));
+    } else {
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) x[e] = coef * weigh.of<false>(g[i].at(e));
+    }
     const uint32_t bits = token_bits(tokens, 256 * i + t);
     if (bits) {
       for (uint32_t j = 0; j < listed; ++j) {
@@ -268,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
         if (off < uint32_t(kGroup)) {
 #pragma unroll
           for (int e = 0; e < kGroup; ++e)
-            if (off == uint32_t(e)) x[e] = scale * (row_weight(g[i].at(e), rec.ref, c) * rec.scale - tokens.p[j]);
+            if (off == uint32_t(e)) x[e] = entry_gradient(g[i].at(e), tokens.p[j], rec, c, scale);
         }
       }
     }

@@ -203,6 +203,38 @@ def test_in_place_strided_and_repeated(gpu_lib, N, V, dtype):
     assert torch.equal(wide[:, :3], edge[0]) and torch.equal(wide[:, 3 + V:], edge[1])
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 7), ("bf16", 30000), ("bf16", 50257), ("bf16", 70001), ("bf16", 128256),
+                                     ("bf16", 152064), ("bf16", 160001), ("fp32", 9), ("fp32", 40001),
+                                     ("fp32", 65536), ("fp32", 70001), ("fp32", 128256)])
+def test_step_of_many_rows(gpu_lib, dtype, V):
+    """The one-pass form of the fused call, at every width of it and beyond, against the definition."""
+    N, K, T = 300, min(V, 40), 1.3
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = (3.0 * torch.randn(N, V, generator=g, device="cuda")).to(DT[dtype])
+    t = (z.float() + torch.randn(N, V, generator=g, device="cuda")).to(DT[dtype]).float()
+    v, ids = t.topk(K, dim=1)
+    ids = ids.int()
+    ids[5, ::2] = -1
+    ids[6] = -1
+    ids[7, 0] = V
+    lse = torch.logsumexp(t.double() / T, 1).float()
+    w = torch.rand(N, generator=g, device="cuda") + 0.1
+    w[8] = 0.0
+    for l in (lse, None):
+        o = gpu_lib.distill_step(z, ids, v, w, teacher_lse=l, temperature=T)
+        two = gpu_lib.distill_loss(z, ids, v, teacher_lse=l, temperature=T)
+        torch.cuda.synchronize()
+        rows = [0, 5, 6, 9, 100, 299]
+        want = reference(z[rows].cpu(), ids[rows].cpu(), v[rows].cpu(), None if l is None else l[rows].cpu(), T,
+                         w[rows].cpu())
+        near(o["loss"][rows].cpu(), o["grad"][rows].cpu(), want, w[rows].cpu(), T, dtype)
+        assert int(o["row_err"][7]) == gpu_lib.ERR_TOKEN and bool(o["loss"][7].isnan()) and bool((o["grad"][7] == 0).all())
+        assert float(o["loss"][8]) == 0.0 and bool((o["grad"][8] == 0).all())
+        keep = torch.ones(N, dtype=torch.bool, device="cuda")
+        keep[7:9] = False
+        assert float((o["loss"] - two["loss"])[keep].abs().max()) <= 4e-6
+
+
 def test_graph_replays(gpu_lib):
     N, V, K = 300, 9000, 12
     s, ids, t, lse = inputs(N, V, K, "bf16", seed=3)
