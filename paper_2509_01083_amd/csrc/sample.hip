@@ -166,28 +166,30 @@ __device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
   return __shfl_xor((unsigned long long)v, STRIDE);
 }
 template <int SIZE, int STRIDE>
-__device__ __forceinline__ void sort_steps(uint64_t &v, uint64_t *lds) {
+__device__ __forceinline__ void sort_steps(uint64_t &v, bool used, uint64_t *lds) {
   const uint32_t t = threadIdx.x;
-  uint64_t o;
+  const bool larger = ((t & STRIDE) == 0) == ((t & SIZE) == 0);  // this thread keeps the larger of the two
   if constexpr (STRIDE >= 64) {
     lds[t] = v;
     __syncthreads();
-    o = lds[t ^ STRIDE];
+    const uint64_t o = lds[t ^ STRIDE];
     __syncthreads();
-  } else {
-    o = lane_xor<STRIDE>(v);
+    v = larger == (v < o) ? o : v;
+    sort_steps<SIZE, STRIDE / 2>(v, used, lds);
+  } else if (used) {
+    const uint64_t o = lane_xor<STRIDE>(v);
+    v = larger == (v < o) ? o : v;
+    if constexpr (STRIDE > 1) sort_steps<SIZE, STRIDE / 2>(v, used, lds);
   }
-  const bool first = (t & STRIDE) == 0, desc = (t & SIZE) == 0;
-  v = (first == desc) == (v < o) ? o : v;
-  if constexpr (STRIDE > 1) sort_steps<SIZE, STRIDE / 2>(v, lds);
 }
 // Sorts one value per thread, descending over the first P threads (P the
-// smallest power of two >= n, at least 2; the others pass through): a
-// bitonic network whose partners inside one wavefront exchange by DPP moves
+// smallest power of two >= n, at least 64; the other wavefronts only keep the
+// barriers): a bitonic network whose partners inside one wavefront exchange by DPP moves
 // and shuffles, others through LDS.
 template <int T, int SIZE = 2>
 __device__ __forceinline__ void block_sort(uint64_t &v, uint32_t n, uint64_t *lds) {
-  sort_steps<SIZE, SIZE / 2>(v, lds);
+  const bool used = n > 1 && (threadIdx.x & ~63u) < (1u << (32 - __builtin_clz(n - 1)));
+  sort_steps<SIZE, SIZE / 2>(v, used, lds);
   if constexpr (SIZE < T) {
     if (n > SIZE) block_sort<T, SIZE * 2>(v, n, lds);
   }
@@ -288,6 +290,29 @@ struct KeyTile {
         m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w));
     return m.x > m.y ? m.x : m.y;
   }
+  // The keys that reach kappa (> 0), a bit each: bits w and 16 + w of mask i stand for the two
+  // keys of word 16 i + w.
+  static constexpr int kMasks = (4 * kKeyLoads + 15) / 16;
+  __device__ __forceinline__ void reaching(uint32_t kappa, uint32_t (&mask)[kMasks]) const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 below = {uint16_t(kappa - 1), uint16_t(kappa - 1)}, one = {1, 1};
+#pragma unroll
+    for (int i = 0; i < kMasks; ++i) mask[i] = 0;
+#pragma unroll
+    for (int j = 0; j < kKeyLoads; ++j) {
+      const uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u16x2 d = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, w[i]), below);
+        const u16x2 b = __builtin_elementwise_min(d, one);
+        mask[(4 * j + i) / 16] |= __builtin_bit_cast(uint32_t, b) << ((4 * j + i) % 16);
+      }
+    }
+  }
+  __device__ __forceinline__ static uint32_t mask_place(uint32_t base, int i, int bit) {
+    const uint32_t word = uint32_t(16 * i + (bit & 15));
+    return base + 8 * ((word >> 2) * T + threadIdx.x) + 2 * (word & 3) + uint32_t(bit >> 4);
+  }
   // f(key, place) on every key
   template <typename F>
   __device__ __forceinline__ void each(uint32_t base, F f) const {
@@ -338,19 +363,19 @@ struct Selector {
     if (threadIdx.x == 0) L.n_groups = 0;
     __syncthreads();
     tiles([&](const Tile &x, uint32_t base) {
-      uint32_t n = 0;
-      x.each(base, [&](uint32_t k, uint32_t) { n += k >= kappa; });
+      uint32_t mask[Tile::kMasks], n = 0;
+      x.reaching(kappa, mask);
+#pragma unroll
+      for (int i = 0; i < Tile::kMasks; ++i) n += __popc(mask[i]);
       if (__ballot(n != 0) == 0) return;
       const lanes::Scan<uint32_t> sc = lanes::wave_scan(n);
       uint32_t at = 0;
       if ((threadIdx.x & 63) == 63) at = atomicAdd(&L.n_groups, sc.incl);
       at = lanes::readlane(at, 63) + sc.excl;
-      x.each(base, [&](uint32_t k, uint32_t q) {
-        if (k >= kappa) {
-          if (at < LDS::kGroups) L.list[at] = place_group(q);
-          ++at;
-        }
-      });
+#pragma unroll
+      for (int i = 0; i < Tile::kMasks; ++i)
+        for (; mask[i]; mask[i] &= mask[i] - 1, ++at)
+          if (at < LDS::kGroups) L.list[at] = place_group(Tile::mask_place(base, i, __ffs(mask[i]) - 1));
     });
     __syncthreads();
     return L.n_groups;
