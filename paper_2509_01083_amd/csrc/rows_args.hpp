@@ -19,10 +19,10 @@ inline size_t select_row_bytes(int64_t V) {
   return size_t(num_chunks(V)) * (sizeof(float) * (1 + kSegs) + sizeof(uint16_t) * kChunkGroups) + sizeof(WideRow);
 }
 inline int64_t select_rows_per_pass(int64_t R, int64_t V) {
-  const int64_t n = int64_t(kSelectBytes / select_row_bytes(V));
+  const int64_t n = int64_t((kSelectBytes - 1024) / select_row_bytes(V));
   return n < R ? n : R;
 }
-static_assert(kSelectBytes >= (DSDE_MAX_VOCAB / kChunk) * (4 * (1 + kSegs) + 2 * kChunkGroups) + sizeof(WideRow), "one row fits");
+static_assert(kSelectBytes - 1024 >= (DSDE_MAX_VOCAB / kChunk) * (4 * (1 + kSegs) + 2 * kChunkGroups) + sizeof(WideRow), "one row fits");
 struct SelectLayout {
   size_t max, seg, keys, wide, n_wide, total;
 };
@@ -35,7 +35,9 @@ inline SelectLayout select_layout(int64_t R, int64_t V) {
   l.keys = l.seg + align_up(sizeof(float) * kSegs * n);
   l.wide = l.keys + align_up(sizeof(uint16_t) * kChunkGroups * n);
   l.n_wide = l.wide + align_up(sizeof(WideRow) * size_t(select_rows_per_pass(R, V)));
-  l.total = (all < kSelectBytes ? align_up(all) : kSelectBytes) + 6 * 256;  // grows with R and with V
+  // grows with R and with V; each of the five parts is padded to 256 bytes
+  const size_t whole = align_up(all) + 6 * 256, most = kSelectBytes + 1024;
+  l.total = whole < most ? whole : most;
   return l;
 }
 

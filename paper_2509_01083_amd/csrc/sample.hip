@@ -1167,9 +1167,8 @@ int launch(const SelectArgs &a0, int64_t R, hipStream_t stream) {
       constexpr int DT = decltype(dt)::value, ROW = decltype(row)::value;
       row_scan_kernel<DT, ROW><<<dim3(unsigned(n * nc)), dim3(kThreads), 0, stream>>>(a, r0, nc);
       select_kernel<DT, ROW, TOP><<<dim3(unsigned(n)), dim3(kSelThreads), 0, stream>>>(a, r0, nc);
-      if constexpr (!TOP)
-        if (a.top_k || a.top_p || a.min_p)
-          wide_kernel<DT, ROW><<<dim3(unsigned(n < 256 ? n : 256)), dim3(kWideThreads), 0, stream>>>(a, r0, nc);
+      if constexpr (!TOP)  // without filters too: a greedy row of equal logits may be among its rows
+        wide_kernel<DT, ROW><<<dim3(unsigned(n < 256 ? n : 256)), dim3(kWideThreads), 0, stream>>>(a, r0, nc);
     });
   }
   return hipGetLastError() == hipSuccess ? DSDE_OK : DSDE_DEVICE_ERROR;

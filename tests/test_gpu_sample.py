@@ -177,6 +177,24 @@ def test_graph_replays(gpu_lib):
         assert torch.equal(out["tokens"], want["tokens"]) and torch.equal(out["logprob"], want["logprob"])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_greedy_rows_without_filters(gpu_lib, dtype):
+    """T = 0 with no filter array at all: the lowest of very many equal maxima, and ordinary rows beside."""
+    V = 50000
+    z = torch.randn(6, V, generator=torch.Generator().manual_seed(2))
+    z[0] = 1.5
+    z[1] = -3.3895313892515355e38
+    z[2, 100:] = 9.0
+    z[3, ::2] = -math.inf
+    z = z.to(DT[dtype])
+    T = torch.tensor([0.0, 0.0, 0.0, 0.0, 1.0, 0.0])
+    o = gpu_lib.sample(z.cuda(), T.cuda(), torch.full((6,), 0.5, device="cuda"), kept=True)
+    for i in (0, 1, 2, 3, 5):
+        best = int((z[i].float() == z[i].float().max()).int().argmax())
+        assert int(o["tokens"][i]) == best and int(o["kept"][i]) == 1 and int(o["row_err"][i]) == 0
+    check_draw(z[4].float(), 1.0, 0, 1.0, 0.0, 0.5, int(o["tokens"][4]), float(o["logprob"][4]), int(o["kept"][4]))
+
+
 def test_frequencies(gpu_lib):
     """Draws under top-k and top-p over many uniforms have the kept tokens' probabilities."""
     g = torch.Generator().manual_seed(4)
