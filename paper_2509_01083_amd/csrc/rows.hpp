@@ -39,8 +39,8 @@ inline int strided_rows_form(const void *p, int64_t stride_bytes, int32_t dtype,
 template <int DT, int ROW>
 struct Group {
   static constexpr bool kBf16 = DT == DSDE_BF16;
-  u32x4_t h[ROW != kScalarRows && kBf16 ? 1 : 1];
-  f32x4_t f[ROW == kScalarRows || !kBf16 ? 2 : 1];
+  u32x4_t h[1];  // bf16 rows
+  f32x4_t f[2];  // fp32 rows, and any narrower than one load
   __device__ __forceinline__ void get(const char *row, uint32_t V, uint32_t w) {
     if constexpr (ROW == kScalarRows) {
 #pragma unroll
