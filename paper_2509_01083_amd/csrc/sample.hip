@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
 // took 105 us in two kernels, 74 in three; a call none of whose rows needs it pays 2 to 4 us.
 // A row whose cut lies within the 10,000 largest logits takes about 26 us on its
 // CU, of which 13 are the listing; beyond that its passes over all logits are
-// bound by their instructions (280 per group of 8): 90 us for V = 128,256.
+// bound by their instructions (by the code's count, some 280 per group of 8): 90 us for V = 128,256.
 template <int DT, int ROW>
 __global__ __launch_bounds__(kWideThreads) void wide_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
   __shared__ WideLds L;
