@@ -117,6 +117,25 @@ __device__ __forceinline__ T block_reduce(T v, T *red, OP op) {
   __syncthreads();
   return r;
 }
+// Two sums with one pair of barriers; `red` holds 2 WAVES entries.
+template <int WAVES>
+__device__ __forceinline__ void block_sum2(double &a, double &b, double *red) {
+  a = lanes::wave_sum(a);
+  b = lanes::wave_sum(b);
+  if ((threadIdx.x & 63) == 0) {
+    red[threadIdx.x >> 6] = a;
+    red[WAVES + (threadIdx.x >> 6)] = b;
+  }
+  __syncthreads();
+  a = red[0];
+  b = red[WAVES];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) {
+    a += red[w];
+    b += red[WAVES + w];
+  }
+  __syncthreads();
+}
 // Prefix sums in thread order and their total.
 template <typename T>
 struct BlockScan {

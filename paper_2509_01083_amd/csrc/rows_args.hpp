@@ -9,20 +9,32 @@ namespace dsde {
 // their rows in several passes.  The cap also keeps a pass's keys (an eighth of
 // its logits) inside the last-level cache.
 constexpr size_t kSelectBytes = size_t(192) << 20;
+// The weights of a segment's logits against the largest logit of its chunk: how many logits are that
+// one, and the sum of all others.  A row's log-normaliser is log(ones) + log1p(rest / ones), and the
+// log-probability of a token with nearly all mass is its rest alone, which one fp32 sum with the
+// largest weight, 1, among its terms would round to 2^-24.
+struct SegWeight {
+  float ones, rest;
+};
+// The same of a whole row against its largest logit.
+struct RowSum {
+  double ones, rest;
+};
 // A row left to the cuts over many tokens, with its maximum and the weight of all its logits.
 struct WideRow {
   int32_t row;
   float max;
-  double sum;
+  RowSum sum;
 };
 inline size_t select_row_bytes(int64_t V) {
-  return size_t(num_chunks(V)) * (sizeof(float) * (1 + kSegs) + sizeof(uint16_t) * kChunkGroups) + sizeof(WideRow);
+  return size_t(num_chunks(V)) * (sizeof(float) + sizeof(SegWeight) * kSegs + sizeof(uint16_t) * kChunkGroups) +
+         sizeof(WideRow);
 }
 inline int64_t select_rows_per_pass(int64_t R, int64_t V) {
   const int64_t n = int64_t((kSelectBytes - 1024) / select_row_bytes(V));
   return n < R ? n : R;
 }
-static_assert(kSelectBytes - 1024 >= (DSDE_MAX_VOCAB / kChunk) * (4 * (1 + kSegs) + 2 * kChunkGroups) + sizeof(WideRow), "one row fits");
+static_assert(kSelectBytes - 1024 >= (DSDE_MAX_VOCAB / kChunk) * (4 + 8 * kSegs + 2 * kChunkGroups) + sizeof(WideRow), "one row fits");
 struct SelectLayout {
   size_t max, seg, keys, wide, n_wide, total;
 };
@@ -32,7 +44,7 @@ inline SelectLayout select_layout(int64_t R, int64_t V) {
   SelectLayout l;
   l.max = 0;
   l.seg = l.max + align_up(sizeof(float) * n);
-  l.keys = l.seg + align_up(sizeof(float) * kSegs * n);
+  l.keys = l.seg + align_up(sizeof(SegWeight) * kSegs * n);
   l.wide = l.keys + align_up(sizeof(uint16_t) * kChunkGroups * n);
   l.n_wide = l.wide + align_up(sizeof(WideRow) * size_t(select_rows_per_pass(R, V)));
   // grows with R and with V; each of the five parts is padded to 256 bytes
@@ -54,7 +66,7 @@ struct SelectArgs {
   bool keys_always;
   struct {
     float *max;      // [R, nc] largest logit of each chunk; NaN: a NaN in it
-    float *seg;      // [R, nc, 16] weights of its segments against that
+    SegWeight *seg;  // [R, nc, 16] weights of its segments against that
     uint16_t *keys;  // [R, nc, 1024] high halves of its groups' largest ordered keys
     WideRow *wide;   // [*n_wide] rows left to wide_kernel
     uint32_t *n_wide;

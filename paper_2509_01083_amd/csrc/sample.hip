@@ -4,8 +4,9 @@
 // tokens: the kept set of every filter is a prefix of that order.
 //   row_scan_kernel  reads each row once, one workgroup per chunk of 8,192 logits, and
 //                    leaves per chunk its maximum, the weight of each of its 16 segments
-//                    of 512 logits, and the 16-bit ordered key of the largest logit of each
-//                    group of 8: an eighth of the row's length in keys;
+//                    of 512 logits (the largest logits apart from the rest), and the
+//                    16-bit ordered key of the largest logit of each group of 8: an
+//                    eighth of the row's length in keys;
 //   select_kernel    one workgroup per row: draws without filters from the segments'
 //                    weights; else finds from the keys alone a threshold that enough groups
 //                    reach, reads those groups again, sorts the few logits that reach it too, and cuts;
@@ -85,6 +86,8 @@ __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, 
   const float M = block_max(tm, red);
   float seg[4];
   const float ref = finite_ref(M);
+  const int wave = t >> 6, lane = t & 63;
+  uint32_t ones = 0;  // in lane i: of segment i of the wavefront
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float x = 0.f, y = 0.f;
@@ -94,11 +97,23 @@ __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, 
       y += row_weight(g[i].at(e + 1), ref, s.c);
     }
     seg[i] = x + y;
+    if (__ballot(gm[i] == ref)) {  // one wavefront of the chunk, as a rule: the largest logits apart
+      uint32_t n = 0;
+      x = 0.f;
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) {
+        const float z = g[i].at(e);
+        n += z == ref;
+        x += z == ref ? 0.f : row_weight(z, ref, s.c);
+      }
+      seg[i] = x;
+      n = lanes::wave_sum(n);
+      if (lane == i) ones = n;
+    }
   }
-  const float total = lanes::wave_sum4(seg);
-  const int wave = t >> 6, lane = t & 63;
+  const float rest = lanes::wave_sum4(seg);
   // segment 4 i + wave of the chunk: groups 256 i + 64 wave ...
-  if (lane < 4) a.scan.seg[unit * kSegs + 4 * lane + wave] = total;
+  if (lane < 4) a.scan.seg[unit * kSegs + 4 * lane + wave] = SegWeight{float(ones), rest};
   if (t == 0) a.scan.max[unit] = bad ? NAN : M;
   if (t == 0 && unit == 0) *a.scan.n_wide = 0;
   if (a.keys_always || s.filtered) {
@@ -113,8 +128,11 @@ __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, 
 // the two kernels behind it
 // ---------------------------------------------------------------------------
 
-__device__ __forceinline__ float row_logprob(float z, float m, float T, double S) {
-  return float((double(z) - double(m)) / double(T) - log(S));
+__device__ __forceinline__ double log_of(const RowSum &s) {
+  return s.ones == 1.0 ? log1p(s.rest) : log(s.ones) + log1p(s.rest / s.ones);
+}
+__device__ __forceinline__ float row_logprob(float z, float m, float T, const RowSum &s) {
+  return float((double(z) - double(m)) / double(T) - log_of(s));
 }
 
 // A little below the smallest logit that min_p keeps, as the upper half of a key.
@@ -139,13 +157,14 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   const int64_t r = blockIdx.x, out = row0 + r;
   const Setting s = row_setting(a, out);
   const float *cmax = a.scan.max + r * nc;
-  const float *seg = a.scan.seg + r * nc * kSegs;
+  const SegWeight *seg = a.scan.seg + r * nc * kSegs;
   const int32_t nseg = nc * kSegs;
   const uint32_t V = uint32_t(a.V);
   Selector<DT, ROW, LDS> sel{a.rows.row(out), a.scan.keys + r * nc * kChunkGroups, V, (V + kGroup - 1) / kGroup,
                         uint32_t(nc) * kChunkGroups, 0.f, s.c, L, {}, false, false, 0, 9};
   // the loads that the kernel starts with, together
-  float first_max = -INFINITY, first_seg = 0.f, first_ref = -INFINITY;
+  float first_max = -INFINITY, first_ref = -INFINITY;
+  SegWeight first_seg{0.f, 0.f};
   if (t < nc) first_max = cmax[t];
   if (t < nseg) {
     first_seg = seg[t];
@@ -175,11 +194,22 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
     return;
   }
   sel.m = m;
-  const double part0 = double(first_seg) * double(row_weight(first_ref, m, s.c));
-  double part = part0;
-  for (int32_t i = t + kSelThreads; i < nseg; i += kSelThreads)
-    part += double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c));
-  const double S = block_reduce<W>(part, reinterpret_cast<double *>(L.red64), lanes::Add{});
+  // a segment's weight against m
+  auto seg_weight = [&](const SegWeight &x, float ref) {
+    return (double(x.ones) + double(x.rest)) * double(row_weight(ref, m, s.c));
+  };
+  const double part0 = seg_weight(first_seg, first_ref);
+  RowSum S{0.0, 0.0};
+  auto add = [&](const SegWeight &x, float ref, double weight) {
+    S.ones += ref == m ? double(x.ones) : 0.0;
+    S.rest += ref == m ? double(x.rest) : weight;
+  };
+  add(first_seg, first_ref, part0);
+  for (int32_t i = t + kSelThreads; i < nseg; i += kSelThreads) {
+    const float ref = cmax[i / kSegs];
+    add(seg[i], ref, seg_weight(seg[i], ref));
+  }
+  block_sum2<W>(S.ones, S.rest, reinterpret_cast<double *>(L.red64));
 
   auto emit = [&](int32_t token, float z, int32_t kept) {
     a.tokens[out] = token;
@@ -188,7 +218,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   };
 
   if constexpr (TOP) {
-    if (t == 0) a.lse[out] = float(double(m) / double(s.T) + log(S));
+    if (t == 0) a.lse[out] = float(double(m) / double(s.T) + log_of(S));
     const int32_t k = a.one_k;
     uint64_t v = 0;
     int32_t n = sel.gather(sel.threshold(uint32_t(k)), &v);
@@ -222,7 +252,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
       sel.draw_segment(
           nseg, s.u,
           [&](int32_t i) {
-            return i == t ? part0 : double(seg[i]) * double(row_weight(cmax[i / kSegs], m, s.c));
+            return i == t ? part0 : seg_weight(seg[i], cmax[i / kSegs]);
           });
       if (t < 64) {
         int32_t token;
@@ -250,7 +280,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
         const bool k_in = s.k > 0 && s.k <= n;
         if (k_in && t == s.k - 1) L.mass = cs.incl;
         const int32_t n_min = __syncthreads_count(t < n && e >= s.m);
-        const double mass = k_in ? L.mass : all ? cs.total : S;
+        const double mass = k_in ? L.mass : all ? cs.total : S.ones + S.rest;
         const int32_t n_below = __syncthreads_count(t < n && cs.incl < double(s.p) * mass);
         int32_t lim = kUndecided;
         if (k_in) lim = s.k;
@@ -311,8 +341,9 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(const SelectArgs a, 
                                    false, 0, 9};
     sel.tile.load(sel.keys, sel.places, 0);
     int32_t kept = 0;
-    sel.list_relevant(s.k, s.p, float(w.sum), min_p_key(s, w.max));
-    Cut cut{kEvery, uint64_t(w.sum * double(kFixed))};
+    const double sum = w.sum.ones + w.sum.rest;
+    sel.list_relevant(s.k, s.p, float(sum), min_p_key(s, w.max));
+    Cut cut{kEvery, uint64_t(sum * double(kFixed))};
     const bool by_p = s.p < 1.f;
     if (s.k > 0 || by_p) sel.histogram();
     if (s.k > 0) cut = sel.template weight_cut<false>(uint64_t(s.k), !by_p, s.m, &kept);
@@ -350,7 +381,7 @@ int launch(const SelectArgs &a0, int64_t R, hipStream_t stream) {
   const SelectLayout l = select_layout(R, a.V);
   char *ws = static_cast<char *>(a.workspace);
   a.scan.max = reinterpret_cast<float *>(ws + l.max);
-  a.scan.seg = reinterpret_cast<float *>(ws + l.seg);
+  a.scan.seg = reinterpret_cast<SegWeight *>(ws + l.seg);
   a.scan.keys = reinterpret_cast<uint16_t *>(ws + l.keys);
   a.scan.wide = reinterpret_cast<WideRow *>(ws + l.wide);
   a.scan.n_wide = reinterpret_cast<uint32_t *>(ws + l.n_wide);

@@ -38,7 +38,7 @@ struct SelectLdsOf {
   };
   uint64_t cand[T];  // what the workgroup sorts, one per thread
   uint64_t elems[ELEMS];
-  uint64_t red64[kWaves];
+  uint64_t red64[2 * kWaves];
   uint32_t red32[kWaves];
   float redf[kWaves];
   uint32_t n_groups, n_cand, n_elems;
