@@ -80,11 +80,12 @@ struct Args {
 };
 
 constexpr int kAny = -1;
+constexpr int kErr = -2;  // error bits: int32 or uint32
 constexpr int kI32 = int(at::ScalarType::Int), kI64 = int(at::ScalarType::Long), kU8 = int(at::ScalarType::Byte);
 constexpr int kF32 = int(at::ScalarType::Float), kF64 = int(at::ScalarType::Double);
 
 const char *type_name(int type) {
-  return type == kI32   ? "torch.int32"
+  return type == kI32 || type == kErr ? "torch.int32"
          : type == kI64 ? "torch.int64"
          : type == kU8  ? "torch.uint8"
          : type == kF32 ? "torch.float32"
@@ -98,7 +99,9 @@ void *ptr(PyObject *o, int type, int64_t n, const char *name) {
   if (!THPVariable_Check(o)) fail(std::string(name) + " must be a GPU tensor");
   const at::Tensor &t = THPVariable_Unpack(o);
   if (!t.is_cuda()) fail(std::string(name) + " must be a GPU tensor");
-  if (type != kAny && int(t.scalar_type()) != type) {
+  const at::ScalarType is = t.scalar_type();
+  if (type != kAny && int(is) != type &&
+      !(type == kErr && (is == at::ScalarType::Int || is == at::ScalarType::UInt32))) {
     std::string got = "another type";
     if (PyObject *d = PyObject_GetAttrString(o, "dtype")) {
       if (PyObject *s = PyObject_Str(d)) {
@@ -298,7 +301,7 @@ PyObject *py_verify(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const int32_t k_max = a.int32(), pad = a.int32();
     PyObject *dict = a.next(), *lse = a.next();
     const VerifyOut o = take_verify_out(dict, lse, a.flag(), B, r.N, k_max);
-    uint32_t *err = out<uint32_t>(dict, "seq_err", kAny, B);
+    uint32_t *err = out<uint32_t>(dict, "seq_err", kErr, B);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -325,7 +328,7 @@ PyObject *py_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
     PyObject *dict = a.next(), *lse = a.next();
     const VerifyOut o = take_verify_out(dict, lse, a.flag(), B, r.N, k_max);
     const Signal s = take_signal(a, dict, B);
-    uint32_t *err = out<uint32_t>(dict, "seq_err", kAny, B);
+    uint32_t *err = out<uint32_t>(dict, "seq_err", kErr, B);
     const bool fixed = a.at < a.end && *a.at == Py_False;
     size_t bytes = 0;
     void *ws = nullptr;
@@ -367,7 +370,7 @@ PyObject *py_kld_signal(PyObject *, PyObject *const *args, Py_ssize_t n) {
     float *mu = out<float>(d, "mu_last", kF32, B), *vs = out<float>(d, "var_short", kF32, B);
     float *vl = out<float>(d, "var_long", kF32, B), *wvir = out<float>(d, "wvir", kF32, B);
     float *sf = out<float>(d, "sf", kF32, B);
-    uint32_t *err = out<uint32_t>(d, "seq_err", kAny, B);
+    uint32_t *err = out<uint32_t>(d, "seq_err", kErr, B);
     void *stream = a.stream();
     a.done();
     call([&] {
@@ -390,7 +393,7 @@ PyObject *py_next_sl(PyObject *, PyObject *const *args, Py_ssize_t n) {
     PyObject *d = a.next();
     float *hat = out<float>(d, "sl_hat", kF32, B), *cap = out<float>(d, "sl_cap", kF32, 1);
     int32_t *next = out<int32_t>(d, "sl_next", kI32, B);
-    uint32_t *err = out<uint32_t>(d, "seq_err", kAny, B);
+    uint32_t *err = out<uint32_t>(d, "seq_err", kErr, B);
     void *stream = a.stream();
     a.done();
     call([&] {
@@ -409,7 +412,7 @@ PyObject *py_calibration_update(PyObject *, PyObject *const *args, Py_ssize_t n)
     const auto *cu = static_cast<const int32_t *>(ptr(cu_o, kI32, B + 1, "cu_sl"));
     const auto *acc = static_cast<const int32_t *>(ptr(acc_o, kI32, B, "accepted"));
     const auto *kld = N > 0 ? static_cast<const float *>(ptr(kld_o, kF32, N, "kld")) : nullptr;
-    const auto *err = static_cast<const uint32_t *>(ptr(err_o, kAny, B, "seq_err"));
+    const auto *err = static_cast<const uint32_t *>(ptr(err_o, kErr, B, "seq_err"));
     int32_t *a_max = out<int32_t>(d, "a_max", kI32, B);
     double *sum = out<double>(d, "kld_sum", kF64, B);
     int64_t *cnt = out<int64_t>(d, "kld_count", kI64, B);
@@ -436,7 +439,7 @@ PyObject *py_shard_stats(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void *ws = take_workspace(a, &bytes);
     PyObject *part_o = a.next();
     void *part = r.N > 0 ? ptr(part_o, kU8, r.N * int64_t(sizeof(dsde_shard_partial)), "part") : nullptr;
-    uint32_t *err = take<uint32_t>(a, kAny, B, "seq_err");
+    uint32_t *err = take<uint32_t>(a, kErr, B, "seq_err");
     void *stream = a.stream();
     a.done();
     call([&] {
@@ -468,7 +471,7 @@ PyObject *py_shard_accept(PyObject *, PyObject *const *args, Py_ssize_t n) {
     PyObject *dict = a.next(), *lse = a.next();
     const VerifyOut o = take_verify_out(dict, lse, a.flag(), B, N, k_max);
     auto *jobs = out<dsde_draw_job>(dict, "jobs", kU8, B * int64_t(sizeof(dsde_draw_job)));
-    uint32_t *err = take<uint32_t>(a, kAny, B, "seq_err");
+    uint32_t *err = take<uint32_t>(a, kErr, B, "seq_err");
     Signal s{};
     if (fused) s = take_signal(a, dict, B);
     void *stream = a.stream();
@@ -526,7 +529,7 @@ PyObject *py_shard_draw_pick(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const int32_t k_max = a.int32(), pad = a.int32();
     int32_t *accepted = take<int32_t>(a, kI32, B, "accepted");
     int32_t *tokens = take<int32_t>(a, kI32, B * (k_max + 1), "tokens"), *drawn = take<int32_t>(a, kI32, B, "drawn");
-    uint32_t *err = take<uint32_t>(a, kAny, B, "seq_err");
+    uint32_t *err = take<uint32_t>(a, kErr, B, "seq_err");
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -573,7 +576,7 @@ PyObject *py_sample(PyObject *, PyObject *const *args, Py_ssize_t n) {
     auto *tokens = out<int32_t>(dict, "tokens", kI32, z.R);
     auto *lp = PyMapping_HasKeyString(dict, "logprob") ? out<float>(dict, "logprob", kF32, z.R) : nullptr;
     auto *kept = PyMapping_HasKeyString(dict, "kept") ? out<int32_t>(dict, "kept", kI32, z.R) : nullptr;
-    auto *err = out<uint32_t>(dict, "row_err", kAny, z.R);
+    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -594,7 +597,7 @@ PyObject *py_top_logits(PyObject *, PyObject *const *args, Py_ssize_t n) {
     auto *values = out<float>(dict, "values", kF32, z.R * k);
     auto *ids = out<int32_t>(dict, "ids", kI32, z.R * k);
     auto *lse = out<float>(dict, "lse", kF32, z.R);
-    auto *err = out<uint32_t>(dict, "row_err", kAny, z.R);
+    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -640,7 +643,7 @@ PyObject *py_distill_loss(PyObject *, PyObject *const *args, Py_ssize_t n) {
     PyObject *dict = a.next();
     auto *loss = out<float>(dict, "loss", kF32, z.R);
     auto *record = out<dsde_distill_row>(dict, "record", kU8, z.R * int64_t(sizeof(dsde_distill_row)));
-    auto *err = out<uint32_t>(dict, "row_err", kAny, z.R);
+    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -679,7 +682,7 @@ PyObject *py_distill_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const auto *weight = take<float>(a, kF32, z.R, "weight");
     auto *loss = take<float>(a, kF32, z.R, "loss");
     const LogitRows g = take_gradient(a, z);
-    auto *err = take<uint32_t>(a, kAny, z.R, "row_err");
+    auto *err = take<uint32_t>(a, kErr, z.R, "row_err");
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
