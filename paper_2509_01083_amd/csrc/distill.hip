@@ -16,20 +16,24 @@
 namespace dsde {
 namespace {
 
-// 2^(z c - ref c), one fused operation and an exponential.  ref c is rounded, but
-// to the same number for every token that is weighed against it.  Where it is
-// beyond 2^100 (rows masked with the type's lowest value throughout) the difference is taken first.
+// 2^(z c - ref c), one fused operation and an exponential.  ref c is rounded, by up to
+// half a unit of its last place, but to the same number for every token that is weighed
+// against it: a weight against ref itself is then 2^(ref c - scaled), within 2^(1/32) of 1 as long
+// as |ref c| < 2^20.  Beyond that (chunks masked throughout, with -1e9 or the type's lowest
+// value, say) the difference is taken first; the rounding would soon carry weights out of fp32's range.
 struct Weigher {
   float ref, c, scaled;
   bool far;
   __device__ __forceinline__ Weigher(float M, float c_) : ref(finite_ref(M)), c(c_) {
     scaled = ref * c;
-    far = !(fabsf(scaled) < 0x1p100f);
+    far = !(fabsf(scaled) < 0x1p20f);
   }
   template <bool FAR>
   __device__ __forceinline__ float of(float z) const {
     return FAR ? row_weight(z, ref, c) : fast_exp2(fmaf(z, c, -scaled));
   }
+  // the log2 that weights of 1 stand for
+  __device__ __forceinline__ double base() const { return far ? double(ref) * double(c) : double(scaled); }
 };
 // A group's weights: four pairs in fp32, added in fp32.
 template <bool FAR, typename G>
@@ -135,15 +139,13 @@ __device__ __forceinline__ double log_of(double s) {
   return (double(e) + double(__builtin_amdgcn_logf(f)) + double(d * kLog2e * __builtin_amdgcn_rcpf(f))) * kLn2;
 }
 
-// The log2 of a reference's scale, ref c as Weigher rounds it, against that of m, and the factor that
+// The log2 of what a weight of 1 against `ref` stands for, against 2^(m c), and the factor that
 // takes sums against `ref` to sums against `to`.
 __device__ __forceinline__ double ref_log2(float ref, float m, float c) {
-  const Weigher w(ref, c);
-  return w.far ? (double(ref) - double(m)) * double(c) : double(w.scaled) - double(m) * double(c);
+  return Weigher(ref, c).base() - double(m) * double(c);
 }
 __device__ __forceinline__ double ref_factor(float ref, float to, float c) {
-  const Weigher x(ref, c), y(to, c);
-  return x.far || y.far ? double(row_weight(ref, to, c)) : exp2_of(double(x.scaled) - double(y.scaled));
+  return exp2_of(Weigher(ref, c).base() - Weigher(to, c).base());
 }
 
 // The teacher's side of one row and the student's logits at its tokens, by one
