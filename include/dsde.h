@@ -474,7 +474,8 @@ size_t dsde_sample_workspace_bytes(int64_t R, int64_t V);
  *   pad_id                    token of flagged rows
  * Outputs:
  *   tokens [R]        int32   the smallest id whose cumulative weight over the kept
- *                             tokens, in ascending id order, exceeds u times their total
+ *                             tokens, in ascending id order, exceeds u times their total (tokens
+ *                             under 2^-116 of the largest weight may count as weight 0)
  *   logprob [R]       float   optional: log softmax(z / T) of that token over the whole row
  *                             (T = 0: at T = 1)
  *   kept [R]          int32   optional: how many tokens the filters kept (at least 1),

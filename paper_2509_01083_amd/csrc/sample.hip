@@ -249,11 +249,12 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
   } else {
     if (!s.filtered) {
       const uint32_t n = a.kept ? block_reduce<W>(sel.unmasked(), L.red32, lanes::Add{}) : 0u;
-      sel.draw_segment(
-          nseg, s.u,
-          [&](int32_t i) {
-            return i == t ? part0 : seg_weight(seg[i], cmax[i / kSegs]);
-          });
+      // A segment's weight is a product of two, of which the smaller may be of any size, while its
+      // tokens are weighed against m at once and vanish under 2^-126: of 512 that add up to 2^-116 one does not.
+      sel.draw_segment(nseg, s.u, [&](int32_t i) {
+        const double x = i == t ? part0 : seg_weight(seg[i], cmax[i / kSegs]);
+        return x >= 0x1p-116 ? x : 0.0;
+      });
       if (t < 64) {
         int32_t token;
         float z;

@@ -1,6 +1,11 @@
-"""dsde_sample and dsde_top_logits at the ends of their ranges: rows whose largest logit holds nearly all mass."""
+"""dsde_sample and dsde_top_logits at the ends of their ranges: rows whose largest logit holds nearly all mass,
+uniforms of 0 on rows whose weights underflow."""
+import math
+
 import pytest
 import torch
+
+from rows_reference import check_draw
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
@@ -17,6 +22,13 @@ def draw(lib, z, par, u):
     o = lib.sample(z.cuda(), T, torch.as_tensor(u, dtype=torch.float32).cuda(), top_k=k, top_p=p, min_p=m, kept=True)
     assert (o["row_err"] == 0).all()
     return {k: v.cpu() for k, v in o.items()}
+
+
+def check(o, z, par, u):
+    for i, row in enumerate(par):
+        T, k, p, m = (float(torch.tensor(x, dtype=torch.float32)) for x in row)
+        check_draw(z[i].float(), T, int(k), p, m, float(torch.tensor(u[i], dtype=torch.float32)), int(o["tokens"][i]),
+                   float(o["logprob"][i]), int(o["kept"][i]))
 
 
 # log p = -log1p(rest), and the row's lse = log1p(rest) where its largest logit is 0: as exact as the sum of the other
@@ -63,3 +75,19 @@ def test_logprob_of_several_equal_maxima(gpu_lib, dtype):
         rest = z.double().exp().sum(1) - n
         want = n.log() + torch.log1p(rest / n)
         assert bool(((o["logprob"].double() + want).abs() <= rest_tol(22.0) * want).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T", [0.05, 0.01, 2.0 ** -10])
+@pytest.mark.parametrize("masked", [0, 1, 600, 9000])
+def test_uniform_of_zero_where_weights_underflow(gpu_lib, masked, T, dtype):
+    """Segments whose weight is the product of two tiny numbers hold no token of positive weight: the draw passes them
+    over.  The first tokens are masked, so that none of them may be drawn."""
+    V, R = 128256, 24
+    g = torch.Generator().manual_seed(masked + 1)
+    z = 4.0 * torch.randn(R, V, generator=g)
+    z[:, :masked] = -math.inf
+    z = z.to(DT[dtype])
+    for par in ((T, 0, 1.0, 0.0), (T, 50, 1.0, 0.0), (T, 3000, 1.0, 0.0)):
+        o = draw(gpu_lib, z, [par] * R, [0.0] * R)
+        check(o, z, [par] * R, [0.0] * R)
