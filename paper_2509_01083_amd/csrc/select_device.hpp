@@ -532,7 +532,9 @@ struct Selector {
     const uint64_t count0 = L.found_before, mass0 = L.mass_before;
     __syncthreads();
     Cut cut;
-    if (bin < 0 && min_bound) {  // min_p's tokens, which are listed, end before the cut
+    // min_p's tokens, which are listed, end before the cut; that the histogram does not reach it says so
+    // only where it holds all of them (weights over 2^-32), and key_cut looks further where it does not
+    if (bin < 0 && min_bound && min_p >= 0x1p-31f) {
       if (last) add_segments(kEvery, min_p, kept);
       return Cut{kEvery, 0};
     }

@@ -1,11 +1,11 @@
 """dsde_sample and dsde_top_logits at the ends of their ranges: rows whose largest logit holds nearly all mass,
-uniforms of 0 on rows whose weights underflow."""
+uniforms of 0 on rows whose weights underflow, filters below the histogram's range."""
 import math
 
 import pytest
 import torch
 
-from rows_reference import check_draw
+from rows_reference import check_draw, sample_row
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
@@ -91,3 +91,19 @@ def test_uniform_of_zero_where_weights_underflow(gpu_lib, masked, T, dtype):
     for par in ((T, 0, 1.0, 0.0), (T, 50, 1.0, 0.0), (T, 3000, 1.0, 0.0)):
         o = draw(gpu_lib, z, [par] * R, [0.0] * R)
         check(o, z, [par] * R, [0.0] * R)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [6001, 50257, 131072])
+def test_min_p_below_the_histogram(gpu_lib, V, dtype):
+    """min_p under 2^-32 with a top_k whose last token lies more than 32 octaves below the maximum: top_k cuts where it
+    is the shorter one, and min_p where that is."""
+    par = [(0.2, 300, 1.0, 1e-12), (0.1, 300, 1.0, 1e-30), (0.1, 2000, 1.0, 1e-20), (0.1, 600, 1.0, 1e-25),
+           (0.05, 1000, 1.0, 1e-37), (0.2, 1200, 1.0, 2.0 ** -31), (0.2, 1200, 1.0, 2.0 ** -32), (0.1, 300, 1.0, 1e-12),
+           (0.1, 700, 0.999999, 1e-30), (0.1, 0, 0.999999, 1e-30), (0.1, 0, 1.0, 1e-30)]
+    g = torch.Generator().manual_seed(V)
+    z = (3.0 * torch.randn(len(par), V, generator=g)).to(DT[dtype])
+    u = torch.rand(len(par), generator=g).tolist()
+    cut = [sample_row(z[i].float(), T, k, p, float(torch.tensor(m)))[3] for i, (T, k, p, m) in enumerate(par)]
+    assert 300 in cut or V < 10000  # top_k is what cuts at least one of the wider ones
+    check(draw(gpu_lib, z, par, u), z, par, u)
