@@ -128,18 +128,31 @@ int64_t size_of(PyObject *o, int64_t dim, const char *name) {
   if (t.dim() <= dim) fail(std::string(name) + " has too few dimensions");
   return t.size(dim);
 }
+// Raises the version of a tensor that the call writes, as torch's own operations in place do: a
+// backward that has saved it then refuses it.  (Inference tensors have no version.)
+void written(PyObject *o) {
+  if (o == Py_None) return;
+  const at::Tensor &t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // Outputs are taken from the caller's dict, or other mapping, by key.  A
 // mapping's item is a new reference, dropped once its pointer is known (as
-// with the inputs, the caller keeps the tensor itself alive).
+// with the inputs, the caller keeps the tensor itself alive).  `versioned`: outputs that a
+// graph may hold, as the teacher's entries of a distillation.
 template <typename T>
-T *out(PyObject *dict, const char *key, int type, int64_t n) {
+T *out(PyObject *dict, const char *key, int type, int64_t n, bool versioned = false) {
+  const auto take = [&](PyObject *o) {
+    T *p = static_cast<T *>(ptr(o, type, n, key));
+    if (versioned) written(o);
+    return p;
+  };
   if (PyDict_CheckExact(dict)) {
     PyObject *o = PyDict_GetItemString(dict, key);
     if (!o) {
       PyErr_SetString(PyExc_KeyError, key);
       throw Failed{};
     }
-    return static_cast<T *>(ptr(o, type, n, key));
+    return take(o);
   }
   struct Ref {
     PyObject *o;
@@ -148,7 +161,7 @@ T *out(PyObject *dict, const char *key, int type, int64_t n) {
   const Ref k{PyUnicode_FromString(key)};
   const Ref o{k.o ? PyObject_GetItem(dict, k.o) : nullptr};
   if (!o.o) throw Failed{};
-  return static_cast<T *>(ptr(o.o, type, n, key));
+  return take(o.o);
 }
 
 int32_t logits_type(const at::Tensor &t) {
@@ -573,10 +586,10 @@ PyObject *py_sample(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const auto *u = take<float>(a, kF32, z.R, "u");
     const int32_t pad = a.int32();
     PyObject *dict = a.next();
-    auto *tokens = out<int32_t>(dict, "tokens", kI32, z.R);
-    auto *lp = PyMapping_HasKeyString(dict, "logprob") ? out<float>(dict, "logprob", kF32, z.R) : nullptr;
-    auto *kept = PyMapping_HasKeyString(dict, "kept") ? out<int32_t>(dict, "kept", kI32, z.R) : nullptr;
-    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R);
+    auto *tokens = out<int32_t>(dict, "tokens", kI32, z.R, true);
+    auto *lp = PyMapping_HasKeyString(dict, "logprob") ? out<float>(dict, "logprob", kF32, z.R, true) : nullptr;
+    auto *kept = PyMapping_HasKeyString(dict, "kept") ? out<int32_t>(dict, "kept", kI32, z.R, true) : nullptr;
+    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R, true);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -594,10 +607,10 @@ PyObject *py_top_logits(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const int32_t k = a.int32();
     const float T = a.real();
     PyObject *dict = a.next();
-    auto *values = out<float>(dict, "values", kF32, z.R * k);
-    auto *ids = out<int32_t>(dict, "ids", kI32, z.R * k);
-    auto *lse = out<float>(dict, "lse", kF32, z.R);
-    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R);
+    auto *values = out<float>(dict, "values", kF32, z.R * k, true);
+    auto *ids = out<int32_t>(dict, "ids", kI32, z.R * k, true);
+    auto *lse = out<float>(dict, "lse", kF32, z.R, true);
+    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R, true);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -630,6 +643,7 @@ Teacher take_teacher(Args &a, int64_t N) {
 LogitRows take_gradient(Args &a, const LogitRows &z) {
   const LogitRows g = take_strided(a, "grad");
   if (g.R != z.R || g.V != z.V || g.dtype != z.dtype) fail("grad must have the logits' shape and type");
+  written(a.at[-1]);
   return g;
 }
 
@@ -641,9 +655,9 @@ PyObject *py_distill_loss(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const auto *lse = take<float>(a, kF32, z.R, "teacher_lse");
     const float T = a.real();
     PyObject *dict = a.next();
-    auto *loss = out<float>(dict, "loss", kF32, z.R);
-    auto *record = out<dsde_distill_row>(dict, "record", kU8, z.R * int64_t(sizeof(dsde_distill_row)));
-    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R);
+    auto *loss = out<float>(dict, "loss", kF32, z.R, true);
+    auto *record = out<dsde_distill_row>(dict, "record", kU8, z.R * int64_t(sizeof(dsde_distill_row)), true);
+    auto *err = out<uint32_t>(dict, "row_err", kErr, z.R, true);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
@@ -681,8 +695,10 @@ PyObject *py_distill_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const float T = a.real();
     const auto *weight = take<float>(a, kF32, z.R, "weight");
     auto *loss = take<float>(a, kF32, z.R, "loss");
+    written(a.at[-1]);
     const LogitRows g = take_gradient(a, z);
     auto *err = take<uint32_t>(a, kErr, z.R, "row_err");
+    written(a.at[-1]);
     size_t bytes;
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
