@@ -123,33 +123,19 @@ __global__ __launch_bounds__(kThreads) void distill_scan_kernel(const DistillArg
   if (t == 0) a.part[unit] = DistillPartial{bad ? NAN : M, tokens.twice, sum};
 }
 
-// exp and log of a row's scalars in fp64, good to about 1e-7 of the value and of 1: the
-// hardware's fp32 functions on what is left of the argument after its power of
-// two.  The library's take some twenty constants each, which a loop over rows keeps
-// in registers.
-__device__ __forceinline__ double exp2_of(double x) {
-  const double y = fmax(x, -4096.0), n = rint(y);
-  return ldexp(double(fast_exp2(float(y - n))), int(n));
-}
-__device__ __forceinline__ double exp_of(double x) { return exp2_of(x * 1.4426950408889634); }
-__device__ __forceinline__ double log_of(double s) {
-  int e;
-  const double m = frexp(s, &e);
-  const float f = float(m), d = float(m - double(f));
-  return (double(e) + double(__builtin_amdgcn_logf(f)) + double(d * kLog2e * __builtin_amdgcn_rcpf(f))) * kLn2;
-}
-
 // The log2 of what a weight of 1 against `ref` stands for, against 2^(m c), and the factor that
 // takes sums against `ref` to sums against `to`.
 __device__ __forceinline__ double ref_log2(float ref, float m, float c) {
   return Weigher(ref, c).base() - double(m) * double(c);
 }
 __device__ __forceinline__ double ref_factor(float ref, float to, float c) {
-  return exp2_of(Weigher(ref, c).base() - Weigher(to, c).base());
+  return exp2(Weigher(ref, c).base() - Weigher(to, c).base());
 }
 
 // The teacher's side of one row and the student's logits at its tokens, by one
-// wavefront (entry k in lane k % 64), the same in every lane.
+// wavefront (entry k in lane k % 64), the same in every lane.  A row's few scalars take fp64's exp and
+// log: 1 - sum p of a teacher of nearly one token, and the logarithm of a student's sum just over 1, are
+// small differences, of which functions good to 1e-7 would leave a loss of 1e-5 two or three digits.
 constexpr int kPerLane = DSDE_MAX_TOP / 64;
 constexpr float kInf = __builtin_inff();
 struct TeacherRow {
@@ -206,8 +192,8 @@ __device__ __forceinline__ TeacherRow teacher_row(const DistillArgs &a, int64_t 
   r.student = lanes::wave_sum(r.student);
   esum = lanes::wave_sum(esum);
   // log p_k = (t_k - tmax) / T + log scale
-  const double logs = r.tmax == -kInf ? 0.0 : tail ? double(r.tmax) * iT - L : -log_of(esum);
-  r.scale = exp_of(logs);
+  const double logs = r.tmax == -kInf ? 0.0 : tail ? double(r.tmax) * iT - L : -log(esum);
+  r.scale = exp(logs);
   r.sum = esum * r.scale;
   double cross = 0.0;
 #pragma unroll
@@ -235,12 +221,12 @@ __device__ __forceinline__ RowLoss row_loss(const DistillArgs &a, const TeacherR
   const float c = kLog2e / a.temperature;
   const double ds = r.smax > -kInf ? (double(r.smax) - double(m)) * double(c) * kLn2 : 0.0;
   const double dr = rmax > -kInf ? ref_log2(rmax, m, c) * kLn2 : 0.0;
-  const double es = exp_of(ds), er = rmax > -kInf ? exp_of(dr) : 0.0;
-  const double S = r.student * es + rest * er, logS = log_of(S);
+  const double es = exp(ds), er = rmax > -kInf ? exp(dr) : 0.0;
+  const double S = r.student * es + rest * er, logS = log(S);
   const double tail = a.teacher_lse && r.sum < 1.0 ? 1.0 - r.sum : 0.0;
   double loss = r.cross - r.sum * (ds - logS), share = 0.0;  // share: what the rest's gradient adds up to
   if (rest > 0.0) {
-    if (tail > 0.0) loss += tail * (log_of(tail) - (dr + log_of(rest) - logS));
+    if (tail > 0.0) loss += tail * (log(tail) - (dr + log(rest) - logS));
     share = rest * er / S - tail;
   }
   return RowLoss{float(loss), 0,

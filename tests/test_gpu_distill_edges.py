@@ -1,7 +1,8 @@
-"""dsde_distill_* at the ends of their ranges: masks of any size over whole chunks."""
+"""dsde_distill_* at the ends of their ranges: masks of any size over whole chunks, losses near 0."""
 import pytest
 import torch
 
+from rows_reference import WEIGHT_TOL
 from test_gpu_distill import DT, inputs, near, reference, run_all
 
 pytestmark = pytest.mark.gpu
@@ -13,7 +14,7 @@ MASKS = (-1e4, -1e6, -1e9, -1e10, -1e11, -1e12, -1e13, -1e18, -1e20, -1e29, -1e3
 @pytest.mark.parametrize("T", [0.5, 1.0, 1.5, 2.0])
 @pytest.mark.parametrize("tail", [False, True])
 def test_chunks_of_masked_logits(gpu_lib, tail, T, dtype):
-    """A finite mask over whole chunks of 8,192 logits and over a short last one: the chunks' own maxima are the mask."""
+    """A finite mask over whole chunks of 8,192 logits and over a short last one, whose maxima are the mask."""
     V, K = 3 * 8192 + 700, 24
     s, _, t, _ = inputs(len(MASKS), V, K, "fp32", seed=9)
     out = torch.zeros(V, dtype=torch.bool)
@@ -46,3 +47,41 @@ def test_chunks_on_both_sides_of_a_large_offset(gpu_lib, tail, base):
     want = reference(s, ids.int(), v, lse, 1.0, torch.ones(N))
     for loss, grad in run_all(gpu_lib, s, ids.int(), v, lse, 1.0, torch.ones(N)):
         near(loss, grad, want, torch.ones(N), 1.0, "fp32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_loss_near_zero(gpu_lib, dtype):
+    """A teacher of one token that the student nearly always gives: loss = log1p(rest), as exact as the sum of the rest's
+    weights.  A weight e^-x is off by (1.5 x + 1) 2^-23 of itself at most, the sums of eight in fp32 by 3 2^-24, the
+    result by 2^-24."""
+    V, gaps = 50257, (12.0, 14.0, 16.0, 18.0, 20.0, 22.0, 24.0)
+    g = torch.Generator().manual_seed(8)
+    s = torch.randn(len(gaps), V, generator=g) - torch.tensor(gaps)[:, None]
+    ids = torch.randint(0, V, (len(gaps), 1), generator=g)
+    s = s.scatter(1, ids, 0.0).to(DT[dtype])
+    want = torch.log1p(s.double().exp().scatter(1, ids, 0.0).sum(1))
+    tol = ((1.5 * torch.tensor(gaps).double() + 1) * 2.0 ** -23 + 4 * 2.0 ** -24) * want
+    for loss, _ in run_all(gpu_lib, s, ids.int(), torch.zeros(len(gaps), 1), None, 1.0, torch.ones(len(gaps))):
+        assert bool(((loss.double() - want).abs() <= tol).all()), loss.double() / want - 1
+
+
+def test_small_tail_of_the_teacher(gpu_lib):
+    """One entry with all but r of the mass: r = 1 - exp(t - lse) keeps its digits, and the loss's terms theirs.  Each
+    term is a product of p or r (exact here but for the fp64 functions) and a logarithm of the student's sums."""
+    V, N = 9001, 12
+    g = torch.Generator().manual_seed(4)
+    s = torch.randn(N, V, generator=g) - 14.0
+    ids = torch.randint(0, V, (N, 1), generator=g)
+    s.scatter_(1, ids, 0.0)
+    lse = 2.0 ** -torch.arange(4, 4 + N).float() * (1 + torch.rand(N, generator=g))
+    t = torch.zeros(N, 1)
+    p = (-lse.double()).exp()
+    r = 1 - p
+    rest = s.double().exp().scatter(1, ids, 0.0).sum(1)
+    log_all = torch.log1p(rest)
+    terms = torch.stack([p * -lse.double(), p * log_all, r * r.log(), -r * rest.log(), r * log_all])
+    want = terms.sum(0)
+    # rest's weights and their sum move log1p(rest) and log(rest); then fp32's rounding
+    tol = (WEIGHT_TOL + 4 * 2.0 ** -24) * (p * log_all + r + r * log_all) + 2.0 ** -24 * want.abs()
+    for loss, _ in run_all(gpu_lib, s, ids.int(), t, lse, 1.0, torch.ones(N)):
+        assert bool(((loss.double() - want).abs() <= tol).all()), (loss.double() - want) / tol
