@@ -377,23 +377,48 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
 
 }  // namespace
 
-int launch_distill_loss(const DistillArgs &a, int64_t N, hipStream_t stream) {
+// A launch takes fewer than 2^32 threads: rows of 2^23 chunks at a time (2^31 threads).
+template <typename F>
+static void each_pass(const DistillArgs &a0, int64_t N, F f) {
+  const int64_t nc = num_chunks(a0.V), per_pass = (int64_t(1) << 23) / nc;
+  for (int64_t r0 = 0; r0 < N; r0 += per_pass) {
+    DistillArgs a = a0;
+    a.rows.base += r0 * a.rows.stride;
+    a.ids += r0 * a.K;
+    a.teacher += r0 * a.K;
+    if (a.teacher_lse) a.teacher_lse += r0;
+    if (a.weight) a.weight += r0;
+    if (a.part) a.part += r0 * nc;
+    a.record += r0;
+    if (a.loss) a.loss += r0;
+    if (a.row_err) a.row_err += r0;
+    if (a.grad) a.grad += r0 * a.grad_stride;
+    f(a, N - r0 < per_pass ? N - r0 : per_pass, int32_t(nc));
+  }
+}
+static_assert((int64_t(1) << 23) / (DSDE_MAX_VOCAB / kChunk) > 0, "a row fits a launch");
+
+int launch_distill_loss(const DistillArgs &a0, int64_t N, hipStream_t stream) {
   (void)hipGetLastError();
-  const int32_t nc = int32_t(num_chunks(a.V));
-  by_rows(a.dtype, strided_rows_form(a.rows.base, a.rows.stride, a.dtype, a.V), [&](auto dt, auto row) {
-    distill_scan_kernel<decltype(dt)::value, decltype(row)::value>
-        <<<dim3(unsigned(N * nc)), dim3(kThreads), 0, stream>>>(a, nc);
+  const int form = strided_rows_form(a0.rows.base, a0.rows.stride, a0.dtype, a0.V);
+  each_pass(a0, N, [&](const DistillArgs &a, int64_t n, int32_t nc) {
+    by_rows(a.dtype, form, [&](auto dt, auto row) {
+      distill_scan_kernel<decltype(dt)::value, decltype(row)::value>
+          <<<dim3(unsigned(n * nc)), dim3(kThreads), 0, stream>>>(a, nc);
+    });
+    distill_finish_kernel<<<dim3(unsigned((n + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream>>>(a, n, nc);
   });
-  distill_finish_kernel<<<dim3(unsigned((N + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream>>>(a, N, nc);
   return hipGetLastError() == hipSuccess ? DSDE_OK : DSDE_DEVICE_ERROR;
 }
 
-int launch_distill_grad(const DistillArgs &a, int64_t N, hipStream_t stream) {
+int launch_distill_grad(const DistillArgs &a0, int64_t N, hipStream_t stream) {
   (void)hipGetLastError();
-  const int32_t nc = int32_t(num_chunks(a.V));
-  by_rows(a.dtype, strided_rows_form(a.rows.base, a.rows.stride, a.dtype, a.V), [&](auto dt, auto row) {
-    distill_grad_kernel<decltype(dt)::value, decltype(row)::value>
-        <<<dim3(unsigned(N * nc)), dim3(kThreads), 0, stream>>>(a, nc);
+  const int form = strided_rows_form(a0.rows.base, a0.rows.stride, a0.dtype, a0.V);
+  each_pass(a0, N, [&](const DistillArgs &a, int64_t n, int32_t nc) {
+    by_rows(a.dtype, form, [&](auto dt, auto row) {
+      distill_grad_kernel<decltype(dt)::value, decltype(row)::value>
+          <<<dim3(unsigned(n * nc)), dim3(kThreads), 0, stream>>>(a, nc);
+    });
   });
   return hipGetLastError() == hipSuccess ? DSDE_OK : DSDE_DEVICE_ERROR;
 }

@@ -1,4 +1,4 @@
-"""dsde_distill_* at the ends of their ranges: masks of any size over whole chunks, losses near 0."""
+"""dsde_distill_* at the ends of their ranges: masks of any size over whole chunks, losses near 0, very many rows."""
 import pytest
 import torch
 
@@ -85,3 +85,26 @@ def test_small_tail_of_the_teacher(gpu_lib):
     tol = (WEIGHT_TOL + 4 * 2.0 ** -24) * (p * log_all + r + r * log_all) + 2.0 ** -24 * want.abs()
     for loss, _ in run_all(gpu_lib, s, ids.int(), t, lse, 1.0, torch.ones(N)):
         assert bool(((loss.double() - want).abs() <= tol).all()), (loss.double() - want) / tol
+
+
+def test_more_rows_than_one_launch_takes(gpu_lib):
+    """2^24 rows and more: a launch of 256 threads for each would pass 2^32 threads."""
+    N, V, K = (1 << 24) + 5, 8, 1
+    z = torch.zeros(N, V, dtype=torch.bfloat16, device="cuda")
+    rows = [0, 1, (1 << 23) - 1, 1 << 23, (1 << 24) - 1, 1 << 24, N - 1]
+    g = torch.Generator().manual_seed(3)
+    z[rows] = torch.randn(len(rows), V, generator=g).to(torch.bfloat16).cuda()
+    ids = torch.full((N, K), 3, dtype=torch.int32, device="cuda")
+    t = torch.ones(N, K, device="cuda")
+    w = torch.ones(N, device="cuda")
+    s = z[rows].cpu()
+    want = reference(s, ids[rows].cpu(), t[rows].cpu(), None, 1.0, torch.ones(len(rows)))
+    o = gpu_lib.distill_loss(z, ids, t)
+    grad = gpu_lib.distill_grad(z, ids, t, o["record"], w)
+    f = gpu_lib.distill_step(z, ids, t, w)
+    for x, y in ((o["loss"], grad), (f["loss"], f["grad"])):
+        near(x[rows].cpu(), y[rows].cpu(), want, torch.ones(len(rows)), 1.0, "bf16")
+        plain = torch.ones(N, dtype=torch.bool, device="cuda")
+        plain[rows] = False
+        # all other rows are equal
+        assert bool((x[plain] == x[2]).all()) and bool((y[plain] == y[2]).all())
