@@ -302,14 +302,11 @@ __device__ __forceinline__ void put_group(char *row, uint32_t V, uint32_t w, con
   }
 }
 
-// The teacher's probability of an entry, and the gradient there; without contraction of the
-// products, so that every caller sees the same bits.
+// The teacher's probability of an entry, and the gradient there.
 __device__ __forceinline__ float teacher_p(float logit, const dsde_distill_row &r, float c) {
-#pragma clang fp contract(off)
   return row_weight(logit, r.teacher_ref, c) * r.teacher_scale;
 }
 __device__ __forceinline__ float entry_gradient(float z, float p, const dsde_distill_row &r, float c, float scale) {
-#pragma clang fp contract(off)
   return scale * (row_weight(z, r.ref, c) * r.scale - p);
 }
 
