@@ -1,4 +1,5 @@
-"""dsde_distill_* at the ends of their ranges: masks of any size over whole chunks, losses near 0, very many rows."""
+"""dsde_distill_* at the ends of their ranges: masks of any size over whole chunks, losses near 0, very many rows; the
+fused call against the two it stands for."""
 import pytest
 import torch
 
@@ -108,3 +109,18 @@ def test_more_rows_than_one_launch_takes(gpu_lib):
         plain[rows] = False
         # all other rows are equal
         assert bool((x[plain] == x[2]).all()) and bool((y[plain] == y[2]).all())
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype,V", [("bf16", 7), ("bf16", 30001), ("bf16", 128256), ("fp32", 9), ("fp32", 70001)])
+def test_step_is_loss_and_gradient_bit_for_bit(gpu_lib, dtype, V, tail):
+    """The fused call runs the kernels of the other two: the same bits, on rows that are neither left out nor flagged."""
+    N, T = 64, 1.3
+    s, ids, t, lse = inputs(N, V, min(V, 40), dtype, seed=V, T=T)
+    z, i, v, l = s.cuda(), ids.cuda(), t.cuda(), lse.cuda() if tail else None
+    w = torch.rand(N, generator=torch.Generator().manual_seed(2)).cuda() - 0.5
+    f = gpu_lib.distill_step(z, i, v, w, teacher_lse=l, temperature=T)
+    o = gpu_lib.distill_loss(z, i, v, teacher_lse=l, temperature=T)
+    g = gpu_lib.distill_grad(z, i, v, o["record"], w, temperature=T)
+    torch.cuda.synchronize()
+    assert torch.equal(f["loss"], o["loss"]) and torch.equal(f["grad"], g)
