@@ -78,7 +78,7 @@ __device__ __forceinline__ uint32_t token_bits(const ChunkTokens &c, int group) 
 
 // Sums of one chunk of a row over the tokens outside the teacher's entries.  HBM-bound:
 // 1,152 rows of 128,256 bf16 logits in 50 us (5.9 TB/s); behind the gradient's writes
-// of an earlier call 4,096 rows take 205 us (5.1 TB/s).  With a difference and a
+// of an earlier call 4,096 rows take 200 us (5.3 TB/s).  With a difference and a
 // product for each exponent, and pairs added in fp64, 55 and 219.
 template <int DT, int ROW>
 __global__ __launch_bounds__(kThreads) void distill_scan_kernel(const DistillArgs a, int32_t nc) {
@@ -312,7 +312,7 @@ __device__ __forceinline__ float entry_gradient(float z, float p, const dsde_dis
 
 // The gradient of one chunk of a row.  It may overwrite the logits: every
 // logit is read by the thread that writes its gradient.  HBM-bound: 4,096 rows of
-// 128,256 bf16 logits in 357 us (5.9 TB/s read and written; torch's copy of 4 GiB
+// 128,256 bf16 logits in 352 us (6.0 TB/s read and written; torch's copy of 4 GiB
 // runs at 4.6).  A form that held a row in the registers of 1,024 threads, to read it
 // once for the sums and the gradient, took 628 us for both against 570: its CU's exponentials
 // (two for every logit) and barriers did not hide behind its one row's traffic.

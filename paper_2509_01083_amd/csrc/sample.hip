@@ -61,8 +61,10 @@ __device__ __forceinline__ Setting row_setting(const SelectArgs &a, int64_t r) {
 
 // Per logit a subtraction, a product, an exponential and an addition, against the
 // chunk's own maximum, so that no chunk waits for another; HBM-bound.  1,024 rows of
-// 128,256 bf16 logits take 42 us (6.25 TB/s; a plain read of that size runs at 6.9).
-// With keys (an eighth of the bytes, written) 1,408 rows take 67 us.
+// 128,256 bf16 logits take 42.6 us (6.2 TB/s; a plain read of that size runs at 6.9).
+// With keys (an eighth of the bytes, written) 1,408 rows take 68 us.  The weights are added
+// in fp32, over the eight of a group and then across the wavefront: a segment is good to 6e-7 of itself at
+// worst.  The largest logits, weights of 1, stay out of its sum (SegWeight).
 template <int DT, int ROW>
 __global__ __launch_bounds__(kThreads) void row_scan_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
   __shared__ float red[kWaves];
@@ -144,9 +146,9 @@ __device__ __forceinline__ uint32_t min_p_key(const Setting &s, float m) {
 
 // One row per workgroup of 512 threads: 40 keys of a 163,840-token row per thread,
 // and one thread for each candidate.  Bound by a chain of some ten dependent steps
-// (round trips to the last-level cache for the row's sums, keys and groups; barriers): 10.8 us for a row with a nucleus.
+// (round trips to the last-level cache for the row's sums, keys and groups; barriers): 11.1 us for a row with a nucleus.
 // With many rows it is the instructions of its eight wavefronts: the 64 largest of
-// 1,408 rows take 27.6 us.  (With 1,024 threads and a histogram of all keys: 53 us
+// 1,408 rows take 28.7 us.  (With 1,024 threads and a histogram of all keys: 53 us
 // and 103 us.)
 template <int DT, int ROW, bool TOP>
 __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
@@ -325,9 +327,12 @@ __global__ __launch_bounds__(kSelThreads, 4) void select_kernel(const SelectArgs
 // that may lie above them, then the draw over segments.  A kernel of its own, since
 // its lists take the LDS of a CU: with them in the select kernel, 256 mixed rows
 // took 105 us in two kernels, 74 in three; a call none of whose rows needs it pays 2 to 4 us.
-// A row whose cut lies within the 10,000 largest logits takes about 26 us on its
-// CU, of which 13 are the listing; beyond that its passes over all logits are
-// bound by their instructions (by the code's count, some 280 per group of 8): 90 us for V = 128,256.
+// A row whose cut lies within the 10,000 largest logits takes about 28 us on its CU for V =
+// 50,257 and 42 for V = 128,256, about half of it the listing; beyond that its passes over all logits are
+// bound by their instructions (by the code's count, some 280 per group of 8): 92 us for V = 128,256.
+// Rows with fewer unmasked tokens than top_k end in key_cut, a pass over all logits for every 2,048
+// values of the keys' upper halves from the maximum down: 256 rows of V = 128,256 masked to 300
+// tokens, with top_k = 500, take 410 us (-inf) and 720 (the type's lowest value) against 55 unmasked.
 template <int DT, int ROW>
 __global__ __launch_bounds__(kWideThreads) void wide_kernel(const SelectArgs a, int64_t row0, int32_t nc) {
   __shared__ WideLds L;
