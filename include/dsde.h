@@ -67,6 +67,7 @@ extern "C" {
 /* logit element types */
 #define DSDE_FP32 0
 #define DSDE_BF16 1
+#define DSDE_E4M3 2 /* elements of a key-value cache only: 8-bit floats (1-4-3, no infinities), with scales */
 
 /* per-sequence device error bits */
 #define DSDE_ERR_LAYOUT 1u   /* SL_b outside [0, k_max], or cu_sl not the prefix sums of sl with cu_sl[B] = N */
@@ -79,6 +80,7 @@ extern "C" {
 #define DSDE_ERR_STATE 64u   /* ring head outside [0, W) or count outside [0, W] */
 
 #define DSDE_ERR_FILTER 128u /* top_p outside (0, 1] or min_p outside [0, 1] */
+#define DSDE_ERR_PAGES 256u /* no free page, a table too narrow, or a page or slot outside the cache */
 
 /* Largest supported speculation length bound (one wavefront lane per drafted position). */
 #define DSDE_MAX_K 63
@@ -87,6 +89,11 @@ extern "C" {
 #define DSDE_MAX_VOCAB 4194304
 /* Most entries per row of dsde_top_logits and of a teacher in dsde_distill_*. */
 #define DSDE_MAX_TOP 256
+/* Most rows of one sequence in dsde_kv_attention: SL + 1 at the largest SL. */
+#define DSDE_MAX_ROWS 64
+/* Largest head size, and number of query heads, of the cache's calls. */
+#define DSDE_MAX_DIM 256
+#define DSDE_MAX_HEADS 1024
 
 /* The ABI version this library implements (DSDE_ABI_VERSION). */
 int32_t dsde_abi_version(void);
@@ -556,6 +563,122 @@ int32_t dsde_distill_grad(const void *logits, int64_t row_stride, int32_t dtype,
 int32_t dsde_distill_step(const void *logits, int64_t row_stride, int32_t dtype, int64_t V, int64_t N, int32_t K,
                           const int32_t *ids, const float *teacher, const float *teacher_lse, float temperature,
                           const float *weight, float *loss, void *grad, int64_t grad_stride, uint32_t *row_err,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The paged key-value cache of a ragged step: the look-ahead of Sec. 3.2 (slots for
+ * SL_b + 1 rows per sequence, pages mapped and given back as the SLs change), and
+ * the rows' attention over the cache.  A step of a serving loop:
+ *
+ *   1. dsde_kv_map        from the accepted counts of the last step and the SLs of the coming one:
+ *                         how many tokens stay, pages for the new rows, each row's slot
+ *   2. dsde_kv_write      per layer: the rows' keys and values into their slots
+ *   3. dsde_kv_attention  per layer: the rows' queries over each sequence's cache
+ *   4. dsde_step          on the logits
+ *
+ * Common to them:
+ *   - a cache is pages of page_size tokens (a power of two, 16 to 1024); slot
+ *     p * page_size + i is token i of page p (pages * page_size < 2^31); a sequence's token t is
+ *     in page table[b, t / page_size];
+ *   - rows are packed by sequence: sequence b has rows cu_rows[b] .. cu_rows[b+1] - 1, its newest
+ *     tokens in order (with n_b = SL_b + 1 the target rows of dsde_verify: cu_rows[b] = cu_sl[b] + b);
+ *   - dim is a multiple of 16 up to DSDE_MAX_DIM; strides are in elements, a head's dim elements lie
+ *     together, and rows of dim elements start at multiples of 16 bytes.
+ */
+
+/* Workspace bytes of dsde_kv_map; 0 when B is invalid. */
+size_t dsde_kv_map_workspace_bytes(int32_t B);
+
+/*
+ * Pages and slots of the coming rows.  For every sequence
+ *   base_b = kv_len[b] + accepted[b] + 1    tokens that stay (accepted NULL: kv_len[b])
+ *   n_b = sl[b] + extra                     rows to come
+ *   need_b = ceil((base_b + n_b) / page_size)
+ * Pages behind need_b go back onto the stack of free pages, the last sequence's last one first; then the
+ * sequences in order take what they lack from its top.  (A call that gives back what the one before
+ * it took leaves the stack as it was.)
+ *
+ *   B, pages, width             sequences (1 to 2^20), pages in the cache, entries of a table row
+ *                               (width * page_size < 2^31)
+ *   rows                        rows the slot arrays have room for (0 <= rows < 2^31)
+ *   sl [B]             int32    rows to come, less extra
+ *   kv_len [B]         int32    tokens in the cache before the last step
+ *   accepted [B]       int32    optional: dsde_verify's counts; -1: nothing to add
+ *   table [B, width]   int32    in/out: entries behind held[b] are not read; those given back become -1
+ *   held [B]           int32    in/out: pages of each sequence
+ *   free_pages [pages] int32    in/out: the stack, n_free[0] entries; those above are left as they are
+ *   n_free [1]         int32    in/out
+ * Outputs:
+ *   base [B], context [B]  int32   base_b, and base_b + n_b (base may be kv_len itself)
+ *   cu_rows [B+1]      int32    exclusive prefix sums of n_b
+ *   slots, positions [rows]  int32   of each row; -1 behind the last one
+ *   seq_err [B]        uint32   DSDE_ERR_LAYOUT: a negative n_b, kv_len or base, accepted under -1, or rows that do
+ *                               not fit `rows`; DSDE_ERR_STATE: held outside [0, width], or (for sequences whose
+ *                               pages change) n_free outside [0, pages] or more pages given back than the stack
+ *                               takes; DSDE_ERR_PAGES: need_b over width, not enough free pages left (then for all later
+ *                               sequences that need any too), or a page id outside [0, pages) at one of its rows.
+ *                               A flagged sequence keeps its pages (except after such a page id, whose rows alone have slot -1),
+ *                               has context 0, and slots -1 for its rows, which still count (0 if n_b is negative).
+ */
+int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, int64_t rows, const int32_t *sl,
+                    int32_t extra, const int32_t *kv_len, const int32_t *accepted, int32_t *table, int32_t *held,
+                    int32_t *free_pages, int32_t *n_free, int32_t *base, int32_t *context, int32_t *cu_rows,
+                    int32_t *slots, int32_t *positions, uint32_t *seq_err, void *workspace, size_t workspace_bytes,
+                    void *stream);
+
+/* A cache (passed by pointer, read during the call only).  Element (p, h, i, d) of the keys is
+ * k[p * page_stride + h * head_stride + i * token_stride + d], so a page may hold heads of tokens or tokens of
+ * heads; the values have the same strides. */
+typedef struct {
+  void *k, *v;
+  int32_t dtype;              /* DSDE_FP32, DSDE_BF16 or DSDE_E4M3 */
+  int32_t pages, page_size, heads, dim;
+  int64_t page_stride, head_stride, token_stride;
+  const float *k_scale, *v_scale; /* [heads], device, DSDE_E4M3 only: an element stands for itself times its head's scale */
+} dsde_kv_cache;
+
+/*
+ * Keys and values into their slots.
+ *   k, v [T, heads, dim]  dtype   row t, head h at t * token_stride + h * head_stride (of each)
+ *   dtype                         the cache's type, or DSDE_BF16 for a DSDE_E4M3 cache, which then takes
+ *                                 x / scale (in fp32) rounded to the nearest, ties to even, at most +-448; NaN stays NaN
+ *   slots [T]             int32   -1: the row is left out; no slot twice
+ *   row_err [T]           uint32  DSDE_ERR_PAGES: a slot outside [-1, pages * page_size); nothing is written then
+ */
+int32_t dsde_kv_write(const dsde_kv_cache *cache, const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                      const void *v, int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, int64_t T,
+                      const int32_t *slots, uint32_t *row_err, void *stream);
+
+/* Workspace bytes of dsde_kv_attention for B sequences of at most max_rows rows, group query heads for each
+ * of `heads` key heads; it grows with every argument; 0 when the sizes are invalid. */
+size_t dsde_kv_attention_workspace_bytes(int32_t B, int32_t heads, int32_t group, int32_t max_rows, int32_t dim);
+
+/*
+ * Attention of each sequence's newest rows over its cache.  Row j of sequence b (n_b rows) is token
+ * p = context[b] - n_b + j and sees the tokens t <= p of the sequence, with a window > 0 those with t > p - window:
+ *   s_t = scale * q . k_t,  lse = log sum_t exp s_t,  out = sum_t exp(s_t - lse) v_t
+ * A row that sees nothing has out 0 and lse -inf.  Nothing that a row does not see has an effect on it, whatever it holds.
+ *
+ *   q [T, q_heads, dim]   dtype   the cache's type, or DSDE_BF16 for DSDE_E4M3; q_heads a multiple of cache->heads:
+ *                                 query head h reads key head h / (q_heads / heads)
+ *   B, max_rows                   sequences (1 to 2^20), most rows of one (1 to DSDE_MAX_ROWS)
+ *   table [B, width]      int32   as dsde_kv_map leaves it; entries behind a sequence's tokens are not read
+ *   context [B]           int32   tokens of each sequence, its new rows among them (fewer than n_b: the first rows see nothing)
+ *   cu_rows [B+1]         int32   rows of each sequence, cu_rows[B] <= T; rows of no sequence are left as they are
+ *   scale                         finite
+ *   window                        >= 0
+ * Outputs:
+ *   out [T, q_heads, dim] dtype   each value rounded once, from fp32
+ *   lse [T, q_heads]      float   optional (may be NULL)
+ *   seq_err [B]           uint32  DSDE_ERR_LAYOUT: rows outside [0, T], a negative number of them or more than max_rows (none of
+ *                                 them is written), or a context outside [0, width * page_size] (rows NaN);
+ *                                 DSDE_ERR_PAGES: an id outside [0, pages) among the pages that its rows see (the rows
+ *                                 that see it are NaN)
+ */
+int32_t dsde_kv_attention(const dsde_kv_cache *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                          int32_t dtype, int32_t q_heads, int64_t T, int32_t B, int32_t max_rows, const int32_t *table,
+                          int32_t width, const int32_t *context, const int32_t *cu_rows, float scale, int32_t window,
+                          void *out, int64_t out_token_stride, int64_t out_head_stride, float *lse, uint32_t *seq_err,
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /*

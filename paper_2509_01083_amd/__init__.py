@@ -17,11 +17,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdsde.so")
 
 OK, INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE_ERROR = 0, 1, 2, 3
-FP32, BF16 = 0, 1
+FP32, BF16, E4M3 = 0, 1, 2
 ERR_LAYOUT, ERR_TOKEN, ERR_LOGIT, ERR_TEMP, ERR_UNIFORM, ERR_SIGNAL, ERR_STATE = 1, 2, 4, 8, 16, 32, 64
-ERR_FILTER = 128
+ERR_FILTER, ERR_PAGES = 128, 256
 MAX_K = 63
 MAX_TOP = 256
+MAX_ROWS = 64  # rows of one sequence in kv_attention
 DISTILL_ROW_BYTES = 32
 STATIC_SCRATCH_BYTES = 16 << 20  # DSDE_STATIC_SCRATCH_BYTES: the scratch array of dsde_step_static
 EXPORTS = ("dsde_abi_version", "dsde_status_string", "dsde_verify_workspace_bytes", "dsde_verify",
@@ -29,7 +30,8 @@ EXPORTS = ("dsde_abi_version", "dsde_status_string", "dsde_verify_workspace_byte
            "dsde_set_profile_events", "dsde_stream_read", "dsde_shard_workspace_bytes", "dsde_shard_stats",
            "dsde_shard_accept", "dsde_shard_accept_step", "dsde_shard_draw_mass", "dsde_shard_draw_pick",
            "dsde_sample_workspace_bytes", "dsde_sample", "dsde_top_logits", "dsde_distill_workspace_bytes",
-           "dsde_distill_loss", "dsde_distill_grad", "dsde_distill_step")
+           "dsde_distill_loss", "dsde_distill_grad", "dsde_distill_step", "dsde_kv_map_workspace_bytes", "dsde_kv_map",
+           "dsde_kv_write", "dsde_kv_attention_workspace_bytes", "dsde_kv_attention")
 # sizes of the records the vocabulary-shard calls exchange (dsde_shard_partial,
 # dsde_draw_job, dsde_shard_mass); kept as raw bytes on the Python side
 SHARD_PARTIAL_BYTES, DRAW_JOB_BYTES, SHARD_MASS_BYTES = 64, 44, 32
@@ -109,6 +111,17 @@ def load(path: str = LIB_PATH):
     lib.dsde_distill_grad.argtypes = [P, i64, i32, i64, i64, i32, P, P, f32, P, P, P, i64, P]
     lib.dsde_distill_step.restype = i32
     lib.dsde_distill_step.argtypes = [P, i64, i32, i64, i64, i32, P, P, P, f32, P, P, P, i64, P, P, sz, P]
+    lib.dsde_kv_map_workspace_bytes.restype = sz
+    lib.dsde_kv_map_workspace_bytes.argtypes = [i32]
+    lib.dsde_kv_map.restype = i32
+    lib.dsde_kv_map.argtypes = [i32, i32, i32, i32, i64, P, i32, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
+    lib.dsde_kv_write.restype = i32
+    lib.dsde_kv_write.argtypes = [P, P, i64, i64, P, i64, i64, i32, i64, P, P, P]
+    lib.dsde_kv_attention_workspace_bytes.restype = sz
+    lib.dsde_kv_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.dsde_kv_attention.restype = i32
+    lib.dsde_kv_attention.argtypes = [P, P, i64, i64, i32, i32, i64, i32, i32, P, i32, P, P, f32, i32, P, i64, i64, P, P,
+                                      P, sz, P]
     _lib = lib
     return lib
 
@@ -505,6 +518,119 @@ def distill(logits, ids, teacher, teacher_lse=None, temperature=1.0):
     """``distill_loss`` [N] for autograd: differentiable with respect to the logits
     (the teacher is taken as constant)."""
     return _Distill.apply(logits, ids, teacher, teacher_lse, temperature)
+
+
+# ---------------------------------------------------------------------------
+# the paged key-value cache of a step: pages and slots, writing, attention
+# ---------------------------------------------------------------------------
+
+def _gpu_tensor(t, name):
+    """A tensor that a call takes sizes from, or the same refusal as the marshalling's."""
+    if not isinstance(t, torch.Tensor):
+        raise DsdeError(f"{name} must be a GPU tensor")
+    return t
+
+
+def new_kv_cache(pages, page_size, heads, dim, dtype=torch.bfloat16, device="cuda"):
+    """Keys and values [pages, heads, page_size, dim] of ``pages`` pages of ``page_size``
+    tokens (a power of two, 16 to 1024), in bfloat16, float32 or float8_e4m3fn.  What a slot
+    holds before its first write is not read."""
+    k = torch.empty((2, pages, heads, page_size, dim), dtype=dtype, device=device)
+    return k[0], k[1]
+
+
+def new_kv_pool(B, width, pages, device="cuda"):
+    """Page tables of ``B`` sequences of at most ``width`` pages, none held yet, and the stack
+    of all ``pages`` free pages: a dict with table [B, width], held [B], free [pages], n_free [1]."""
+    i32 = dict(dtype=torch.int32, device=device)
+    return {"table": torch.full((B, width), -1, **i32), "held": torch.zeros(B, **i32),
+            "free": torch.arange(pages - 1, -1, -1, **i32), "n_free": torch.full((1,), pages, **i32)}
+
+
+def new_kv_map_workspace(B, device="cuda"):
+    """The workspace of ``kv_map`` for B sequences or fewer."""
+    n = int(load().dsde_kv_map_workspace_bytes(B))
+    if n == 0:
+        raise DsdeError("invalid sizes for the map's workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def new_kv_map_out(B, rows, device="cuda"):
+    """The outputs of ``kv_map`` for B sequences with room for ``rows`` rows."""
+    i32 = dict(dtype=torch.int32, device=device)
+    out = {"base": torch.empty(B, **i32), "context": torch.empty(B, **i32), "cu_rows": torch.empty(B + 1, **i32),
+           "seq_err": torch.empty(B, **i32)}
+    if rows > 0:
+        out["slots"], out["positions"] = torch.empty(rows, **i32), torch.empty(rows, **i32)
+    return out
+
+
+def kv_map(sl, kv_len, pool, page_size, rows, extra=1, accepted=None, out=None, workspace=None, stream=None):
+    """``dsde_kv_map``: pages for the coming ``sl + extra`` rows of every sequence (those
+    no longer needed go back first) and the slot of each row.  ``kv_len`` [B] int32 are the tokens in
+    the cache before the last step, ``accepted`` [B] int32 that step's counts (``verify``'s; -1 or
+    None: nothing to add), ``pool`` the state of ``new_kv_pool``, updated in place, ``rows`` the room
+    for rows.  Returns a dict with base, context [B], cu_rows [B + 1], slots, positions [rows]
+    (-1 behind the last row; not with rows = 0) and seq_err."""
+    native = _native or _bind()
+    if out is None or workspace is None:
+        B, dev = _rows(_gpu_tensor(sl, "sl")), sl.device
+        with _on(stream):
+            if out is None:
+                out = new_kv_map_out(B, int(rows), dev)
+            if workspace is None:
+                workspace = new_kv_map_workspace(B, dev)
+    native.kv_map(sl, int(extra), kv_len, accepted, pool, int(page_size), int(rows), out, workspace, _handle(stream))
+    return out
+
+
+def kv_write(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, row_err=None, stream=None):
+    """``dsde_kv_write``: rows ``k``, ``v`` [T, heads, dim] (any strides of whole 16 bytes) into
+    the ``slots`` [T] int32 of a cache (-1: left out).  A float8_e4m3fn cache takes bfloat16 rows
+    divided by ``k_scale``, ``v_scale`` [heads] float32.  Returns row_err [T]."""
+    native = _native or _bind()
+    if row_err is None:
+        _gpu_tensor(k, "k")
+        with _on(stream):
+            row_err = torch.empty(_rows(k), dtype=torch.int32, device=k.device)
+    native.kv_write(k, v, slots, k_cache, v_cache, k_scale, v_scale, row_err, _handle(stream))
+    return row_err
+
+
+def new_kv_attention_workspace(B, heads, group, max_rows, dim, device="cuda"):
+    """The workspace of ``kv_attention`` for B sequences of at most ``max_rows`` rows and
+    ``group`` query heads for each of ``heads`` key heads; one made for the largest sizes serves all smaller ones."""
+    n = int(load().dsde_kv_attention_workspace_bytes(B, heads, group, max_rows, dim))
+    if n == 0:
+        raise DsdeError("invalid sizes for the attention workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def kv_attention(q, k_cache, v_cache, table, context, cu_rows, max_rows, scale=None, window=0, k_scale=None,
+                 v_scale=None, lse=False, out=None, workspace=None, stream=None):
+    """``dsde_kv_attention``: the rows ``q`` [T, q_heads, dim] of all sequences (``cu_rows``
+    [B + 1] int32, at most ``max_rows`` each, the newest of ``context`` [B] int32 tokens) over the cache
+    through ``table`` [B, width] int32.  ``scale`` defaults to dim ** -0.5; ``window`` > 0: a row sees
+    that many tokens, itself the last.  Returns a dict with out [T, q_heads, dim], seq_err (and lse
+    [T, q_heads] float32 when asked for); pass ``out`` to reuse its buffers (lse is computed where it has one)."""
+    native = _native or _bind()
+    if out is None or workspace is None or (lse and "lse" not in out):
+        if _gpu_tensor(q, "q").dim() != 3 or _gpu_tensor(k_cache, "k_cache").dim() != 4:
+            raise DsdeError("q must be [rows, heads, dim] and k_cache [pages, heads, page_size, dim]")
+        (T, heads, dim), B, dev = q.shape, _rows(_gpu_tensor(table, "table")), q.device
+        with _on(stream):
+            if out is None:
+                out = {"out": torch.empty((T, heads, dim), dtype=q.dtype, device=dev),
+                       "seq_err": torch.empty(B, dtype=torch.int32, device=dev)}
+            if lse and "lse" not in out:
+                out["lse"] = torch.empty((T, heads), dtype=torch.float32, device=dev)
+            if workspace is None:
+                kv_heads = int(k_cache.shape[1])
+                workspace = new_kv_attention_workspace(B, kv_heads, heads // max(kv_heads, 1), max_rows, dim, dev)
+    native.kv_attention(q, k_cache, v_cache, k_scale, v_scale, table, context, cu_rows, max_rows,
+                        q.shape[-1] ** -0.5 if scale is None else float(scale), int(window), out, workspace,
+                        _handle(stream))
+    return out
 
 
 # ---------------------------------------------------------------------------

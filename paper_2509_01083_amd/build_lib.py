@@ -31,7 +31,7 @@ LIB = os.path.join(HERE, "libdsde.so")
 BINDING = os.path.join(HERE, "_binding.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["api.hip", "stats.hip", "verify.hip", "shard.hip", "signal.hip", "probe.hip", "rows_api.hip", "sample.hip",
-           "distill.hip"]
+           "distill.hip", "kv_api.hip", "kv_cache.hip", "kv_attention.hip"]
 
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.environ.get("HIPCC", os.path.join(ROCM, "bin", "hipcc"))

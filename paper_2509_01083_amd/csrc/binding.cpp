@@ -6,11 +6,13 @@
 // ctypes' conversion of 45 arguments) took 21 us of host time, as long as the
 // step's kernels take in small batches.
 #include <Python.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
+#include <vector>
 
 #include "dsde.h"
 
@@ -24,6 +26,7 @@ PyObject *g_error = nullptr;  // paper_2509_01083_amd.DsdeError
   X(dsde_status_string)                                                                                         \
   X(dsde_verify) X(dsde_step) X(dsde_step_static) X(dsde_kld_signal) X(dsde_next_sl) X(dsde_calibration_update) \
   X(dsde_sample) X(dsde_top_logits) X(dsde_distill_loss) X(dsde_distill_grad) X(dsde_distill_step)              \
+  X(dsde_kv_map) X(dsde_kv_write) X(dsde_kv_attention)                                                          \
   X(dsde_shard_stats) X(dsde_shard_accept) X(dsde_shard_accept_step) X(dsde_shard_draw_mass) X(dsde_shard_draw_pick)
 struct Library {
 #define X(name) decltype(&::name) name;
@@ -709,6 +712,218 @@ PyObject *py_distill_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
   });
 }
 
+// The cache's calls: their tensors lie on one device, which is made the current one for the call (its
+// current stream too, where no stream is given).
+struct OneDevice {
+  c10::OptionalDeviceGuard guard;
+  int device = -1;
+  std::vector<PyObject *> items;  // taken from mappings, held for the call
+
+  ~OneDevice() {
+    for (PyObject *o : items) Py_DECREF(o);
+  }
+  PyObject *item(PyObject *dict, const char *key) {
+    PyObject *o = PyMapping_GetItemString(dict, key);
+    if (!o) throw Failed{};
+    items.push_back(o);
+    return o;
+  }
+
+  void see(PyObject *o, const char *name) {
+    if (o == Py_None || !THPVariable_Check(o)) return;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) return;  // refused where its pointer is taken
+    if (device < 0)
+      guard.reset_device(t.device()), device = t.get_device();
+    else if (t.get_device() != device)
+      fail(std::string(name) + " must be on the device of the other tensors");
+  }
+};
+// An array of a call: on the call's device, contiguous; `write`: raises its version.
+template <typename T>
+T *take_on(Args &a, OneDevice &dev, int type, int64_t n, const char *name, bool write = false) {
+  PyObject *o = a.next();
+  dev.see(o, name);
+  T *p = static_cast<T *>(ptr(o, type, n, name));
+  if (write) written(o);
+  return p;
+}
+template <typename T>
+T *out_on(PyObject *dict, OneDevice &dev, const char *key, int type, int64_t n) {
+  PyObject *o = dev.item(dict, key);
+  dev.see(o, key);
+  T *p = static_cast<T *>(ptr(o, type, n, key));
+  written(o);
+  return p;
+}
+
+// Rows [T, heads, dim] with dense heads.
+struct HeadRows {
+  void *data;
+  int64_t T, heads, dim, token_stride, head_stride;
+  at::ScalarType type;
+};
+HeadRows head_rows(PyObject *o, OneDevice &dev, const char *name) {
+  size_of(o, 2, name);
+  const at::Tensor &t = THPVariable_Unpack(o);
+  if (t.dim() != 3) fail(std::string(name) + " must be [rows, heads, dim]");
+  if (t.scalar_type() != at::ScalarType::BFloat16 && t.scalar_type() != at::ScalarType::Float)
+    fail(std::string(name) + " must be bfloat16 or float32");
+  if (!t.is_cuda()) fail(std::string(name) + " must be a GPU tensor");
+  dev.see(o, name);
+  HeadRows r{t.data_ptr(), t.size(0), t.size(1), t.size(2), t.size(0) > 1 ? t.stride(0) : 0,
+             t.size(1) > 1 ? t.stride(1) : 0, t.scalar_type()};
+  if (t.numel() > 0 && r.dim > 1 && t.stride(2) != 1) fail(std::string(name) + " must have dense heads");
+  const int64_t e = t.element_size();
+  if (t.numel() > 0 && (reinterpret_cast<uintptr_t>(r.data) % 16 != 0 || r.token_stride * e % 16 != 0 || r.head_stride * e % 16 != 0))
+    fail(std::string(name) + " must have heads that start at multiples of 16 bytes");
+  return r;
+}
+int32_t row_type(const HeadRows &r) { return r.type == at::ScalarType::BFloat16 ? DSDE_BF16 : DSDE_FP32; }
+
+// A cache of two tensors [pages, heads, page_size, dim] of one layout, and its scales.
+dsde_kv_cache take_cache(Args &a, OneDevice &dev, bool write) {
+  PyObject *o[2] = {a.next(), a.next()};
+  const char *names[2] = {"k_cache", "v_cache"};
+  dsde_kv_cache c{};
+  for (int i = 0; i < 2; ++i) {
+    size_of(o[i], 3, names[i]);
+    const at::Tensor &t = THPVariable_Unpack(o[i]);
+    if (t.dim() != 4) fail(std::string(names[i]) + " must be [pages, heads, page_size, dim]");
+    const at::ScalarType is = t.scalar_type();
+    if (is != at::ScalarType::BFloat16 && is != at::ScalarType::Float && is != at::ScalarType::Float8_e4m3fn)
+      fail(std::string(names[i]) + " must be bfloat16, float32 or float8_e4m3fn");
+    if (!t.is_cuda()) fail(std::string(names[i]) + " must be a GPU tensor");
+    dev.see(o[i], names[i]);
+    int64_t size[4], stride[4];
+    for (int d = 0; d < 4; ++d) {
+      size[d] = t.size(d);
+      stride[d] = size[d] > 1 ? t.stride(d) : 0;
+    }
+    if (size[0] < 1 || size[0] > 0x7fffffff || size[1] < 1 || size[1] > DSDE_MAX_HEADS) fail(std::string(names[i]) + " has too few or too many pages or heads");
+    if (size[2] < 16 || size[2] > 1024 || (size[2] & (size[2] - 1)) != 0) fail("page_size must be a power of two in 16..1024");
+    if (size[3] < 16 || size[3] > DSDE_MAX_DIM || size[3] % 16 != 0) fail("dim must be a multiple of 16 in 16..256");
+    if (stride[3] != 1) fail(std::string(names[i]) + " must have dense heads");
+    const int32_t type = is == at::ScalarType::BFloat16 ? DSDE_BF16 : is == at::ScalarType::Float ? DSDE_FP32 : DSDE_E4M3;
+    const int64_t e = t.element_size();
+    if (reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 != 0 || stride[0] * e % 16 != 0 || stride[1] * e % 16 != 0 || stride[2] * e % 16 != 0)
+      fail(std::string(names[i]) + " must have rows that start at multiples of 16 bytes");
+    if (i == 0) {
+      c = dsde_kv_cache{t.data_ptr(), nullptr, type, int32_t(size[0]), int32_t(size[2]), int32_t(size[1]), int32_t(size[3]),
+                        stride[0], stride[1], stride[2], nullptr, nullptr};
+    } else {
+      if (c.dtype != type || c.pages != size[0] || c.heads != size[1] || c.page_size != size[2] || c.dim != size[3] ||
+          c.page_stride != stride[0] || c.head_stride != stride[1] || c.token_stride != stride[2])
+        fail("k_cache and v_cache must have one type, shape and layout");
+      c.v = t.data_ptr();
+    }
+    if (write) written(o[i]);
+  }
+  c.k_scale = take_on<float>(a, dev, kF32, c.heads, "k_scale");
+  c.v_scale = take_on<float>(a, dev, kF32, c.heads, "v_scale");
+  if ((c.dtype == DSDE_E4M3) != (c.k_scale != nullptr) || (c.dtype == DSDE_E4M3) != (c.v_scale != nullptr))
+    fail("k_scale and v_scale belong to a cache of float8_e4m3fn, and both to each");
+  return c;
+}
+void check_rows(const dsde_kv_cache &c, const HeadRows &r, const char *name) {
+  if (r.dim != c.dim) fail(std::string(name) + " must have the cache's dim");
+  if (row_type(r) != (c.dtype == DSDE_E4M3 ? DSDE_BF16 : c.dtype))
+    fail(std::string(name) + " must be of the cache's type, or bfloat16 for a cache of float8_e4m3fn");
+}
+
+// kv_map(sl, extra, kv_len, accepted, pool, page_size, rows, out, workspace, stream)
+PyObject *py_kv_map(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    OneDevice dev;
+    if (n < 1) a.next();
+    const int64_t B = size_of(args[0], 0, "sl");
+    const auto *sl = take_on<int32_t>(a, dev, kI32, B, "sl");
+    const int32_t extra = a.int32();
+    const auto *kv_len = take_on<int32_t>(a, dev, kI32, B, "kv_len"), *accepted = take_on<int32_t>(a, dev, kI32, B, "accepted");
+    PyObject *pool = a.next();
+    const int64_t page = a.integer(), rows = a.integer();
+    PyObject *table_o = dev.item(pool, "table"), *free_o = dev.item(pool, "free");
+    const int64_t width = size_of(table_o, 1, "table"), pages = size_of(free_o, 0, "free");
+    if (THPVariable_Unpack(table_o).dim() != 2 || size_of(table_o, 0, "table") != B) fail("table must be [B, width]");
+    if (width > 0x7fffffff || pages > 0x7fffffff || page < 1 || page > 1024 || rows < 0 || B > 0x7fffffff)
+      fail("kv_map: a size is out of range");
+    auto *table = out_on<int32_t>(pool, dev, "table", kI32, B * width), *held = out_on<int32_t>(pool, dev, "held", kI32, B);
+    auto *stack = out_on<int32_t>(pool, dev, "free", kI32, pages), *n_free = out_on<int32_t>(pool, dev, "n_free", kI32, 1);
+    PyObject *dict = a.next();
+    auto *base = out_on<int32_t>(dict, dev, "base", kI32, B), *context = out_on<int32_t>(dict, dev, "context", kI32, B);
+    auto *cu = out_on<int32_t>(dict, dev, "cu_rows", kI32, B + 1);
+    auto *slots = rows > 0 ? out_on<int32_t>(dict, dev, "slots", kI32, rows) : nullptr;
+    auto *positions = rows > 0 ? out_on<int32_t>(dict, dev, "positions", kI32, rows) : nullptr;
+    auto *err = out_on<uint32_t>(dict, dev, "seq_err", kErr, B);
+    if (a.at != a.end) dev.see(*a.at, "workspace");
+    size_t bytes;
+    void *ws = take_workspace(a, &bytes), *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_kv_map(int32_t(B), int32_t(page), int32_t(pages), int32_t(width), rows, sl, extra, kv_len, accepted,
+                               table, held, stack, n_free, base, context, cu, slots, positions, err, ws, bytes, stream);
+    });
+  });
+}
+
+// kv_write(k, v, slots, k_cache, v_cache, k_scale, v_scale, row_err, stream)
+PyObject *py_kv_write(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    OneDevice dev;
+    const HeadRows k = head_rows(a.next(), dev, "k"), v = head_rows(a.next(), dev, "v");
+    const auto *slots = take_on<int32_t>(a, dev, kI32, k.T, "slots");
+    const dsde_kv_cache c = take_cache(a, dev, true);
+    check_rows(c, k, "k");
+    check_rows(c, v, "v");
+    if (k.T != v.T || k.heads != c.heads || v.heads != c.heads) fail("k and v must be [rows, heads, dim] of the cache's heads");
+    auto *err = take_on<uint32_t>(a, dev, kErr, k.T, "row_err", true);
+    void *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_kv_write(&c, k.data, k.token_stride, k.head_stride, v.data, v.token_stride, v.head_stride, row_type(k),
+                                 k.T, slots, err, stream);
+    });
+  });
+}
+
+// kv_attention(q, k_cache, v_cache, k_scale, v_scale, table, context, cu_rows, max_rows, scale, window, out, workspace,
+//              stream); lse where out has it
+PyObject *py_kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  return guarded(args, n, [&](Args &a) {
+    OneDevice dev;
+    const HeadRows q = head_rows(a.next(), dev, "q");
+    const dsde_kv_cache c = take_cache(a, dev, false);
+    check_rows(c, q, "q");
+    if (q.heads < 1 || q.heads % c.heads != 0) fail("q must have a multiple of the cache's heads");
+    PyObject *table_o = a.next();
+    dev.see(table_o, "table");
+    const int64_t B = size_of(table_o, 0, "table"), width = size_of(table_o, 1, "table");
+    if (THPVariable_Unpack(table_o).dim() != 2 || B > 0x7fffffff || width > 0x7fffffff) fail("table must be [B, width]");
+    const auto *table = static_cast<const int32_t *>(ptr(table_o, kI32, B * width, "table"));
+    const auto *context = take_on<int32_t>(a, dev, kI32, B, "context"), *cu = take_on<int32_t>(a, dev, kI32, B + 1, "cu_rows");
+    const int32_t max_rows = a.int32();
+    const float scale = a.real();
+    const int64_t window = a.integer();
+    if (window < 0 || window > 0x7fffffff) fail("window must be in 0..2^31-1");
+    PyObject *dict = a.next();
+    PyObject *out_o = dev.item(dict, "out");
+    const HeadRows o = head_rows(out_o, dev, "out");
+    if (o.T != q.T || o.heads != q.heads || o.dim != q.dim || o.type != q.type) fail("out must have the queries' shape and type");
+    written(out_o);
+    auto *lse = PyMapping_HasKeyString(dict, "lse") ? out_on<float>(dict, dev, "lse", kF32, q.T * q.heads) : nullptr;
+    auto *err = out_on<uint32_t>(dict, dev, "seq_err", kErr, B);
+    if (a.at != a.end) dev.see(*a.at, "workspace");
+    size_t bytes;
+    void *ws = take_workspace(a, &bytes), *stream = a.stream();
+    a.done();
+    call([&] {
+      return g_lib.dsde_kv_attention(&c, q.data, q.token_stride, q.head_stride, row_type(q), int32_t(q.heads), q.T, int32_t(B),
+                                     max_rows, table, int32_t(width), context, cu, scale, int32_t(window), o.data,
+                                     o.token_stride, o.head_stride, lse, err, ws, bytes, stream);
+    });
+  });
+}
+
 // set_error(type): the exception the checks raise
 PyObject *py_set_error(PyObject *, PyObject *type) {
   Py_INCREF(type);
@@ -754,6 +969,9 @@ PyMethodDef g_methods[] = {entry("verify", py_verify),
                            entry("distill_loss", py_distill_loss),
                            entry("distill_grad", py_distill_grad),
                            entry("distill_step", py_distill_step),
+                           entry("kv_map", py_kv_map),
+                           entry("kv_write", py_kv_write),
+                           entry("kv_attention", py_kv_attention),
                            {"set_error", py_set_error, METH_O, nullptr},
                            {"set_library", py_set_library, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};

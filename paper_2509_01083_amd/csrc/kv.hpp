@@ -1,0 +1,104 @@
+// Arguments, workspaces and launchers of the paged key-value cache.
+#pragma once
+
+#include "common.hpp"
+
+namespace dsde {
+
+constexpr int32_t kMaxKvSeqs = 1 << 20;
+constexpr int32_t kMinPage = 16, kMaxPage = 1024;
+
+// dsde_kv_map's workspace: the stack's height behind the pages given back, then per
+// sequence the pages it held and the prefix sums of pages taken and given back.
+struct MapLayout {
+  size_t top, from, taken, back, total;
+};
+inline MapLayout map_layout(int32_t B) {
+  MapLayout l;
+  l.top = 0;
+  l.from = align_up(sizeof(int32_t));
+  l.taken = l.from + align_up(sizeof(int32_t) * size_t(B));
+  l.back = l.taken + align_up(sizeof(int32_t) * (size_t(B) + 1));
+  l.total = l.back + align_up(sizeof(int32_t) * (size_t(B) + 1));
+  return l;
+}
+struct MapArgs {
+  int32_t B, shift, pages, width;
+  int64_t rows;
+  const int32_t *sl;
+  int32_t extra;
+  const int32_t *kv_len, *accepted;  // accepted may be null
+  int32_t *table, *held, *stack, *n_free, *base, *context, *cu_rows, *slots, *positions;
+  uint32_t *seq_err;
+  int32_t *top, *from, *taken, *back;  // workspace
+};
+int launch_kv_map(const MapArgs &a, hipStream_t stream);
+
+// Rows [T, heads, dim] of one array, strides in bytes.
+struct KvRows {
+  const char *data;
+  int64_t token_stride, head_stride;
+};
+struct CacheView {
+  char *k, *v;
+  int32_t dtype, pages, shift, heads, dim;
+  int64_t page_stride, head_stride;  // bytes
+  int32_t token_stride;              // bytes
+  const float *k_scale, *v_scale;
+};
+struct KvWriteArgs {
+  CacheView cache;
+  KvRows k, v;
+  int32_t dtype;
+  int64_t T;
+  const int32_t *slots;
+  uint32_t *row_err;
+};
+int launch_kv_write(const KvWriteArgs &a, hipStream_t stream);
+
+struct AttendArgs {
+  CacheView cache;
+  KvRows q;
+  int32_t dtype, group, B, max_rows;
+  int64_t T;
+  const int32_t *table;
+  int32_t width;
+  const int32_t *context, *cu_rows;
+  float scale;
+  int32_t window;
+  char *out;
+  int64_t out_token_stride, out_head_stride;  // bytes
+  float *lse;
+  uint32_t *seq_err;
+  void *workspace;
+};
+// Row blocks (of 16 rows each) that one workgroup takes, and the bytes of its two partial results.
+inline int row_tiles(int32_t group, int32_t max_rows, int32_t dim) {
+  const int64_t m = int64_t(group) * max_rows;
+  const int most = dim > 128 ? 2 : 4;
+  return m <= 16 ? 1 : m <= 32 || most == 2 ? 2 : 4;
+}
+constexpr int kAttendGroups = 1024;  // workgroups of the largest launch
+inline int padded_dim(int32_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+// A partial result: a row's values, its reference and its sum of weights.
+inline size_t partial_floats(int tiles, int32_t dim) { return size_t(16) * tiles * (padded_dim(dim) + 2); }
+struct AttendLayout {
+  size_t units, partial, total;
+};
+__host__ __device__ constexpr size_t attend_layout_partial(int32_t B) {
+  return (sizeof(int64_t) * (size_t(B) + 1) + 255) & ~size_t(255);
+}
+inline AttendLayout attend_layout(int32_t B, int32_t group, int32_t max_rows, int32_t dim) {
+  AttendLayout l;
+  l.units = 0;  // [B+1] int64: prefix sums of the sequences' work
+  l.partial = attend_layout_partial(B);
+  // grows with dim too, where larger heads take fewer row blocks
+  const size_t wide = partial_floats(row_tiles(group, max_rows, dim), dim);
+  const int32_t d = dim < 128 ? dim : 128;
+  const size_t narrow = partial_floats(row_tiles(group, max_rows, d), d);
+  l.total = l.partial + align_up(sizeof(float) * 2 * kAttendGroups * (wide > narrow ? wide : narrow));
+  return l;
+}
+int launch_kv_attention(const AttendArgs &a, hipStream_t stream);
+
+}  // namespace dsde

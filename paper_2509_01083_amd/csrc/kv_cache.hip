@@ -1,0 +1,282 @@
+// Pages and slots of a ragged step's rows, and their keys and values into the cache.
+//
+// The map is integer arithmetic on a few numbers per sequence: three prefix sums
+// (rows, pages given back, pages taken) decide where each sequence's rows and pages lie, so any
+// number of threads can move pages at once and the result is the one of a loop over the
+// sequences.  It is bound by dependent round trips to memory, not by bytes (0.1 MB for 1,024 sequences).
+#include "kv.hpp"
+
+namespace dsde {
+namespace {
+
+constexpr int kMapThreads = 1024, kMapWaves = kMapThreads / 64;
+constexpr int kSmallSeqs = 1024;     // sequences whose prefix sums stay in LDS
+constexpr int64_t kSmallRows = 8192;  // rows that the planning workgroup maps itself
+
+struct Sums {
+  int64_t rows, taken, back;
+  __device__ Sums operator+(const Sums &o) const { return Sums{rows + o.rows, taken + o.taken, back + o.back}; }
+};
+__device__ __forceinline__ Sums shift_up(const Sums &s, int n) {
+  return Sums{__shfl_up(s.rows, n), __shfl_up(s.taken, n), __shfl_up(s.back, n)};
+}
+// Inclusive sums over the workgroup's threads, and their total.
+__device__ Sums block_scan(Sums s, Sums *total) {
+  __shared__ Sums wave[kMapWaves];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  for (int n = 1; n < 64; n <<= 1) {
+    const Sums o = shift_up(s, n);
+    if (lane >= n) s = s + o;
+  }
+  __syncthreads();  // the last call's sums have been read
+  if (lane == 63) wave[w] = s;
+  __syncthreads();
+  Sums all{0, 0, 0};
+  for (int i = 0; i < kMapWaves; ++i) {
+    if (i == w) s = s + all;
+    all = all + wave[i];
+  }
+  *total = all;
+  return s;
+}
+
+// Prefix sums as they are kept: sums that reach 2^31 are beyond any page or row there is.
+__device__ __forceinline__ int32_t kept(int64_t x) { return int32_t(x < 0x7fffffff ? x : 0x7fffffff); }
+
+// One sequence's share of the call.
+struct Want {
+  int64_t n, base;
+  int32_t from, to;  // pages held before and wanted after
+  uint32_t err;
+};
+__device__ __forceinline__ Want wanted(const MapArgs &a, int32_t b) {
+  Want x;
+  const int64_t len = a.kv_len[b], acc = a.accepted ? a.accepted[b] : -1;
+  x.n = int64_t(a.sl[b]) + a.extra;
+  x.base = len + acc + 1;
+  x.from = a.held[b];
+  x.err = 0;
+  if (x.n < 0 || len < 0 || acc < -1) x.err |= DSDE_ERR_LAYOUT;
+  if (len < 0 || acc < -1) x.base = len;  // as it was
+  if (x.n < 0) x.n = 0;
+  if (x.from < 0 || x.from > a.width) x.err |= DSDE_ERR_STATE;
+  x.to = x.from;
+  if (!x.err) {
+    const int64_t need = (x.base + x.n + (int64_t(1) << a.shift) - 1) >> a.shift;
+    if (need > a.width)
+      x.err |= DSDE_ERR_PAGES;
+    else
+      x.to = int32_t(need);
+  }
+  return x;
+}
+// Pages that a sequence takes and gives back; none where its rows do not fit.
+__device__ __forceinline__ Sums moved(const Want &x, bool fits) {
+  const bool ok = !x.err && fits;
+  return Sums{x.n, ok && x.to > x.from ? x.to - x.from : 0, ok && x.to < x.from ? x.from - x.to : 0};
+}
+
+// The sequence (smallest index) whose range of the prefix sums pre [B+1] holds i.
+__device__ __forceinline__ int32_t find(const int32_t *pre, int32_t B, int32_t i) {
+  int32_t lo = 0, hi = B;  // pre[lo] <= i < pre[hi]
+  while (hi - lo > 1) {
+    const int32_t mid = (lo + hi) >> 1;
+    if (pre[mid] <= i)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// Page c of a sequence, where its table has it or, taken in this call, on the stack.
+__device__ __forceinline__ void map_row(const MapArgs &a, const int32_t *cu, const int32_t *taken, int32_t top, int64_t t) {
+  const int32_t total = cu[a.B];
+  int32_t slot = -1, pos = -1;
+  if (t < total) {
+    const int32_t b = find(cu, a.B, int32_t(t));
+    const int32_t context = a.context[b];
+    if (context > 0) {  // a sequence with rows that is not flagged
+      pos = a.base[b] + (int32_t(t) - cu[b]);
+      const int32_t c = pos >> a.shift, grown = c - a.from[b];
+      const int32_t page = grown >= 0 ? a.stack[top - 1 - (taken[b] + grown)] : a.table[int64_t(b) * a.width + c];
+      if (page >= 0 && page < a.pages)
+        slot = (page << a.shift) | (pos & ((1 << a.shift) - 1));
+      else
+        a.seq_err[b] = DSDE_ERR_PAGES;  // every thread that comes here stores the same
+    }
+  }
+  a.slots[t] = slot;
+  a.positions[t] = pos;
+}
+__device__ __forceinline__ void take_page(const MapArgs &a, const int32_t *taken, int32_t top, int32_t i) {
+  const int32_t b = find(taken, a.B, i);
+  const int32_t c = a.from[b] + (i - taken[b]);
+  if (c < a.held[b]) a.table[int64_t(b) * a.width + c] = a.stack[top - 1 - i];  // not of a sequence that went without
+}
+
+// The plan, by one workgroup.  ALL: it also takes the pages and maps the rows, which
+// saves a launch (2 us) where they are few; with more rows one CU takes longer than that.
+template <bool ALL>
+__global__ __launch_bounds__(kMapThreads) void map_plan_kernel(MapArgs a) {
+  __shared__ int32_t s_cu[kSmallSeqs + 1], s_taken[kSmallSeqs + 1], s_back[kSmallSeqs + 1];
+  const bool local = a.B <= kSmallSeqs;
+  // rows as they are packed, then what moves for sequences whose rows fit
+  Sums before{0, 0, 0}, total;
+  for (int32_t b0 = 0; b0 < a.B; b0 += kMapThreads) {
+    const int32_t b = b0 + threadIdx.x;
+    Want x{0, 0, 0, 0, 0};
+    if (b < a.B) x = wanted(a, b);
+    const Sums rows = block_scan(Sums{x.n, 0, 0}, &total);
+    const bool fits = before.rows + rows.rows <= a.rows;
+    const Sums own = moved(x, fits);
+    Sums moves;
+    const Sums end = block_scan(Sums{0, own.taken, own.back}, &moves);
+    if (b < a.B) {
+      const Sums last = before + Sums{rows.rows, end.taken, end.back};
+      const auto store = [&](int32_t i, int64_t r, int64_t t, int64_t g) {
+        a.cu_rows[i] = kept(r);
+        a.taken[i] = kept(t);
+        a.back[i] = kept(g);
+        if (local) s_cu[i] = kept(r), s_taken[i] = kept(t), s_back[i] = kept(g);
+      };
+      store(b, last.rows - x.n, last.taken - own.taken, last.back - own.back);
+      a.from[b] = x.from;
+      if (b == a.B - 1) store(a.B, last.rows, last.taken, last.back);
+    }
+    before = before + Sums{total.rows, moves.taken, moves.back};
+  }
+  __syncthreads();
+  const int32_t *cu = local ? s_cu : a.cu_rows, *taken = local ? s_taken : a.taken, *back = local ? s_back : a.back;
+  const int32_t have = a.n_free[0];
+  const bool sound = have >= 0 && have <= a.pages && before.back <= a.pages - have;
+  const int32_t F = sound ? int32_t(before.back) : 0, top = sound ? have + F : 0;
+  __syncthreads();  // everyone has read n_free
+  // pages given back; those of the sequences behind come first
+  for (int32_t i = threadIdx.x; i < F; i += kMapThreads) {
+    const int32_t b = find(back, a.B, i);
+    const int32_t c = a.from[b] - (back[b + 1] - i);  // ascending pages, descending places
+    int32_t *entry = a.table + int64_t(b) * a.width + c;
+    a.stack[have + (F - 1 - i)] = *entry;
+    *entry = -1;
+  }
+  // every sequence's outcome
+  int32_t used = 0;
+  for (int32_t b0 = 0; b0 < a.B; b0 += kMapThreads) {
+    const int32_t b = b0 + threadIdx.x;
+    if (b >= a.B) break;
+    Want x = wanted(a, b);
+    const bool fits = int64_t(cu[b]) + x.n <= a.rows;
+    const Sums own = moved(x, fits);
+    if (!fits) x.err |= DSDE_ERR_LAYOUT;
+    if (own.taken + own.back > 0 && !sound) x.err |= DSDE_ERR_STATE;
+    if (own.taken > 0 && sound && taken[b + 1] > top) x.err |= DSDE_ERR_PAGES;
+    if (!x.err) {
+      if (own.taken > 0) used = taken[b + 1];
+      if (x.to != x.from) a.held[b] = x.to;
+    }
+    a.base[b] = kept(x.base);
+    a.context[b] = x.err ? 0 : int32_t(x.base + x.n);
+    a.seq_err[b] = x.err;
+  }
+  __shared__ int32_t s_used;
+  if (threadIdx.x == 0) s_used = 0;
+  __syncthreads();
+  if (used > 0) atomicMax(&s_used, used);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (sound) a.n_free[0] = top - s_used;
+    a.top[0] = top;
+  }
+  if (!ALL) return;
+  const int32_t n = s_used;
+  for (int32_t i = threadIdx.x; i < n; i += kMapThreads) take_page(a, taken, top, i);
+  for (int64_t t = threadIdx.x; t < a.rows; t += kMapThreads) map_row(a, cu, taken, top, t);
+}
+
+// Pages taken and rows mapped by the whole card.
+__global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
+  const int64_t stride = int64_t(gridDim.x) * 256, at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int32_t top = a.top[0], n = top > 0 ? top - a.n_free[0] : 0;
+  for (int64_t i = at; i < n; i += stride) take_page(a, a.taken, top, int32_t(i));
+  for (int64_t t = at; t < a.rows; t += stride) map_row(a, a.cu_rows, a.taken, top, t);
+}
+
+// Rows into slots: 16 bytes of a row per lane, a wavefront per row of keys or values.
+// Bound by HBM.
+template <int CACHE>
+__global__ __launch_bounds__(256) void kv_write_kernel(KvWriteArgs a, int64_t first, uint32_t per_head, uint32_t magic) {
+  const int64_t t = first + int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= a.T) return;
+  const int lane = threadIdx.x & 63;
+  const bool values = blockIdx.y != 0;
+  const CacheView &c = a.cache;
+  const int32_t slot = a.slots[t];
+  const bool inside = slot >= 0 && (slot >> c.shift) < c.pages;
+  if (!values && lane == 0) a.row_err[t] = slot >= -1 && (slot < 0 || inside) ? 0u : DSDE_ERR_PAGES;
+  if (!inside) return;
+  const KvRows &rows = values ? a.v : a.k;
+  const char *src = rows.data + t * rows.token_stride;
+  char *dst = (values ? c.v : c.k) + int64_t(slot >> c.shift) * c.page_stride +
+              int64_t(slot & ((1 << c.shift) - 1)) * c.token_stride;
+  const uint32_t n = per_head * uint32_t(c.heads);
+  for (uint32_t i = lane; i < n; i += 64) {
+    const uint32_t h = __umulhi(i, magic), j = i - h * per_head;
+    const uint4 x = *reinterpret_cast<const uint4 *>(src + int64_t(h) * rows.head_stride + j * 16);
+    char *to = dst + int64_t(h) * c.head_stride;
+    if constexpr (CACHE != DSDE_E4M3) {
+      *reinterpret_cast<uint4 *>(to + j * 16) = x;
+    } else {
+      const float s = (values ? c.v_scale : c.k_scale)[h];
+      const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+      uint32_t out[2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        float f[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t bits = q & 1 ? in[2 * p + q / 2] & 0xffff0000u : in[2 * p + q / 2] << 16;
+          const float y = __uint_as_float(bits) / s;
+          f[q] = y != y ? y : fminf(fmaxf(y, -448.0f), 448.0f);
+        }
+        int packed = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+        packed = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], packed, true);
+        out[p] = uint32_t(packed);
+      }
+      *reinterpret_cast<uint2 *>(to + j * 8) = make_uint2(out[0], out[1]);
+    }
+  }
+}
+
+}  // namespace
+
+int launch_kv_map(const MapArgs &a, hipStream_t stream) {
+  if (a.rows <= kSmallRows) {
+    map_plan_kernel<true><<<1, kMapThreads, 0, stream>>>(a);
+  } else {
+    map_plan_kernel<false><<<1, kMapThreads, 0, stream>>>(a);
+    const int64_t blocks = (a.rows + 255) / 256;
+    map_rows_kernel<<<uint32_t(blocks < 2048 ? blocks : 2048), 256, 0, stream>>>(a);
+  }
+  return hipGetLastError() == hipSuccess ? DSDE_OK : DSDE_DEVICE_ERROR;
+}
+
+int launch_kv_write(const KvWriteArgs &a, hipStream_t stream) {
+  const int32_t e = a.dtype == DSDE_FP32 ? 4 : 2;
+  const uint32_t per_head = uint32_t(a.cache.dim * e / 16);  // 2 and more
+  // i / per_head as a high product: exact below 2^27
+  const uint32_t magic = uint32_t(((uint64_t(1) << 32) + per_head - 1) / per_head);
+  // a launch takes fewer than 2^32 threads
+  constexpr int64_t kPass = int64_t(1) << 24;
+  for (int64_t first = 0; first < a.T; first += kPass) {
+    const int64_t n = a.T - first < kPass ? a.T - first : kPass;
+    const dim3 grid(uint32_t((n + 3) / 4), 2);
+    if (a.cache.dtype == DSDE_E4M3)
+      kv_write_kernel<DSDE_E4M3><<<grid, 256, 0, stream>>>(a, first, per_head, magic);
+    else  // the same bits
+      kv_write_kernel<DSDE_BF16><<<grid, 256, 0, stream>>>(a, first, per_head, magic);
+  }
+  return hipGetLastError() == hipSuccess ? DSDE_OK : DSDE_DEVICE_ERROR;
+}
+
+}  // namespace dsde
