@@ -31,6 +31,10 @@ constexpr float kLn2f = 0.69314718f;
 // A row's reference is raised once a score passes it by this much (weights stay under 2^8).
 constexpr float kSlack = 8.0f;
 
+// A call's integer arrays through scalar loads where the index is the same in all lanes (nothing writes them
+// meanwhile): a page that lay in vector registers would take two of them for every load's address.
+using ConstInt = const int32_t __attribute__((address_space(4))) *;
+__device__ __forceinline__ ConstInt constant(const int32_t *p) { return (ConstInt) reinterpret_cast<uintptr_t>(p); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -54,17 +58,23 @@ template <int WORDS>
 struct Words {
   uint32_t w[WORDS];
 };
+// Memory that lanes read through one scalar descriptor and 32-bit offsets; what lies at or behind `bytes` reads as 0.
+using Buffer = __amdgpu_buffer_rsrc_t;
+__device__ __forceinline__ Buffer buffer(const char *base, int32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, bytes, 0x00020000);
+}
+constexpr uint32_t kOutside = 0x40000000;  // an offset behind every buffer here
 template <int WORDS>
-__device__ __forceinline__ Words<WORDS> load_words(const char *base, uint32_t off) {
+__device__ __forceinline__ Words<WORDS> load_words(Buffer from, uint32_t off, uint32_t base = 0) {
   Words<WORDS> r;
   if constexpr (WORDS == 4) {
-    const u32x4 x = *reinterpret_cast<const u32x4 *>(base + off);
+    const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, off, base, 0));
     r.w[0] = x.x, r.w[1] = x.y, r.w[2] = x.z, r.w[3] = x.w;
   } else if constexpr (WORDS == 2) {
-    const u32x2 x = *reinterpret_cast<const u32x2 *>(base + off);
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, off, base, 0));
     r.w[0] = x.x, r.w[1] = x.y;
   } else {
-    r.w[0] = *reinterpret_cast<const uint32_t *>(base + off);
+    r.w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, off, base, 0);
   }
   return r;
 }
@@ -99,10 +109,10 @@ struct Seq {
 template <int TILE>
 __device__ __forceinline__ Seq sequence(const AttendArgs &a, int32_t b, int32_t block_rows) {
   Seq s;
-  s.row0 = a.cu_rows[b];
-  const int64_t end = a.cu_rows[b + 1];
+  s.row0 = constant(a.cu_rows)[b];
+  const int64_t end = constant(a.cu_rows)[b + 1];
   s.n = int32_t(end - s.row0);
-  s.context = a.context[b];
+  s.context = constant(a.context)[b];
   s.err = 0;
   if (s.row0 < 0 || end < s.row0 || end > a.T || end - s.row0 > a.max_rows) {
     s.err = DSDE_ERR_LAYOUT;
@@ -168,13 +178,12 @@ struct Wave {
   const AttendArgs &a;
   const Seq &s;
   int lane, r, g;
-  bool whole;  // dim == DP
   const char *k_head, *v_head;  // of the head, from the cache's start
-  const int32_t *table;         // of the sequence
+  ConstInt table;               // of the sequence
   float c;                      // scale log2(e), with the keys' scale
   int32_t mtiles;               // row tiles of this block that have rows
   Rows<MT> rows;
-  uint32_t k_off, v_off[4];
+  uint32_t k_off, v_off;
 
   uint32_t q[MT][S::kQWords];
   f32x4 o[MT][S::kSets][S::kVec];
@@ -183,47 +192,43 @@ struct Wave {
   Words<4> k[S::kSub][S::kChunks];
   Words<S::kVecWords> v[S::kKeys][S::kSets];
 
+  // A subtile's place in the cache.
   struct At {
-    int32_t page, first;  // of a subtile: its page (-1: bad), its first token's place in that page
+    int64_t offset;
+    bool bad;    // its page is none
+    bool there;  // it is to be read
   };
-  __device__ __forceinline__ At locate(int32_t tile, int t) const {
+  __device__ __forceinline__ At locate(int32_t tile, int t, bool wanted) const {
     const int32_t key = tile * S::kTile + 16 * t;
+    const int32_t page = wanted && key < s.context ? table[key >> a.cache.shift] : 0;
     At x;
-    x.page = key < s.context ? table[key >> a.cache.shift] : 0;
-    x.first = key & ((1 << a.cache.shift) - 1);
+    x.bad = uint32_t(page) >= uint32_t(a.cache.pages);
+    x.there = wanted && !x.bad;
+    x.offset = (x.bad ? 0 : int64_t(page) * a.cache.page_stride) + int64_t(key & ((1 << a.cache.shift) - 1)) * a.cache.token_stride;
     return x;
   }
-  __device__ __forceinline__ int64_t offset(const At &x) const {
-    const int32_t page = uint32_t(x.page) < uint32_t(a.cache.pages) ? x.page : 0;
-    return int64_t(page) * a.cache.page_stride + int64_t(x.first) * a.cache.token_stride;
-  }
-  __device__ __forceinline__ bool k_valid(int j) const { return (4 * j + g) * S::kPer16 < a.cache.dim; }
+  // Bytes of a subtile's 16 rows; none of one that is not to be read, whose loads give 0 without memory.
+  __device__ __forceinline__ int32_t span(const At &x) const { return x.there ? 15 * a.cache.token_stride + a.cache.dim * S::kElt : 0; }
 
   __device__ __forceinline__ void load_k(const At (&at)[S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
-      const char *base = k_head + offset(at[t]);
-      if (whole) {
+      const Buffer from = buffer(k_head + at[t].offset, span(at[t]));
 #pragma unroll
-        for (int j = 0; j < S::kChunks; ++j) k[t][j] = load_words<4>(base, k_off + 64 * j);
-      } else {  // chunks behind the row's end: its first one, zeroed when it is used
-#pragma unroll
-        for (int j = 0; j < S::kChunks; ++j) k[t][j] = load_words<4>(base, k_valid(j) ? k_off + 64 * j : k_off - 16 * g);
-      }
+      for (int j = 0; j < S::kChunks; ++j)  // 0 behind the row's end
+        k[t][j] = load_words<4>(from, (4 * j + g) * S::kPer16 < a.cache.dim ? k_off + 64 * j : kOutside);
     }
   }
   __device__ __forceinline__ void load_v(const At (&at)[S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
-      const char *base = v_head + offset(at[t]);
+      const Buffer from = buffer(v_head + at[t].offset, span(at[t]));
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int e = 0; e < S::kSets; ++e) {
+        const uint32_t off = (16 * e + r) * S::kVec < a.cache.dim ? v_off + 16 * S::kVecBytes * e : kOutside;
 #pragma unroll
-        for (int e = 0; e < S::kSets; ++e) {
-          uint32_t off = v_off[i] + 16 * S::kVecBytes * e;
-          if (!whole && (16 * e + r) * S::kVec >= a.cache.dim) off = v_off[i] - S::kVecBytes * r;  // not written in the end
-          v[4 * t + i][e] = load_words<S::kVecWords>(base, off);
-        }
+        for (int i = 0; i < 4; ++i) v[4 * t + i][e] = load_words<S::kVecWords>(from, off, i * a.cache.token_stride);
+      }
     }
   }
 
@@ -242,7 +247,10 @@ struct Wave {
       else
         d = (4 * i + g) * S::kPer16;
       Words<4> x{};
-      if (live && d < a.cache.dim) x = load_words<4>(p, uint32_t(d) * kQElt);
+      if (live && d < a.cache.dim) {
+        const u32x4 y = *reinterpret_cast<const u32x4 *>(p + d * kQElt);
+        x = Words<4>{{y.x, y.y, y.z, y.w}};
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) q[mt][4 * i + e] = x.w[e];
     }
@@ -250,16 +258,15 @@ struct Wave {
     rows.lo[mt] = a.window > 0 && rows.hi[mt] >= a.window ? rows.hi[mt] - a.window + 1 : 0;
   }
 
-  // Scores of a tile, in the log2 domain.
-  __device__ __forceinline__ void scores(f32x4 (&x)[MT][S::kSub]) {
+  // Scores of a tile, in the log2 domain; NaN of a bad page (its keys are 0).
+  __device__ __forceinline__ void scores(f32x4 (&x)[MT][S::kSub], const At (&at)[S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) x[mt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < S::kChunks; ++j) {
-        Words<4> w = k[t][j];
-        if (!whole && !k_valid(j)) w = Words<4>{};
+        const Words<4> &w = k[t][j];
         if constexpr (CACHE == DSDE_FP32) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -286,8 +293,9 @@ struct Wave {
           }
         }
       }
+      const float f = at[t].bad ? NAN : c;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) x[mt][t] *= c;
+      for (int mt = 0; mt < MT; ++mt) x[mt][t] *= f;
     }
   }
 
@@ -371,26 +379,23 @@ struct Wave {
     }
   }
 
-  // Scores that some row does not see, or of a bad page.
-  __device__ __forceinline__ void mask(f32x4 (&x)[MT][S::kSub], int32_t tile, const bool (&bad)[S::kSub]) {
+  // Scores that some row does not see.
+  __device__ __forceinline__ void mask(f32x4 (&x)[MT][S::kSub], int32_t tile) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          x[mt][t][i] = key >= rows.lo[mt] && key <= rows.hi[mt] ? (bad[t] ? NAN : x[mt][t][i]) : -INFINITY;
+        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= rows.lo[mt] && key <= rows.hi[mt] ? x[mt][t][i] : -INFINITY;
       }
   }
-  // The same for values: a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0; where
-  // a value that some rows see is not finite (rare), the tile's values are read again for each of the sequence's tokens, which adds what it sees.
-  __device__ __forceinline__ void add_masked(const f32x4 (&p)[MT][S::kSub], int32_t tile, const At (&from)[S::kSub], const bool (&bad)[S::kSub]) {
+  __device__ __forceinline__ bool keep(int32_t tile, int32_t lo, int32_t hi) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < S::kKeys; ++i) {
       const int32_t key = tile * S::kTile + 16 * (i / 4) + 4 * g + i % 4;
-      const bool seen = key >= rows.lo_any && key <= rows.hi_any && !bad[i / 4];
+      const bool seen = key >= lo && key <= hi;
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
@@ -399,24 +404,19 @@ struct Wave {
           odd |= not_finite<CACHE>(v[i][e].w[w]);
         }
     }
-    if (!__any(odd)) {
-      add(p);
-      return;
-    }
-    const int32_t first = s.context - s.n;
-    for (int32_t at = first; at < s.context; ++at) {
+    return __any(odd);
+  }
+  // The same for values: a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0; where
+  // one that some rows see is not finite (rare), the tile's values are read again for each of the sequence's tokens,
+  // which adds what it sees, and then all become 0.
+  __device__ __forceinline__ void mask_values(const f32x4 (&p)[MT][S::kSub], int32_t tile, const At (&from)[S::kSub]) {
+    if (!keep(tile, rows.lo_any, rows.hi_any)) return;
+    for (int32_t token = s.context - s.n; token < s.context; ++token) {
       load_v(from);
-      const int32_t lo = a.window > 0 && at >= a.window ? at - a.window + 1 : 0;
-#pragma unroll
-      for (int i = 0; i < S::kKeys; ++i) {
-        const int32_t key = tile * S::kTile + 16 * (i / 4) + 4 * g + i % 4;
-#pragma unroll
-        for (int e = 0; e < S::kSets; ++e)
-#pragma unroll
-          for (int w = 0; w < S::kVecWords; ++w) v[i][e].w[w] = key >= lo && key <= at && !bad[i / 4] ? v[i][e].w[w] : 0;
-      }
-      add<true>(p, at);
+      keep(tile, a.window > 0 && token >= a.window ? token - a.window + 1 : 0, token);
+      add<true>(p, token);
     }
+    keep(tile, 0, -1);
   }
 
   // Tiles first, first + step, ... below end.
@@ -424,34 +424,24 @@ struct Wave {
     if (first >= end) return;
     At at[S::kSub], next[S::kSub];
 #pragma unroll
-    for (int t = 0; t < S::kSub; ++t) at[t] = locate(first, t);
+    for (int t = 0; t < S::kSub; ++t) at[t] = locate(first, t, true);
     load_k(at);
     load_v(at);
+    // The next tile's keys are on their way while this one's values are weighed, and its values while the next scores
+    // are taken, into registers that have just been read; a tile behind the last is none.  No load stands behind a
+    // branch: waits could not be counted then.
     for (int32_t tile = first; tile < end; tile += step) {
-      const bool more = tile + step < end;
-      if (more) {
 #pragma unroll
-        for (int t = 0; t < S::kSub; ++t) next[t] = locate(tile + step, t);
-      }
+      for (int t = 0; t < S::kSub; ++t) next[t] = locate(tile + step, t, tile + step < end);
       f32x4 x[MT][S::kSub];
-      scores(x);
-      if (more) load_k(next);
-      bool bad[S::kSub];
-      bool clear = tile * S::kTile >= rows.lo_all && tile * S::kTile + S::kTile - 1 <= rows.hi_all;
-#pragma unroll
-      for (int t = 0; t < S::kSub; ++t) {
-        bad[t] = uint32_t(at[t].page) >= uint32_t(a.cache.pages);
-        clear &= !bad[t];
-      }
-      if (clear) {
-        weigh(x);
-        add(x);
-      } else {
-        mask(x, tile, bad);
-        weigh(x);
-        add_masked(x, tile, at, bad);
-      }
-      if (more) load_v(next);
+      scores(x, at);
+      load_k(next);
+      const bool clear = tile * S::kTile >= rows.lo_all && tile * S::kTile + S::kTile - 1 <= rows.hi_all;
+      if (!clear) mask(x, tile);
+      weigh(x);
+      if (!clear) mask_values(x, tile, at);
+      add(x);
+      load_v(next);
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) at[t] = next[t];
     }
@@ -528,14 +518,13 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs 
 
     Wave<CACHE, DP, MT> w{a, s};
     w.lane = lane, w.r = lane & 15, w.g = lane >> 4;
-    w.whole = a.cache.dim == DP;
     w.k_head = a.cache.k + at.h * a.cache.head_stride;
     w.v_head = a.cache.v + at.h * a.cache.head_stride;
-    w.table = a.table + int64_t(at.b) * a.width;
+    w.table = constant(a.table + int64_t(at.b) * a.width);
     w.c = a.scale * kLog2e;
     if constexpr (CACHE == DSDE_E4M3) w.c *= a.cache.k_scale[at.h];
     w.k_off = uint32_t(w.r * a.cache.token_stride + 16 * w.g);
-    for (int i = 0; i < 4; ++i) w.v_off[i] = uint32_t((4 * w.g + i) * a.cache.token_stride + S::kVecBytes * w.r);
+    w.v_off = uint32_t(4 * w.g * a.cache.token_stride + S::kVecBytes * w.r);
     const char *q = a.q.data + s.row0 * a.q.token_stride + int64_t(at.h) * a.group * a.q.head_stride;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
