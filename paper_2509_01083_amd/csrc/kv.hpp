@@ -78,25 +78,18 @@ inline int row_tiles(int32_t group, int32_t max_rows, int32_t dim) {
   const int most = dim > 128 ? 2 : 4;
   return m <= 16 ? 1 : m <= 32 || most == 2 ? 2 : 4;
 }
-constexpr int kAttendGroups = 1024;  // workgroups of the largest launch
+// Wavefronts of the largest launch times the row blocks of each.
+constexpr int kAttendParts = 4096;
 inline int padded_dim(int32_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-// A partial result: a row's values, its reference and its sum of weights.
-inline size_t partial_floats(int tiles, int32_t dim) { return size_t(16) * tiles * (padded_dim(dim) + 2); }
 struct AttendLayout {
-  size_t units, partial, total;
+  size_t starts, parts, total;
 };
-__host__ __device__ constexpr size_t attend_layout_partial(int32_t B) {
-  return (sizeof(int64_t) * (size_t(B) + 1) + 255) & ~size_t(255);
-}
-inline AttendLayout attend_layout(int32_t B, int32_t group, int32_t max_rows, int32_t dim) {
+inline AttendLayout attend_layout(int32_t, int32_t dim) {
   AttendLayout l;
-  l.units = 0;  // [B+1] int64: prefix sums of the sequences' work
-  l.partial = attend_layout_partial(B);
-  // grows with dim too, where larger heads take fewer row blocks
-  const size_t wide = partial_floats(row_tiles(group, max_rows, dim), dim);
-  const int32_t d = dim < 128 ? dim : 128;
-  const size_t narrow = partial_floats(row_tiles(group, max_rows, d), d);
-  l.total = l.partial + align_up(sizeof(float) * 2 * kAttendGroups * (wide > narrow ? wide : narrow));
+  l.starts = 0;  // where each wavefront's share begins
+  l.parts = align_up(size_t(24) * kAttendParts);
+  // two parts of a wavefront: for each of its rows the values, a reference and a sum
+  l.total = l.parts + align_up(sizeof(float) * 2 * kAttendParts * 16 * size_t(padded_dim(dim) + 2));
   return l;
 }
 int launch_kv_attention(const AttendArgs &a, hipStream_t stream);

@@ -129,39 +129,51 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, int32_t b, int32_t 
   s.blocks = (s.n * a.group + block_rows - 1) / block_rows;
   return s;
 }
-template <int TILE>
-__device__ __forceinline__ int64_t units_of(const AttendArgs &a, int32_t b, int32_t block_rows) {
-  const Seq s = sequence<TILE>(a, b, block_rows);
-  return int64_t(s.tiles) * s.blocks * a.cache.heads;
+// The work in one line: for every sequence, key head and row block an item of kStart units (what it costs to begin
+// and end one, in tiles) and a unit for each tile.  Every wavefront takes an equal share of the line, whatever the
+// lengths are, so that all end together; items that it has a part of leave that part to join_kernel.
+constexpr int32_t kStart = 4;
+constexpr int32_t kLeast = 4;  // units of a share at least: short calls do not end in joining many parts
+__device__ __forceinline__ int64_t share_of(int64_t all, int32_t workers) {
+  const int64_t n = (all + workers - 1) / workers;
+  return n > kLeast ? n : kLeast;
 }
-
-// Units of work (a tile of one head and one row block) that each workgroup takes: a tile per
-// wavefront at least, so that short calls do not end in joining many parts.
-__device__ __forceinline__ int64_t share_of(int64_t all, int32_t groups) {
-  const int64_t n = (all + groups - 1) / groups;
-  return n > kAttendWaves ? n : kAttendWaves;
+__device__ __forceinline__ int64_t units_of(const AttendArgs &a, const Seq &s) {
+  return int64_t(s.tiles + kStart) * s.blocks * a.cache.heads;
 }
-
-// A row's reference, sum and values where parts meet.
-struct Joined {
-  float m, l;
+// Where a wavefront's share begins inside an item (tile > 0), and the wavefronts that have parts of that item.
+struct Start {
+  int32_t b, h, block, tile, w0, w1;
 };
+// A wavefront has two places for parts: 0 for one that another began, 1 for one that it began and did not end.
+__device__ __forceinline__ float *part_of(const AttendArgs &a, size_t at, int64_t worker, int slot, size_t floats) {
+  return reinterpret_cast<float *>(static_cast<char *>(a.workspace) + at) + size_t(2 * worker + slot) * floats;
+}
 
-// Writes columns d .. d+3 of a finished row, and with `stats` its log-normaliser.
+// kVec values of a finished row, from dimension d on.
+template <int CACHE, int VEC>
+__device__ __forceinline__ void store_row(char *row, int32_t d, const float (&x)[VEC]) {
+  if constexpr (CACHE == DSDE_FP32) {
+    *reinterpret_cast<f32x4 *>(row + d * 4) = f32x4{x[0], x[1], x[2], x[3]};
+  } else if constexpr (VEC == 8) {
+    *reinterpret_cast<u32x4 *>(row + d * 2) =
+        u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+  } else {
+    *reinterpret_cast<u32x2 *>(row + d * 2) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  }
+}
+// A finished row's place, its factor and its log-normaliser.
 template <int CACHE>
-__device__ __forceinline__ void finish(const AttendArgs &a, const Seq &s, int32_t h, int32_t row, Joined x, f32x4 o, int32_t d,
-                                       bool stats) {
+__device__ __forceinline__ char *finished(const AttendArgs &a, const Seq &s, int32_t h, int32_t row, float m, float l, bool stats,
+                                          float *factor) {
   const int32_t j = row / a.group, head = h * a.group + (row - j * a.group);
   const int64_t t = int64_t(s.row0) + j;
-  if (stats && a.lse) a.lse[t * (int64_t(a.group) * a.cache.heads) + head] = x.l == 0.0f ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * kLn2f;
-  if (d >= a.cache.dim) return;
-  float inv = x.l == 0.0f ? 0.0f : 1.0f / x.l;
-  if constexpr (CACHE == DSDE_E4M3) inv *= a.cache.v_scale[h];
-  char *to = a.out + t * a.out_token_stride + int64_t(head) * a.out_head_stride;
-  if constexpr (CACHE == DSDE_FP32)
-    *reinterpret_cast<f32x4 *>(to + d * 4) = o * inv;
-  else
-    *reinterpret_cast<u32x2 *>(to + d * 2) = u32x2{pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv)};
+  if (stats && a.lse)
+    a.lse[t * (int64_t(a.group) * a.cache.heads) + head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2f;
+  float f = l == 0.0f ? 0.0f : 1.0f / l;
+  if constexpr (CACHE == DSDE_E4M3) f *= a.cache.v_scale[h];
+  *factor = f;
+  return a.out + t * a.out_token_stride + int64_t(head) * a.out_head_stride;
 }
 
 // The wavefront's view of its rows.
@@ -180,7 +192,9 @@ struct Wave {
   int lane, r, g;
   const char *k_head, *v_head;  // of the head, from the cache's start
   ConstInt table;               // of the sequence
-  float c;                      // scale log2(e), with the keys' scale
+  float c;                      // scale log2(e), with the keys' scale, positive
+  uint32_t flip;                // sign bits of a word of queries, where the scale is negative
+  bool flat;                    // the scale is 0
   int32_t mtiles;               // row tiles of this block that have rows
   Rows<MT> rows;
   uint32_t k_off, v_off;
@@ -249,7 +263,7 @@ struct Wave {
       Words<4> x{};
       if (live && d < a.cache.dim) {
         const u32x4 y = *reinterpret_cast<const u32x4 *>(p + d * kQElt);
-        x = Words<4>{{y.x, y.y, y.z, y.w}};
+        if (!flat) x = Words<4>{{y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip}};
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) q[mt][4 * i + e] = x.w[e];
@@ -258,8 +272,8 @@ struct Wave {
     rows.lo[mt] = a.window > 0 && rows.hi[mt] >= a.window ? rows.hi[mt] - a.window + 1 : 0;
   }
 
-  // Scores of a tile, in the log2 domain; NaN of a bad page (its keys are 0).
-  __device__ __forceinline__ void scores(f32x4 (&x)[MT][S::kSub], const At (&at)[S::kSub]) {
+  // Scores of a tile, without their scale.
+  __device__ __forceinline__ void scores(f32x4 (&x)[MT][S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
 #pragma unroll
@@ -293,19 +307,18 @@ struct Wave {
           }
         }
       }
-      const float f = at[t].bad ? NAN : c;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) x[mt][t] *= f;
     }
   }
 
-  // Raises references where scores pass them, and turns scores into weights.
-  __device__ __forceinline__ void weigh(f32x4 (&x)[MT][S::kSub]) {
+  // Raises references (in the log2 domain) where scores pass them, and turns scores into weights; those of a bad page,
+  // whose keys read as 0, into NaN.
+  __device__ __forceinline__ void weigh(f32x4 (&x)[MT][S::kSub], const At (&at)[S::kSub]) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) top = fmaxf(fmaxf(fmaxf(x[mt][t].x, x[mt][t].y), fmaxf(x[mt][t].z, x[mt][t].w)), top);
+      top *= c;
       if (__any(top > m[mt] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -322,7 +335,9 @@ struct Wave {
       float sum = 0.0f;
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) {
-        x[mt][t] = f32x4{exp2_fast(x[mt][t].x - ref), exp2_fast(x[mt][t].y - ref), exp2_fast(x[mt][t].z - ref), exp2_fast(x[mt][t].w - ref)};
+        const float f = at[t].bad ? NAN : c;
+        x[mt][t] = f32x4{exp2_fast(fmaf(x[mt][t].x, f, -ref)), exp2_fast(fmaf(x[mt][t].y, f, -ref)),
+                         exp2_fast(fmaf(x[mt][t].z, f, -ref)), exp2_fast(fmaf(x[mt][t].w, f, -ref))};
         sum += (x[mt][t].x + x[mt][t].y) + (x[mt][t].z + x[mt][t].w);
       }
       l[mt] += sum;
@@ -409,7 +424,7 @@ struct Wave {
   // The same for values: a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0; where
   // one that some rows see is not finite (rare), the tile's values are read again for each of the sequence's tokens,
   // which adds what it sees, and then all become 0.
-  __device__ __forceinline__ void mask_values(const f32x4 (&p)[MT][S::kSub], int32_t tile, const At (&from)[S::kSub]) {
+  __device__ __forceinline__ void mask_values(const f32x4 (&p)[MT][S::kSub], int32_t tile, const At (&from)[S::kSub], const At (&next)[S::kSub]) {
     if (!keep(tile, rows.lo_any, rows.hi_any)) return;
     for (int32_t token = s.context - s.n; token < s.context; ++token) {
       load_v(from);
@@ -417,11 +432,11 @@ struct Wave {
       add<true>(p, token);
     }
     keep(tile, 0, -1);
+    load_k(next);  // again: this path has had their registers
   }
 
-  // Tiles first, first + step, ... below end.
-  __device__ __forceinline__ void run(int32_t first, int32_t end, int32_t step) {
-    if (first >= end) return;
+  // Tiles first .. end - 1.
+  __device__ __forceinline__ void run(int32_t first, int32_t end) {
     At at[S::kSub], next[S::kSub];
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) at[t] = locate(first, t, true);
@@ -430,16 +445,16 @@ struct Wave {
     // The next tile's keys are on their way while this one's values are weighed, and its values while the next scores
     // are taken, into registers that have just been read; a tile behind the last is none.  No load stands behind a
     // branch: waits could not be counted then.
-    for (int32_t tile = first; tile < end; tile += step) {
+    for (int32_t tile = first; tile < end; ++tile) {
 #pragma unroll
-      for (int t = 0; t < S::kSub; ++t) next[t] = locate(tile + step, t, tile + step < end);
+      for (int t = 0; t < S::kSub; ++t) next[t] = locate(tile + 1, t, tile + 1 < end);
       f32x4 x[MT][S::kSub];
-      scores(x, at);
+      scores(x);
       load_k(next);
       const bool clear = tile * S::kTile >= rows.lo_all && tile * S::kTile + S::kTile - 1 <= rows.hi_all;
       if (!clear) mask(x, tile);
-      weigh(x);
-      if (!clear) mask_values(x, tile, at);
+      weigh(x, at);
+      if (!clear) mask_values(x, tile, at, next);
       add(x);
       load_v(next);
 #pragma unroll
@@ -448,27 +463,27 @@ struct Wave {
   }
 };
 
-// A place in the order of all work: sequence, key head, row block, tile.
-struct Cursor {
-  int32_t b, h, block, tile;
-};
-
 template <int CACHE, int DP, int MT, int OCC>
-__global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs a, AttendLayout at) {
   using S = Shape<CACHE, DP>;
   constexpr int kRows = 16 * MT;
-  constexpr int kPitch = DP + 4;
-  __shared__ float s_o[kAttendWaves][16][kPitch];
-  __shared__ float s_m[kAttendWaves][kRows], s_l[kAttendWaves][kRows];
+  constexpr size_t kPart = kRows * (DP + 2);
+  struct Begin {
+    Start at;
+    int64_t tile0_unit;  // of the item's first tile
+    int32_t used;        // units of its start that lie before the share
+    Seq s;
+  };
   __shared__ int64_t s_sum[kAttendWaves];
-  __shared__ Cursor s_at;
+  __shared__ Begin s_begin[kAttendWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
 
-  // where this workgroup's share of the work begins
+  // where each wavefront's share begins; neighbours in the line are in different workgroups, so that few shares
+  // spread over many CUs
   const int32_t per = (a.B + kAttendThreads - 1) / kAttendThreads;
   const int32_t b0 = tid * per < a.B ? tid * per : a.B, b1 = b0 + per < a.B ? b0 + per : a.B;
   int64_t own = 0;
-  for (int32_t b = b0; b < b1; ++b) own += units_of<S::kTile>(a, b, kRows);
+  for (int32_t b = b0; b < b1; ++b) own += units_of(a, sequence<S::kTile>(a, b, kRows));
   int64_t upto = own;
   for (int n = 1; n < 64; n <<= 1) {
     const int64_t o = __shfl_up(upto, n);
@@ -481,51 +496,59 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs 
     if (i < wave) upto += s_sum[i];
     all += s_sum[i];
   }
-  const int64_t share = share_of(all, gridDim.x);
-  const int64_t begin = int64_t(blockIdx.x) * share, end = begin + share < all ? begin + share : all;
-  int64_t before = upto - own;
-  const bool mine = begin >= before && begin < upto;
-  if (mine || blockIdx.x == 0) {
-    int64_t *units = static_cast<int64_t *>(a.workspace);
+  const int32_t workers = int32_t(gridDim.x) * kAttendWaves;
+  const int64_t share = share_of(all, workers);
+  for (int i = 0; i < kAttendWaves; ++i) {
+    const int64_t begin = (int64_t(i) * gridDim.x + blockIdx.x) * share;
+    int64_t before = upto - own;
+    if (begin < before || begin >= upto) continue;
     for (int32_t b = b0; b < b1; ++b) {
       const Seq s = sequence<S::kTile>(a, b, kRows);
-      const int64_t n = int64_t(s.tiles) * s.blocks * a.cache.heads;
-      if (begin >= before && begin < before + n) {
+      const int64_t n = units_of(a, s);
+      if (begin < before + n) {
         const int64_t x = begin - before;
-        const int32_t item = int32_t(x / s.tiles);
-        s_at = Cursor{b, item / s.blocks, item % s.blocks, int32_t(x % s.tiles)};
+        const int32_t size = s.tiles + kStart, item = int32_t(x / size), u = int32_t(x - int64_t(item) * size);
+        const int64_t unit = before + int64_t(item) * size + kStart;
+        const int32_t h = item / s.blocks;
+        s_begin[i] = Begin{Start{b, h, item - h * s.blocks, u > kStart ? u - kStart : 0, int32_t(unit / share),
+                                 int32_t((unit + s.tiles - 1) / share)}, unit, u < kStart ? u : kStart, s};
+        break;
       }
-      if (blockIdx.x == 0) units[b] = before;
       before += n;
     }
-    if (blockIdx.x == 0 && tid == 0) units[a.B] = all;
   }
-  if (begin >= end) return;
   __syncthreads();
+  const int64_t worker = int64_t(wave) * gridDim.x + blockIdx.x;
+  const int64_t begin = worker * share, end = begin + share < all ? begin + share : all;
+  Start *starts = reinterpret_cast<Start *>(static_cast<char *>(a.workspace) + at.starts);
+  if (begin >= end) {
+    if (lane == 0) starts[worker].tile = 0;
+    return;
+  }
+  Start x = s_begin[wave].at;
+  if (lane == 0) starts[worker] = x;
+  x.b = uniform(x.b), x.h = uniform(x.h), x.block = uniform(x.block), x.tile = uniform(x.tile);
+  Seq s = s_begin[wave].s;
+  s.row0 = uniform(s.row0), s.n = uniform(s.n), s.context = uniform(s.context), s.tile0 = uniform(s.tile0);
+  s.tiles = uniform(s.tiles), s.blocks = uniform(s.blocks), s.err = uint32_t(uniform(int(s.err)));
+  int64_t left = end - begin - (kStart - uniform(s_begin[wave].used));
 
-  int64_t left = end - begin;
-  Cursor at = s_at;
-  at.b = uniform(at.b), at.h = uniform(at.h), at.block = uniform(at.block), at.tile = uniform(at.tile);
-  bool first = true;
-  while (left > 0 && at.b < a.B) {
-    Seq s = sequence<S::kTile>(a, at.b, kRows);
-    if (s.blocks == 0) {
-      at = Cursor{at.b + 1, 0, 0, 0};
-      continue;
-    }
-    const int32_t count = int32_t(left < s.tiles - at.tile ? left : s.tiles - at.tile);
-    const int32_t rows = s.n * a.group, row0 = at.block * kRows;
+  while (left > 0) {
+    const int32_t count = int32_t(left < s.tiles - x.tile ? left : s.tiles - x.tile);
+    const int32_t rows = s.n * a.group, row0 = x.block * kRows;
 
     Wave<CACHE, DP, MT> w{a, s};
     w.lane = lane, w.r = lane & 15, w.g = lane >> 4;
-    w.k_head = a.cache.k + at.h * a.cache.head_stride;
-    w.v_head = a.cache.v + at.h * a.cache.head_stride;
-    w.table = constant(a.table + int64_t(at.b) * a.width);
-    w.c = a.scale * kLog2e;
-    if constexpr (CACHE == DSDE_E4M3) w.c *= a.cache.k_scale[at.h];
+    w.k_head = a.cache.k + x.h * a.cache.head_stride;
+    w.v_head = a.cache.v + x.h * a.cache.head_stride;
+    w.table = constant(a.table + int64_t(x.b) * a.width);
+    const float c = a.scale * kLog2e * (CACHE == DSDE_E4M3 ? a.cache.k_scale[x.h] : 1.0f);
+    w.flat = fabsf(c) < 0x1p-126f;
+    w.c = w.flat ? 1.0f : fabsf(c);
+    w.flip = c < 0.0f ? (CACHE == DSDE_FP32 ? 0x80000000u : 0x80008000u) : 0u;
     w.k_off = uint32_t(w.r * a.cache.token_stride + 16 * w.g);
     w.v_off = uint32_t(4 * w.g * a.cache.token_stride + S::kVecBytes * w.r);
-    const char *q = a.q.data + s.row0 * a.q.token_stride + int64_t(at.h) * a.group * a.q.head_stride;
+    const char *q = a.q.data + s.row0 * a.q.token_stride + int64_t(x.h) * a.group * a.q.head_stride;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       w.load_q(q, row0 + 16 * mt + w.r, rows, mt);
@@ -539,87 +562,74 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs 
     w.rows.hi_all = oldest, w.rows.hi_any = newest;
     w.rows.lo_all = a.window > 0 && newest >= a.window ? newest - a.window + 1 : 0;
     w.rows.lo_any = a.window > 0 && oldest >= a.window ? oldest - a.window + 1 : 0;
-    const int32_t t0 = s.tile0 + at.tile;
-    w.run(t0 + wave, t0 + count, kAttendWaves);
+    w.run(s.tile0 + x.tile, s.tile0 + x.tile + count);
 
-    // join the wavefronts
+    const bool done = count == s.tiles;
+    float *part = part_of(a, at.parts, worker, x.tile > 0 ? 0 : 1, kPart);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
+      const int32_t row = row0 + 16 * mt + w.r;
       float l = w.l[mt];
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
-      if (w.g == 0) s_m[wave][16 * mt + w.r] = w.m[mt], s_l[wave][16 * mt + w.r] = l;
-    }
-    const bool done = count == s.tiles;
-    float *partial = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + attend_layout_partial(a.B)) +
-                     (int64_t(blockIdx.x) * 2 + (first ? 0 : 1)) * (kRows * (DP + 2));
-    for (int mt = 0; mt < MT; ++mt) {
-      if (row0 + 16 * mt >= rows) break;
+      if (s.err) l = NAN;  // a context that is none
+      if (row < rows) {
+        float f = 1.0f;
+        char *to = nullptr;
+        if (done) to = finished<CACHE>(a, s, x.h, row, w.m[mt], l, w.g == 0, &f);
 #pragma unroll
-      for (int x = 0; x < MT; ++x)
-        if (x == mt) {
+        for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
-          for (int e = 0; e < S::kSets; ++e)
+          for (int i = 0; i < 4; ++i) {
+            const int32_t d = (16 * e + 4 * w.g + i) * S::kVec;
+            float y[S::kVec];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < S::kVec; ++j) y[j] = w.o[mt][e][j][i] * f;
+            if (done) {
+              if (d < a.cache.dim) store_row<CACHE, S::kVec>(to, d, y);
+            } else {
 #pragma unroll
               for (int j = 0; j < S::kVec; j += 4)
-                *reinterpret_cast<f32x4 *>(&s_o[wave][w.r][(16 * e + 4 * w.g + i) * S::kVec + j]) =
-                    f32x4{w.o[x][e][j][i], w.o[x][e][j + 1][i], w.o[x][e][j + 2][i], w.o[x][e][j + 3][i]};
+                *reinterpret_cast<f32x4 *>(part + (16 * mt + w.r) * DP + d + j) = f32x4{y[j], y[j + 1], y[j + 2], y[j + 3]};
+            }
+          }
+        if (!done && w.g == 0) {
+          part[kRows * DP + 16 * mt + w.r] = w.m[mt];
+          part[kRows * (DP + 1) + 16 * mt + w.r] = l;
         }
-      __syncthreads();
-      const int32_t rr = tid >> 4, cc = tid & 15, row = row0 + 16 * mt + rr;
-      if (row < rows) {
-        float top = -INFINITY;
-        for (int i = 0; i < kAttendWaves; ++i) top = fmaxf(top, s_m[i][16 * mt + rr]);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float f[kAttendWaves], sum = 0.0f;
-        for (int i = 0; i < kAttendWaves; ++i) {
-          f[i] = exp2_fast(s_m[i][16 * mt + rr] - ref);
-          sum += f[i] * s_l[i][16 * mt + rr];
-        }
-        if (s.err) sum = NAN;  // a context that is none
-#pragma unroll
-        for (int k = 0; k < DP / 64; ++k) {
-          const int32_t d = 64 * k + 4 * cc;
-          f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
-          for (int i = 0; i < kAttendWaves; ++i) o += f[i] * *reinterpret_cast<const f32x4 *>(&s_o[i][rr][d]);
-          if (done)
-            finish<CACHE>(a, s, at.h, row, Joined{top, sum}, o, d, k == 0 && cc == 0);
-          else
-            *reinterpret_cast<f32x4 *>(&partial[(16 * mt + rr) * DP + d]) = o;
-        }
-        if (!done && cc == 0) partial[kRows * DP + 16 * mt + rr] = top, partial[kRows * (DP + 1) + 16 * mt + rr] = sum;
       }
-      __syncthreads();
     }
 
-    left -= count;
-    first = false;
-    at.tile = 0;
-    if (++at.block == s.blocks) {
-      at.block = 0;
-      if (++at.h == a.cache.heads) at = Cursor{at.b + 1, 0, 0, 0};
+    left -= count + kStart;
+    x.tile = 0;
+    if (left <= 0) break;
+    if (++x.block == s.blocks) {
+      x.block = 0;
+      if (++x.h == a.cache.heads) {
+        x.h = 0;
+        do {
+          if (++x.b >= a.B) return;
+          s = sequence<S::kTile>(a, x.b, kRows);
+        } while (s.blocks == 0);
+      }
     }
   }
 }
 
-// Joins the parts of rows whose tokens more than one workgroup had, and checks every sequence.
+// Joins the parts of items that more than one wavefront had.  A workgroup for each wavefront whose share begins
+// inside an item; those of one item divide its values among them, and a value's parts among lanes.  The workgroups
+// behind them check the sequences.
 template <int CACHE, int DP, int MT>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int32_t groups, int32_t max_blocks) {
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at, int32_t workers) {
   using S = Shape<CACHE, DP>;
   constexpr int kRows = 16 * MT;
-  constexpr int64_t kPart = kRows * (DP + 2);
-  __shared__ int s_bad;
-  const int64_t *units = static_cast<const int64_t *>(a.workspace);
-  const float *parts = reinterpret_cast<const float *>(static_cast<const char *>(a.workspace) + attend_layout_partial(a.B));
-  const int64_t share = share_of(units[a.B], groups);
-  const int tid = threadIdx.x, rr = tid >> 4, cc = tid & 15;
-  const int32_t per_seq = a.cache.heads * max_blocks;
-  for (int64_t item = blockIdx.x; item < int64_t(a.B) * per_seq; item += gridDim.x) {
-    const int32_t b = int32_t(item / per_seq), x = int32_t(item % per_seq), h = x / max_blocks, block = x % max_blocks;
-    const Seq s = sequence<S::kTile>(a, b, kRows);
-    if (x == 0) {
+  constexpr size_t kPart = kRows * (DP + 2);
+  const int tid = threadIdx.x;
+  if (int32_t(blockIdx.x) >= workers) {
+    __shared__ int s_bad;
+    for (int32_t b = int32_t(blockIdx.x) - workers; b < a.B; b += int32_t(gridDim.x) - workers) {
+      const Seq s = sequence<S::kTile>(a, b, kRows);
+      __syncthreads();
       if (tid == 0) s_bad = 0;
       __syncthreads();
       if (s.n > 0 && s.context > 0) {
@@ -631,42 +641,63 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int32_t groups,
       }
       __syncthreads();
       if (tid == 0) a.seq_err[b] = s.err | (s_bad ? DSDE_ERR_PAGES : 0u);
-      __syncthreads();
     }
-    if (block >= s.blocks) continue;
-    const int64_t from = units[b] + (int64_t(h) * s.blocks + block) * s.tiles, to = from + s.tiles;
-    const int64_t w0 = from / share, w1 = (to - 1) / share;
-    if (w0 == w1) continue;
-    const int32_t rows = s.n * a.group;
-    const float *start = parts + (2 * w0 + (from > w0 * share ? 1 : 0)) * kPart;
-    for (int32_t i = rr; i < kRows && block * kRows + i < rows; i += 16) {
-      float top = start[kRows * DP + i];
-      for (int64_t w = w0 + 1; w <= w1; ++w) top = fmaxf(top, parts[2 * w * kPart + kRows * DP + i]);
-      const float ref = top == -INFINITY ? 0.0f : top;
-      float sum = 0.0f;
-      f32x4 o[DP / 64];
-      for (int k = 0; k < DP / 64; ++k) o[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      for (int64_t w = w0; w <= w1; ++w) {
-        const float *p = w == w0 ? start : parts + 2 * w * kPart;
-        const float f = exp2_fast(p[kRows * DP + i] - ref);
-        sum += f * p[kRows * (DP + 1) + i];
-#pragma unroll
-        for (int k = 0; k < DP / 64; ++k) o[k] += f * *reinterpret_cast<const f32x4 *>(&p[i * DP + 64 * k + 4 * cc]);
-      }
-#pragma unroll
-      for (int k = 0; k < DP / 64; ++k)
-        finish<CACHE>(a, s, h, block * kRows + i, Joined{top, sum}, o[k], 64 * k + 4 * cc, k == 0 && cc == 0);
+    return;
+  }
+  const int32_t worker = blockIdx.x;
+  const Start x = reinterpret_cast<const Start *>(static_cast<const char *>(a.workspace) + at.starts)[worker];
+  if (x.tile == 0) return;
+  const Seq s = sequence<S::kTile>(a, x.b, kRows);
+  const int32_t rows = s.n * a.group, row0 = x.block * kRows, live = rows - row0 < kRows ? rows - row0 : kRows;
+  // cells of four values; at least four cells (64 bytes) for each workgroup
+  const int32_t cells = live * (DP / 4), parts = x.w1 - x.w0 + 1, sharers = parts - 1;
+  int32_t n = (cells + sharers - 1) / sharers;
+  n = n < 4 ? 4 : n;
+  const int32_t c0 = (worker - x.w0 - 1) * n, c1 = c0 + n < cells ? c0 + n : cells;
+  // lanes that share a cell's parts
+  int32_t span = 1;
+  while (span < 64 && span < parts && span * 2 * n <= 256) span *= 2;
+  const int32_t groups = 256 / span, lane = tid % span;
+  for (int32_t c = c0 + tid / span; c - tid / span < c1; c += groups) {  // all lanes stay for the shuffles
+    const bool mine = c < c1;
+    const int32_t i = (mine ? c : c0 < cells ? c0 : 0) / (DP / 4), d = (mine ? c : 0) % (DP / 4) * 4;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t k = lane; k < parts; k += span) {
+      const float *p = part_of(a, at.parts, x.w0 + k, k == 0 ? 1 : 0, kPart);
+      const float pm = p[kRows * DP + i], pl = p[kRows * (DP + 1) + i];
+      const f32x4 po = *reinterpret_cast<const f32x4 *>(p + i * DP + d);
+      const float now = fmaxf(m, pm), ref = now == -INFINITY ? 0.0f : now;
+      const float f0 = exp2_fast(m - ref), f1 = exp2_fast(pm - ref);
+      m = now;
+      l = l * f0 + pl * f1;
+      o = o * f0 + po * f1;
+    }
+    for (int32_t step = 1; step < span; step *= 2) {
+      const float pm = __shfl_xor(m, step), pl = __shfl_xor(l, step);
+      const f32x4 po{__shfl_xor(o.x, step), __shfl_xor(o.y, step), __shfl_xor(o.z, step), __shfl_xor(o.w, step)};
+      const float now = fmaxf(m, pm), ref = now == -INFINITY ? 0.0f : now;
+      const float f0 = exp2_fast(m - ref), f1 = exp2_fast(pm - ref);
+      m = now;
+      l = l * f0 + pl * f1;
+      o = o * f0 + po * f1;
+    }
+    if (mine && lane == 0) {
+      float f;
+      char *to = finished<CACHE>(a, s, x.h, row0 + i, m, l, d == 0, &f);
+      const float y[4] = {o.x * f, o.y * f, o.z * f, o.w * f};
+      if (d < a.cache.dim) store_row<CACHE, 4>(to, d, y);
     }
   }
 }
 
 template <int CACHE, int DP, int MT, int OCC>
 void launch(const AttendArgs &a, hipStream_t stream) {
-  const int32_t groups = 256 * OCC < kAttendGroups ? 256 * OCC : kAttendGroups;
-  attend_kernel<CACHE, DP, MT, OCC><<<groups, kAttendThreads, 0, stream>>>(a);
-  const int32_t max_blocks = (a.max_rows * a.group + 16 * MT - 1) / (16 * MT);
-  const int64_t items = int64_t(a.B) * a.cache.heads * max_blocks;
-  join_kernel<CACHE, DP, MT><<<uint32_t(items < 4096 ? items : 4096), 256, 0, stream>>>(a, groups, max_blocks);
+  const AttendLayout at = attend_layout(a.B, a.cache.dim);
+  const int32_t groups = 256 * OCC, workers = groups * kAttendWaves;
+  static_assert(256 * OCC * kAttendWaves * MT <= kAttendParts, "workspace");
+  attend_kernel<CACHE, DP, MT, OCC><<<groups, kAttendThreads, 0, stream>>>(a, at);
+  join_kernel<CACHE, DP, MT><<<workers + (a.B < 1024 ? a.B : 1024), 256, 0, stream>>>(a, at, workers);
 }
 template <int CACHE, int DP>
 void by_tiles(const AttendArgs &a, hipStream_t stream) {
