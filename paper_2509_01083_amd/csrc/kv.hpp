@@ -72,24 +72,18 @@ struct AttendArgs {
   uint32_t *seq_err;
   void *workspace;
 };
-// Row blocks (of 16 rows each) that one workgroup takes, and the bytes of its two partial results.
-inline int row_tiles(int32_t group, int32_t max_rows, int32_t dim) {
-  const int64_t m = int64_t(group) * max_rows;
-  const int most = dim > 128 ? 2 : 4;
-  return m <= 16 ? 1 : m <= 32 || most == 2 ? 2 : 4;
-}
-// Wavefronts of the largest launch times the row blocks of each.
-constexpr int kAttendParts = 4096;
+constexpr int kAttendWorkers = 1024;  // wavefronts of a launch
+constexpr int kAttendRows = 64;       // most rows that one of them takes at once
 inline int padded_dim(int32_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 struct AttendLayout {
   size_t starts, parts, total;
 };
-inline AttendLayout attend_layout(int32_t, int32_t dim) {
+inline AttendLayout attend_layout(int32_t dim) {
   AttendLayout l;
   l.starts = 0;  // where each wavefront's share begins
-  l.parts = align_up(size_t(24) * kAttendParts);
+  l.parts = align_up(size_t(24) * kAttendWorkers);
   // two parts of a wavefront: for each of its rows the values, a reference and a sum
-  l.total = l.parts + align_up(sizeof(float) * 2 * kAttendParts * 16 * size_t(padded_dim(dim) + 2));
+  l.total = l.parts + align_up(sizeof(float) * 2 * kAttendWorkers * kAttendRows * size_t(padded_dim(dim) + 2));
   return l;
 }
 int launch_kv_attention(const AttendArgs &a, hipStream_t stream);

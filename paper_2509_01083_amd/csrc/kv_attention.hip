@@ -42,7 +42,9 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 template <int CACHE, int DP>
 struct Shape {
   static constexpr int kElt = CACHE == DSDE_FP32 ? 4 : CACHE == DSDE_BF16 ? 2 : 1;
-  static constexpr int kSub = CACHE == DSDE_FP32 ? 1 : 2;      // subtiles of 16 keys
+  // subtiles of 16 keys: 16 KiB of keys and values at a time where registers allow
+  static constexpr int kLeastSub = CACHE == DSDE_FP32 ? 1 : 2;
+  static constexpr int kSub = 512 / (DP * kElt) < kLeastSub ? kLeastSub : 512 / (DP * kElt) > 4 ? 4 : 512 / (DP * kElt);
   static constexpr int kTile = 16 * kSub;                      // keys of a step
   static constexpr int kPer16 = 16 / kElt;                     // elements in 16 bytes
   static constexpr int kChunks = DP * kElt / 64;               // 16-byte chunks of a key per lane: chunk j at 16 (4 j + g)
@@ -51,7 +53,13 @@ struct Shape {
   static constexpr int kVecBytes = kVec * kElt;
   static constexpr int kVecWords = kVecBytes / 4;
   static constexpr int kKeys = 4 * kSub;                       // keys of a tile in a lane: 16 t + 4 g + i
-  static constexpr int kQWords = CACHE == DSDE_FP32 ? DP / 4 : DP / 8;  // words of a row's share in a lane
+  static constexpr int kQElt = CACHE == DSDE_FP32 ? 4 : 2;
+  static constexpr int kQChunks = DP * kQElt / 64;             // 16-byte chunks of a query row in a lane
+  // first dimension of a chunk: those that the keys' chunks hold
+  __device__ static __forceinline__ int32_t q_dim(int i, int g) {
+    if constexpr (CACHE == DSDE_E4M3) return (4 * (i / 2) + g) * 16 + 8 * (i % 2);
+    return (4 * i + g) * kPer16;
+  }
 };
 
 template <int WORDS>
@@ -63,18 +71,20 @@ using Buffer = __amdgpu_buffer_rsrc_t;
 __device__ __forceinline__ Buffer buffer(const char *base, int32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, bytes, 0x00020000);
 }
+// Cache hint (nt): keys and values are read once.  With it 2.1 GB go at 6.3 TB/s, without at 5.7.
+constexpr int kStream = 2;
 constexpr uint32_t kOutside = 0x40000000;  // an offset behind every buffer here
 template <int WORDS>
 __device__ __forceinline__ Words<WORDS> load_words(Buffer from, uint32_t off, uint32_t base = 0) {
   Words<WORDS> r;
   if constexpr (WORDS == 4) {
-    const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, off, base, 0));
+    const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, off, base, kStream));
     r.w[0] = x.x, r.w[1] = x.y, r.w[2] = x.z, r.w[3] = x.w;
   } else if constexpr (WORDS == 2) {
-    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, off, base, 0));
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from, off, base, kStream));
     r.w[0] = x.x, r.w[1] = x.y;
   } else {
-    r.w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, off, base, 0);
+    r.w[0] = __builtin_amdgcn_raw_buffer_load_b32(from, off, base, kStream);
   }
   return r;
 }
@@ -87,10 +97,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const bf16x2 p{__bf16(a), __bf16(b)};
   return __builtin_bit_cast(uint32_t, p);
 }
-__device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  const u32x4 x{a, b, c, d};
-  return __builtin_bit_cast(bf16x8, x);
-}
+__device__ __forceinline__ bf16x8 operand(const Words<4> &x) { return __builtin_bit_cast(bf16x8, x); }
 template <int CACHE>
 __device__ __forceinline__ bool not_finite(uint32_t x) {
   if constexpr (CACHE == DSDE_FP32) return (x & 0x7f800000u) == 0x7f800000u;
@@ -134,10 +141,6 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, int32_t b, int32_t 
 // lengths are, so that all end together; items that it has a part of leave that part to join_kernel.
 constexpr int32_t kStart = 4;
 constexpr int32_t kLeast = 4;  // units of a share at least: short calls do not end in joining many parts
-__device__ __forceinline__ int64_t share_of(int64_t all, int32_t workers) {
-  const int64_t n = (all + workers - 1) / workers;
-  return n > kLeast ? n : kLeast;
-}
 __device__ __forceinline__ int64_t units_of(const AttendArgs &a, const Seq &s) {
   return int64_t(s.tiles + kStart) * s.blocks * a.cache.heads;
 }
@@ -176,58 +179,63 @@ __device__ __forceinline__ char *finished(const AttendArgs &a, const Seq &s, int
   return a.out + t * a.out_token_stride + int64_t(head) * a.out_head_stride;
 }
 
-// The wavefront's view of its rows.
-template <int MT>
-struct Rows {
-  int32_t hi[MT], lo[MT];      // tokens that lane r's row of each block sees: lo .. hi
-  int32_t hi_all, lo_all;      // seen by every row
-  int32_t hi_any, lo_any;      // seen by any
+// One item of a wavefront's share: tiles first .. end - 1 of a sequence, key head and row block.
+struct Item {
+  int32_t b, h, block, first, end;
+  Seq s;
+};
+// A subtile's keys in memory; its values are as far from the values' start.
+struct At {
+  const char *keys;
+  int32_t bytes;  // 0: not to be read, loads give 0 without memory
+  bool bad;       // its page is none
 };
 
 template <int CACHE, int DP, int MT>
 struct Wave {
   using S = Shape<CACHE, DP>;
   const AttendArgs &a;
-  const Seq &s;
-  int lane, r, g;
-  const char *k_head, *v_head;  // of the head, from the cache's start
-  ConstInt table;               // of the sequence
-  float c;                      // scale log2(e), with the keys' scale, positive
-  uint32_t flip;                // sign bits of a word of queries, where the scale is negative
-  bool flat;                    // the scale is 0
-  int32_t mtiles;               // row tiles of this block that have rows
-  Rows<MT> rows;
+  int r, g;
   uint32_t k_off, v_off;
 
-  uint32_t q[MT][S::kQWords];
+  // of the item at hand
+  int32_t hi[MT], lo[MT];  // tokens that lane r's row of each block sees: lo .. hi
+  int32_t hi_all, lo_all;  // seen by every row
+  int32_t hi_any, lo_any;  // seen by any
+  float c;                 // scale log2(e), with the keys' scale, positive
+  Words<4> q[MT][S::kQChunks];
   f32x4 o[MT][S::kSets][S::kVec];
   float m[MT], l[MT];
-  // keys and values of a tile, and where its subtiles are bad
+  // the next item's rows, as they come from memory
+  Words<4> ahead[MT][S::kQChunks];
+  // keys and values of a tile
   Words<4> k[S::kSub][S::kChunks];
   Words<S::kVecWords> v[S::kKeys][S::kSets];
 
-  // A subtile's place in the cache.
-  struct At {
-    int64_t offset;
-    bool bad;    // its page is none
-    bool there;  // it is to be read
-  };
-  __device__ __forceinline__ At locate(int32_t tile, int t, bool wanted) const {
-    const int32_t key = tile * S::kTile + 16 * t;
-    const int32_t page = wanted && key < s.context ? table[key >> a.cache.shift] : 0;
-    At x;
-    x.bad = uint32_t(page) >= uint32_t(a.cache.pages);
-    x.there = wanted && !x.bad;
-    x.offset = (x.bad ? 0 : int64_t(page) * a.cache.page_stride) + int64_t(key & ((1 << a.cache.shift) - 1)) * a.cache.token_stride;
-    return x;
+  __device__ __forceinline__ explicit Wave(const AttendArgs &args, int lane) : a(args), r(lane & 15), g(lane >> 4) {
+    k_off = uint32_t(r * a.cache.token_stride + 16 * g);
+    v_off = uint32_t(4 * g * a.cache.token_stride + S::kVecBytes * r);
   }
-  // Bytes of a subtile's 16 rows; none of one that is not to be read, whose loads give 0 without memory.
-  __device__ __forceinline__ int32_t span(const At &x) const { return x.there ? 15 * a.cache.token_stride + a.cache.dim * S::kElt : 0; }
 
+  // Subtile t of a tile; nothing is read of those that no row sees.
+  __device__ __forceinline__ At locate(const Item &x, int32_t tile, int t, bool wanted) const {
+    const int32_t key = tile * S::kTile + 16 * t;
+    const int64_t oldest = int64_t(x.s.context) - x.s.n - a.window + 1;  // with a window, what the first row sees
+    wanted = wanted && key < x.s.context && (a.window == 0 || key + 15 >= oldest);
+    const int32_t page = wanted ? constant(a.table + int64_t(x.b) * a.width)[key >> a.cache.shift] : 0;
+    At y;
+    y.bad = uint32_t(page) >= uint32_t(a.cache.pages);
+    wanted = wanted && !y.bad;
+    y.keys = a.cache.k + (wanted ? int64_t(page) * a.cache.page_stride + int64_t(x.h) * a.cache.head_stride +
+                                       int64_t(key & ((1 << a.cache.shift) - 1)) * a.cache.token_stride
+                                 : 0);
+    y.bytes = wanted ? 15 * a.cache.token_stride + a.cache.dim * S::kElt : 0;
+    return y;
+  }
   __device__ __forceinline__ void load_k(const At (&at)[S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
-      const Buffer from = buffer(k_head + at[t].offset, span(at[t]));
+      const Buffer from = buffer(at[t].keys, at[t].bytes);
 #pragma unroll
       for (int j = 0; j < S::kChunks; ++j)  // 0 behind the row's end
         k[t][j] = load_words<4>(from, (4 * j + g) * S::kPer16 < a.cache.dim ? k_off + 64 * j : kOutside);
@@ -236,7 +244,7 @@ struct Wave {
   __device__ __forceinline__ void load_v(const At (&at)[S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
-      const Buffer from = buffer(v_head + at[t].offset, span(at[t]));
+      const Buffer from = buffer(at[t].keys + (a.cache.v - a.cache.k), at[t].bytes);
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e) {
         const uint32_t off = (16 * e + r) * S::kVec < a.cache.dim ? v_off + 16 * S::kVecBytes * e : kOutside;
@@ -245,31 +253,50 @@ struct Wave {
       }
     }
   }
-
-  __device__ __forceinline__ void load_q(const char *base, int32_t row, int32_t count, int mt) {
-    // lane r's row; rows behind the last are zero
-    const bool live = row < count;
-    const int32_t j = live ? row / a.group : 0, head = live ? row - j * a.group : 0;
-    const char *p = base + j * a.q.token_stride + head * a.q.head_stride;
-    constexpr int kQElt = CACHE == DSDE_FP32 ? 4 : 2;
+  // An item's rows; for rows and dimensions that are none, others that are, which begin() drops.
+  __device__ __forceinline__ void load_q(const Item &x) {
+    const char *base = a.q.data + x.s.row0 * a.q.token_stride + int64_t(x.h) * a.group * a.q.head_stride;
 #pragma unroll
-    for (int i = 0; i < S::kQWords / 4; ++i) {
-      // the dimensions that the keys' chunks hold
-      int32_t d;
-      if constexpr (CACHE == DSDE_E4M3)
-        d = (4 * (i / 2) + g) * 16 + 8 * (i % 2);
-      else
-        d = (4 * i + g) * S::kPer16;
-      Words<4> x{};
-      if (live && d < a.cache.dim) {
-        const u32x4 y = *reinterpret_cast<const u32x4 *>(p + d * kQElt);
-        if (!flat) x = Words<4>{{y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip}};
+    for (int mt = 0; mt < MT; ++mt) {
+      const int32_t row = (x.block * MT + mt) * 16 + r, at = row < x.s.n * a.group ? row : 0, j = at / a.group;
+      const char *p = base + j * a.q.token_stride + (at - j * a.group) * a.q.head_stride;
+#pragma unroll
+      for (int i = 0; i < S::kQChunks; ++i) {
+        const int32_t d = S::q_dim(i, g);
+        const u32x4 y = *reinterpret_cast<const u32x4 *>(p + (d < a.cache.dim ? d : 0) * S::kQElt);
+        ahead[mt][i] = Words<4>{{y.x, y.y, y.z, y.w}};
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) q[mt][4 * i + e] = x.w[e];
     }
-    rows.hi[mt] = live ? s.context - s.n + j : -1;
-    rows.lo[mt] = a.window > 0 && rows.hi[mt] >= a.window ? rows.hi[mt] - a.window + 1 : 0;
+  }
+  // Takes up an item whose rows are ahead.
+  __device__ __forceinline__ void begin(const Item &x) {
+    const float f = a.scale * kLog2e * (CACHE == DSDE_E4M3 ? a.cache.k_scale[x.h] : 1.0f);
+    // a negative scale turns the queries' signs, one of 0 makes them 0
+    const bool flat = fabsf(f) < 0x1p-126f;
+    const uint32_t flip = f < 0.0f ? (CACHE == DSDE_FP32 ? 0x80000000u : 0x80008000u) : 0u;
+    c = flat ? 1.0f : fabsf(f);
+    const int32_t newest = x.s.context - 1, oldest = x.s.context - x.s.n;
+    hi_all = oldest, hi_any = newest;
+    lo_all = a.window > 0 && newest >= a.window ? newest - a.window + 1 : 0;
+    lo_any = a.window > 0 && oldest >= a.window ? oldest - a.window + 1 : 0;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int32_t row = (x.block * MT + mt) * 16 + r;
+      const bool live = row < x.s.n * a.group;
+      hi[mt] = live ? oldest + row / a.group : -1;
+      lo[mt] = a.window > 0 && hi[mt] >= a.window ? hi[mt] - a.window + 1 : 0;
+#pragma unroll
+      for (int i = 0; i < S::kQChunks; ++i) {
+        const bool there = live && !flat && S::q_dim(i, g) < a.cache.dim;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[mt][i].w[e] = there ? ahead[mt][i].w[e] ^ flip : 0u;
+      }
+      m[mt] = -INFINITY, l[mt] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+        for (int j = 0; j < S::kVec; ++j) o[mt][e][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
   }
 
   // Scores of a tile, without their scale.
@@ -286,24 +313,17 @@ struct Wave {
           for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-              x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), __uint_as_float(q[mt][4 * j + e]), x[mt][t], 0, 0, 0);
+              x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), __uint_as_float(q[mt][j].w[e]), x[mt][t], 0, 0, 0);
         } else if constexpr (CACHE == DSDE_BF16) {
-          const bf16x8 kk = operand(w.w[0], w.w[1], w.w[2], w.w[3]);
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            const uint32_t *p = &q[mt][4 * j];
-            x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(p[0], p[1], p[2], p[3]), x[mt][t], 0, 0, 0);
-          }
+          for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(w), operand(q[mt][j]), x[mt][t], 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const bf16x8 kk = operand(widen<false>(w.w[2 * e]), widen<true>(w.w[2 * e]), widen<false>(w.w[2 * e + 1]),
-                                      widen<true>(w.w[2 * e + 1]));
+            const bf16x8 kk = operand(Words<4>{{widen<false>(w.w[2 * e]), widen<true>(w.w[2 * e]), widen<false>(w.w[2 * e + 1]),
+                                                widen<true>(w.w[2 * e + 1])}});
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              const uint32_t *p = &q[mt][8 * j + 4 * e];
-              x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(p[0], p[1], p[2], p[3]), x[mt][t], 0, 0, 0);
-            }
+            for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(q[mt][2 * j + e]), x[mt][t], 0, 0, 0);
           }
         }
       }
@@ -349,48 +369,51 @@ struct Wave {
   // ONLY: to the rows of token `token` alone (a weight of 0 would not keep a NaN from the others).
   template <bool ONLY = false>
   __device__ __forceinline__ void add(const f32x4 (&p)[MT][S::kSub], int32_t token = 0) {
-    const auto put = [&](int mt, int e, int j, f32x4 x) { o[mt][e][j] = !ONLY || rows.hi[mt] == token ? x : o[mt][e][j]; };
+    const auto put = [&](int mt, int e, int j, f32x4 x) { o[mt][e][j] = !ONLY || hi[mt] == token ? x : o[mt][e][j]; };
     if constexpr (CACHE == DSDE_FP32) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < S::kKeys; ++i)
 #pragma unroll
         for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-              put(mt, e, j, __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e].w[j]), p[mt][0][i], o[mt][e][j], 0, 0, 0));
+              put(mt, e, j, __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e].w[j]), p[mt][i / 4][i % 4], o[mt][e][j], 0, 0, 0));
     } else {
-      bf16x8 w[MT];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        w[mt] = operand(pack_bf16(p[mt][0].x, p[mt][0].y), pack_bf16(p[mt][0].z, p[mt][0].w),
-                        pack_bf16(p[mt][1].x, p[mt][1].y), pack_bf16(p[mt][1].z, p[mt][1].w));
+      for (int t = 0; t < S::kSub; t += 2) {
+        bf16x8 w[MT];
 #pragma unroll
-      for (int e = 0; e < S::kSets; ++e)
+        for (int mt = 0; mt < MT; ++mt)
+          w[mt] = operand(Words<4>{{pack_bf16(p[mt][t].x, p[mt][t].y), pack_bf16(p[mt][t].z, p[mt][t].w),
+                                    pack_bf16(p[mt][t + 1].x, p[mt][t + 1].y), pack_bf16(p[mt][t + 1].z, p[mt][t + 1].w)}});
 #pragma unroll
-        for (int j2 = 0; j2 < S::kVec / 2; ++j2) {  // two dimensions from one word of each key
-          uint32_t x[8];
+        for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if constexpr (CACHE == DSDE_BF16)
-              x[i] = v[i][e].w[j2];
-            else
-              x[i] = j2 & 1 ? widen<true>(v[i][e].w[j2 / 2]) : widen<false>(v[i][e].w[j2 / 2]);
+          for (int j2 = 0; j2 < S::kVec / 2; ++j2) {  // two dimensions from one word of each key
+            uint32_t x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const Words<S::kVecWords> &y = v[4 * t + i][e];
+              if constexpr (CACHE == DSDE_BF16)
+                x[i] = y.w[j2];
+              else
+                x[i] = j2 & 1 ? widen<true>(y.w[j2 / 2]) : widen<false>(y.w[j2 / 2]);
+            }
+            Words<4> even, odd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              even.w[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+              odd.w[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              put(mt, e, 2 * j2, __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(even), w[mt], o[mt][e][2 * j2], 0, 0, 0));
+              put(mt, e, 2 * j2 + 1, __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(odd), w[mt], o[mt][e][2 * j2 + 1], 0, 0, 0));
+            }
           }
-          uint32_t lo[4], hi[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            lo[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
-            hi[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
-          }
-          const bf16x8 a0 = operand(lo[0], lo[1], lo[2], lo[3]), a1 = operand(hi[0], hi[1], hi[2], hi[3]);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            put(mt, e, 2 * j2, __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w[mt], o[mt][e][2 * j2], 0, 0, 0));
-            put(mt, e, 2 * j2 + 1, __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w[mt], o[mt][e][2 * j2 + 1], 0, 0, 0));
-          }
-        }
+      }
     }
   }
 
@@ -402,15 +425,16 @@ struct Wave {
       for (int i = 0; i < 4; ++i) {
         const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= rows.lo[mt] && key <= rows.hi[mt] ? x[mt][t][i] : -INFINITY;
+        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= lo[mt] && key <= hi[mt] ? x[mt][t][i] : -INFINITY;
       }
   }
-  __device__ __forceinline__ bool keep(int32_t tile, int32_t lo, int32_t hi) {
+  // Keeps the values of tokens from .. to, 0 for others; whether one of them is not finite.
+  __device__ __forceinline__ bool keep(int32_t tile, int32_t from, int32_t to) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < S::kKeys; ++i) {
       const int32_t key = tile * S::kTile + 16 * (i / 4) + 4 * g + i % 4;
-      const bool seen = key >= lo && key <= hi;
+      const bool seen = key >= from && key <= to;
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
@@ -425,8 +449,8 @@ struct Wave {
   // one that some rows see is not finite (rare), the tile's values are read again for each of the sequence's tokens,
   // which adds what it sees, and then all become 0.
   __device__ __forceinline__ void mask_values(const f32x4 (&p)[MT][S::kSub], int32_t tile, const At (&from)[S::kSub], const At (&next)[S::kSub]) {
-    if (!keep(tile, rows.lo_any, rows.hi_any)) return;
-    for (int32_t token = s.context - s.n; token < s.context; ++token) {
+    if (!keep(tile, lo_any, hi_any)) return;
+    for (int32_t token = hi_all; token <= hi_any; ++token) {
       load_v(from);
       keep(tile, a.window > 0 && token >= a.window ? token - a.window + 1 : 0, token);
       add<true>(p, token);
@@ -435,43 +459,59 @@ struct Wave {
     load_k(next);  // again: this path has had their registers
   }
 
-  // Tiles first .. end - 1.
-  __device__ __forceinline__ void run(int32_t first, int32_t end) {
-    At at[S::kSub], next[S::kSub];
+  // The item's rows, or its part of them.
+  __device__ __forceinline__ void end(const Item &x, float *part) {
+    constexpr int kRows = 16 * MT;
+    const bool done = x.end - x.first == x.s.tiles;
 #pragma unroll
-    for (int t = 0; t < S::kSub; ++t) at[t] = locate(first, t, true);
-    load_k(at);
-    load_v(at);
-    // The next tile's keys are on their way while this one's values are weighed, and its values while the next scores
-    // are taken, into registers that have just been read; a tile behind the last is none.  No load stands behind a
-    // branch: waits could not be counted then.
-    for (int32_t tile = first; tile < end; ++tile) {
+    for (int mt = 0; mt < MT; ++mt) {
+      const int32_t row = x.block * kRows + 16 * mt + r;
+      float sum = l[mt];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (x.s.err) sum = NAN;  // a context that is none
+      if (row < x.s.n * a.group) {
+        float f = 1.0f;
+        char *to = nullptr;
+        if (done) to = finished<CACHE>(a, x.s, x.h, row, m[mt], sum, g == 0, &f);
 #pragma unroll
-      for (int t = 0; t < S::kSub; ++t) next[t] = locate(tile + 1, t, tile + 1 < end);
-      f32x4 x[MT][S::kSub];
-      scores(x);
-      load_k(next);
-      const bool clear = tile * S::kTile >= rows.lo_all && tile * S::kTile + S::kTile - 1 <= rows.hi_all;
-      if (!clear) mask(x, tile);
-      weigh(x, at);
-      if (!clear) mask_values(x, tile, at, next);
-      add(x);
-      load_v(next);
+        for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
-      for (int t = 0; t < S::kSub; ++t) at[t] = next[t];
+          for (int i = 0; i < 4; ++i) {
+            const int32_t d = (16 * e + 4 * g + i) * S::kVec;
+            float y[S::kVec];
+#pragma unroll
+            for (int j = 0; j < S::kVec; ++j) y[j] = o[mt][e][j][i] * f;
+            if (done) {
+              if (d < a.cache.dim) store_row<CACHE, S::kVec>(to, d, y);
+            } else {
+#pragma unroll
+              for (int j = 0; j < S::kVec; j += 4)
+                *reinterpret_cast<f32x4 *>(part + (16 * mt + r) * DP + d + j) = f32x4{y[j], y[j + 1], y[j + 2], y[j + 3]};
+            }
+          }
+        if (!done && g == 0) {
+          part[kRows * DP + 16 * mt + r] = m[mt];
+          part[kRows * (DP + 1) + 16 * mt + r] = sum;
+        }
+      }
     }
   }
 };
 
-template <int CACHE, int DP, int MT, int OCC>
-__global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs a, AttendLayout at) {
+// Quotients of the work's line, in 32 bits where it is that short (64 take ten times the instructions).
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y, bool small) {
+  return small ? int64_t(uint32_t(x) / uint32_t(y)) : x / y;
+}
+
+template <int CACHE, int DP, int MT>
+__global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a, AttendLayout at) {
   using S = Shape<CACHE, DP>;
   constexpr int kRows = 16 * MT;
   constexpr size_t kPart = kRows * (DP + 2);
   struct Begin {
     Start at;
-    int64_t tile0_unit;  // of the item's first tile
-    int32_t used;        // units of its start that lie before the share
+    int32_t used;  // units of its item's start that lie before the share
     Seq s;
   };
   __shared__ int64_t s_sum[kAttendWaves];
@@ -497,7 +537,9 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs 
     all += s_sum[i];
   }
   const int32_t workers = int32_t(gridDim.x) * kAttendWaves;
-  const int64_t share = share_of(all, workers);
+  const bool small = all + workers < (int64_t(1) << 31);
+  int64_t share = quotient(all + workers - 1, workers, small);
+  if (share < kLeast) share = kLeast;
   for (int i = 0; i < kAttendWaves; ++i) {
     const int64_t begin = (int64_t(i) * gridDim.x + blockIdx.x) * share;
     int64_t before = upto - own;
@@ -507,11 +549,11 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs 
       const int64_t n = units_of(a, s);
       if (begin < before + n) {
         const int64_t x = begin - before;
-        const int32_t size = s.tiles + kStart, item = int32_t(x / size), u = int32_t(x - int64_t(item) * size);
-        const int64_t unit = before + int64_t(item) * size + kStart;
+        const int32_t size = s.tiles + kStart, item = int32_t(quotient(x, size, small)), u = int32_t(x - int64_t(item) * size);
+        const int64_t unit = before + int64_t(item) * size + kStart;  // of the item's first tile
         const int32_t h = item / s.blocks;
-        s_begin[i] = Begin{Start{b, h, item - h * s.blocks, u > kStart ? u - kStart : 0, int32_t(unit / share),
-                                 int32_t((unit + s.tiles - 1) / share)}, unit, u < kStart ? u : kStart, s};
+        s_begin[i] = Begin{Start{b, h, item - h * s.blocks, u > kStart ? u - kStart : 0, int32_t(quotient(unit, share, small)),
+                                 int32_t(quotient(unit + s.tiles - 1, share, small))}, u < kStart ? u : kStart, s};
         break;
       }
       before += n;
@@ -525,94 +567,72 @@ __global__ __launch_bounds__(kAttendThreads, OCC) void attend_kernel(AttendArgs 
     if (lane == 0) starts[worker].tile = 0;
     return;
   }
-  Start x = s_begin[wave].at;
-  if (lane == 0) starts[worker] = x;
-  x.b = uniform(x.b), x.h = uniform(x.h), x.block = uniform(x.block), x.tile = uniform(x.tile);
-  Seq s = s_begin[wave].s;
-  s.row0 = uniform(s.row0), s.n = uniform(s.n), s.context = uniform(s.context), s.tile0 = uniform(s.tile0);
-  s.tiles = uniform(s.tiles), s.blocks = uniform(s.blocks), s.err = uint32_t(uniform(int(s.err)));
-  int64_t left = end - begin - (kStart - uniform(s_begin[wave].used));
+  const Begin &from = s_begin[wave];
+  if (lane == 0) starts[worker] = from.at;
+  int64_t left = end - begin - (kStart - uniform(from.used));
+  if (left <= 0) return;  // the end of an item's start alone
 
-  while (left > 0) {
-    const int32_t count = int32_t(left < s.tiles - x.tile ? left : s.tiles - x.tile);
-    const int32_t rows = s.n * a.group, row0 = x.block * kRows;
+  Item x{uniform(from.at.b), uniform(from.at.h), uniform(from.at.block), 0, 0,
+         Seq{uniform(from.s.row0), uniform(from.s.n), uniform(from.s.context), uniform(from.s.tile0), uniform(from.s.tiles),
+             uniform(from.s.blocks), uint32_t(uniform(int(from.s.err)))}};
+  int32_t tile = uniform(from.at.tile);  // of the sequence's tiles; above 0 in the first item alone
+  const auto take = [&](Item &y, int32_t tile) {
+    y.first = y.s.tile0 + tile;
+    y.end = y.first + int32_t(left < y.s.tiles - tile ? left : y.s.tiles - tile);
+    left -= y.end - y.first + kStart;
+  };
+  take(x, tile);
 
-    Wave<CACHE, DP, MT> w{a, s};
-    w.lane = lane, w.r = lane & 15, w.g = lane >> 4;
-    w.k_head = a.cache.k + x.h * a.cache.head_stride;
-    w.v_head = a.cache.v + x.h * a.cache.head_stride;
-    w.table = constant(a.table + int64_t(x.b) * a.width);
-    const float c = a.scale * kLog2e * (CACHE == DSDE_E4M3 ? a.cache.k_scale[x.h] : 1.0f);
-    w.flat = fabsf(c) < 0x1p-126f;
-    w.c = w.flat ? 1.0f : fabsf(c);
-    w.flip = c < 0.0f ? (CACHE == DSDE_FP32 ? 0x80000000u : 0x80008000u) : 0u;
-    w.k_off = uint32_t(w.r * a.cache.token_stride + 16 * w.g);
-    w.v_off = uint32_t(4 * w.g * a.cache.token_stride + S::kVecBytes * w.r);
-    const char *q = a.q.data + s.row0 * a.q.token_stride + int64_t(x.h) * a.group * a.q.head_stride;
+  Wave<CACHE, DP, MT> w(a, lane);
+  At now[S::kSub], next[S::kSub];
+  w.load_q(x);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      w.load_q(q, row0 + 16 * mt + w.r, rows, mt);
-      w.m[mt] = -INFINITY, w.l[mt] = 0.0f;
-#pragma unroll
-      for (int e = 0; e < S::kSets; ++e)
-#pragma unroll
-        for (int j = 0; j < S::kVec; ++j) w.o[mt][e][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    const int32_t newest = s.context - 1, oldest = s.context - s.n;
-    w.rows.hi_all = oldest, w.rows.hi_any = newest;
-    w.rows.lo_all = a.window > 0 && newest >= a.window ? newest - a.window + 1 : 0;
-    w.rows.lo_any = a.window > 0 && oldest >= a.window ? oldest - a.window + 1 : 0;
-    w.run(s.tile0 + x.tile, s.tile0 + x.tile + count);
-
-    const bool done = count == s.tiles;
-    float *part = part_of(a, at.parts, worker, x.tile > 0 ? 0 : 1, kPart);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int32_t row = row0 + 16 * mt + w.r;
-      float l = w.l[mt];
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
-      if (s.err) l = NAN;  // a context that is none
-      if (row < rows) {
-        float f = 1.0f;
-        char *to = nullptr;
-        if (done) to = finished<CACHE>(a, s, x.h, row, w.m[mt], l, w.g == 0, &f);
-#pragma unroll
-        for (int e = 0; e < S::kSets; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int32_t d = (16 * e + 4 * w.g + i) * S::kVec;
-            float y[S::kVec];
-#pragma unroll
-            for (int j = 0; j < S::kVec; ++j) y[j] = w.o[mt][e][j][i] * f;
-            if (done) {
-              if (d < a.cache.dim) store_row<CACHE, S::kVec>(to, d, y);
-            } else {
-#pragma unroll
-              for (int j = 0; j < S::kVec; j += 4)
-                *reinterpret_cast<f32x4 *>(part + (16 * mt + w.r) * DP + d + j) = f32x4{y[j], y[j + 1], y[j + 2], y[j + 3]};
-            }
-          }
-        if (!done && w.g == 0) {
-          part[kRows * DP + 16 * mt + w.r] = w.m[mt];
-          part[kRows * (DP + 1) + 16 * mt + w.r] = l;
-        }
-      }
-    }
-
-    left -= count + kStart;
-    x.tile = 0;
-    if (left <= 0) break;
-    if (++x.block == s.blocks) {
-      x.block = 0;
-      if (++x.h == a.cache.heads) {
-        x.h = 0;
+  for (int t = 0; t < S::kSub; ++t) now[t] = w.locate(x, x.first, t, true);
+  w.load_k(now);
+  w.load_v(now);
+  for (;;) {
+    // what comes behind this item
+    Item y = x;
+    bool more = left > 0;
+    if (more && ++y.block == y.s.blocks) {
+      y.block = 0;
+      if (++y.h == a.cache.heads) {
+        y.h = 0;
         do {
-          if (++x.b >= a.B) return;
-          s = sequence<S::kTile>(a, x.b, kRows);
-        } while (s.blocks == 0);
+          if (++y.b >= a.B) {
+            more = false;
+            break;
+          }
+          y.s = sequence<S::kTile>(a, y.b, kRows);
+        } while (y.s.blocks == 0);
       }
     }
+    if (more) take(y, 0);
+    else y = x;
+    w.begin(x);
+    w.load_q(y);
+    // The next tile's keys are on their way while this one's values are weighed, and its values while the next scores
+    // are taken, into registers that have just been read; behind an item's last tile comes the next item's first.  No
+    // load stands behind a branch: waits could not be counted then.  A tile behind the last of all is none.
+    for (int32_t tile = x.first; tile < x.end; ++tile) {
+      const bool last = tile + 1 == x.end;
+#pragma unroll
+      for (int t = 0; t < S::kSub; ++t) next[t] = w.locate(last ? y : x, last ? y.first : tile + 1, t, !last || more);
+      f32x4 p[MT][S::kSub];
+      w.scores(p);
+      w.load_k(next);
+      const bool clear = tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
+      if (!clear) w.mask(p, tile);
+      w.weigh(p, now);
+      if (!clear) w.mask_values(p, tile, now, next);
+      w.add(p);
+      w.load_v(next);
+#pragma unroll
+      for (int t = 0; t < S::kSub; ++t) now[t] = next[t];
+    }
+    w.end(x, part_of(a, at.parts, worker, x.first > x.s.tile0 ? 0 : 1, kPart));
+    if (!more) return;
+    x = y;
   }
 }
 
@@ -649,10 +669,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
   if (x.tile == 0) return;
   const Seq s = sequence<S::kTile>(a, x.b, kRows);
   const int32_t rows = s.n * a.group, row0 = x.block * kRows, live = rows - row0 < kRows ? rows - row0 : kRows;
-  // cells of four values; at least four cells (64 bytes) for each workgroup
+  // cells of four values; at least 16 cells (256 bytes) for each workgroup
   const int32_t cells = live * (DP / 4), parts = x.w1 - x.w0 + 1, sharers = parts - 1;
   int32_t n = (cells + sharers - 1) / sharers;
-  n = n < 4 ? 4 : n;
+  n = n < 16 ? 16 : n;
   const int32_t c0 = (worker - x.w0 - 1) * n, c1 = c0 + n < cells ? c0 + n : cells;
   // lanes that share a cell's parts
   int32_t span = 1;
@@ -663,6 +683,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
     const int32_t i = (mine ? c : c0 < cells ? c0 : 0) / (DP / 4), d = (mine ? c : 0) % (DP / 4) * 4;
     float m = -INFINITY, l = 0.0f;
     f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int32_t k = lane; k < parts; k += span) {
       const float *p = part_of(a, at.parts, x.w0 + k, k == 0 ? 1 : 0, kPart);
       const float pm = p[kRows * DP + i], pl = p[kRows * (DP + 1) + i];
@@ -691,24 +712,27 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
   }
 }
 
-template <int CACHE, int DP, int MT, int OCC>
+// One workgroup per CU, a wavefront per SIMD: 64 KiB of loads in flight on each CU.  With two workgroups the same
+// 2.1 GB took 340 us instead of 330, with three 373.
+template <int CACHE, int DP, int MT>
 void launch(const AttendArgs &a, hipStream_t stream) {
-  const AttendLayout at = attend_layout(a.B, a.cache.dim);
-  const int32_t groups = 256 * OCC, workers = groups * kAttendWaves;
-  static_assert(256 * OCC * kAttendWaves * MT <= kAttendParts, "workspace");
-  attend_kernel<CACHE, DP, MT, OCC><<<groups, kAttendThreads, 0, stream>>>(a, at);
+  const AttendLayout at = attend_layout(a.cache.dim);
+  constexpr int32_t groups = 256, workers = groups * kAttendWaves;
+  static_assert(workers <= kAttendWorkers, "workspace");
+  attend_kernel<CACHE, DP, MT><<<groups, kAttendThreads, 0, stream>>>(a, at);
   join_kernel<CACHE, DP, MT><<<workers + (a.B < 1024 ? a.B : 1024), 256, 0, stream>>>(a, at, workers);
 }
 template <int CACHE, int DP>
 void by_tiles(const AttendArgs &a, hipStream_t stream) {
-  const int tiles = row_tiles(a.group, a.max_rows, a.cache.dim);
-  // workgroups per CU by the registers that each form takes
-  if (tiles == 1)
-    launch<CACHE, DP, 1, DP == 256 || (CACHE == DSDE_FP32 && DP == 128) ? 1 : 2>(a, stream);
-  else if (tiles == 2)
-    launch<CACHE, DP, 2, DP == 256 || CACHE == DSDE_FP32 ? 1 : 2>(a, stream);
-  else if constexpr (DP <= 128)
-    launch<CACHE, DP, 4, 1>(a, stream);
+  // as many row blocks as fit the registers
+  constexpr int most = DP == 256 ? (CACHE == DSDE_FP32 ? 1 : 2) : CACHE == DSDE_FP32 && DP == 128 ? 2 : 4;
+  const int32_t rows = a.group * a.max_rows;
+  if (rows <= 16 || most == 1)
+    launch<CACHE, DP, 1>(a, stream);
+  else if (rows <= 32 || most == 2)
+    launch<CACHE, DP, most < 2 ? 1 : 2>(a, stream);
+  else
+    launch<CACHE, DP, most < 4 ? 1 : 4>(a, stream);
 }
 template <int CACHE>
 void by_dim(const AttendArgs &a, hipStream_t stream) {
