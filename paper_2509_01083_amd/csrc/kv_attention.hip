@@ -206,8 +206,6 @@ struct Wave {
   Words<4> q[MT][S::kQChunks];
   f32x4 o[MT][S::kSets][S::kVec];
   float m[MT], l[MT];
-  // the next item's rows, as they come from memory
-  Words<4> ahead[MT][S::kQChunks];
   // keys and values of a tile
   Words<4> k[S::kSub][S::kChunks];
   Words<S::kVecWords> v[S::kKeys][S::kSets];
@@ -254,7 +252,7 @@ struct Wave {
     }
   }
   // An item's rows; for rows and dimensions that are none, others that are, which begin() drops.
-  __device__ __forceinline__ void load_q(const Item &x) {
+  __device__ __forceinline__ void load_q(const Item &x, Words<4> (&ahead)[MT][S::kQChunks]) const {
     const char *base = a.q.data + x.s.row0 * a.q.token_stride + int64_t(x.h) * a.group * a.q.head_stride;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -268,8 +266,8 @@ struct Wave {
       }
     }
   }
-  // Takes up an item whose rows are ahead.
-  __device__ __forceinline__ void begin(const Item &x) {
+  // Takes up an item whose rows are loaded.
+  __device__ __forceinline__ void begin(const Item &x, const Words<4> (&ahead)[MT][S::kQChunks]) {
     const float f = a.scale * kLog2e * (CACHE == DSDE_E4M3 ? a.cache.k_scale[x.h] : 1.0f);
     // a negative scale turns the queries' signs, one of 0 makes them 0
     const bool flat = fabsf(f) < 0x1p-126f;
@@ -509,6 +507,8 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
   using S = Shape<CACHE, DP>;
   constexpr int kRows = 16 * MT;
   constexpr size_t kPart = kRows * (DP + 2);
+  // the next item's rows are fetched early where registers allow
+  constexpr bool kAhead = MT * DP * S::kQElt <= 512;
   struct Begin {
     Start at;
     int32_t used;  // units of its item's start that lie before the share
@@ -585,7 +585,8 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
 
   Wave<CACHE, DP, MT> w(a, lane);
   At now[S::kSub], next[S::kSub];
-  w.load_q(x);
+  Words<4> ahead[MT][S::kQChunks];
+  w.load_q(x, ahead);
 #pragma unroll
   for (int t = 0; t < S::kSub; ++t) now[t] = w.locate(x, x.first, t, true);
   w.load_k(now);
@@ -609,8 +610,8 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
     }
     if (more) take(y, 0);
     else y = x;
-    w.begin(x);
-    w.load_q(y);
+    w.begin(x, ahead);
+    if (kAhead) w.load_q(y, ahead);
     // The next tile's keys are on their way while this one's values are weighed, and its values while the next scores
     // are taken, into registers that have just been read; behind an item's last tile comes the next item's first.  No
     // load stands behind a branch: waits could not be counted then.  A tile behind the last of all is none.
@@ -633,6 +634,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
     w.end(x, part_of(a, at.parts, worker, x.first > x.s.tile0 ? 0 : 1, kPart));
     if (!more) return;
     x = y;
+    if (!kAhead) w.load_q(x, ahead);
   }
 }
 
@@ -731,6 +733,8 @@ void by_tiles(const AttendArgs &a, hipStream_t stream) {
     launch<CACHE, DP, 1>(a, stream);
   else if (rows <= 32 || most == 2)
     launch<CACHE, DP, most < 2 ? 1 : 2>(a, stream);
+  else if (rows <= 48)
+    launch<CACHE, DP, most < 4 ? 1 : 3>(a, stream);
   else
     launch<CACHE, DP, most < 4 ? 1 : 4>(a, stream);
 }
