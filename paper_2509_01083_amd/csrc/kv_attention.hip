@@ -266,13 +266,25 @@ struct Wave {
       }
     }
   }
-  // Takes up an item whose rows are loaded.
-  __device__ __forceinline__ void begin(const Item &x, const Words<4> (&ahead)[MT][S::kQChunks]) {
+  // Takes over an item's loaded rows.  A negative scale turns their signs, one of 0 makes them 0.
+  __device__ __forceinline__ void take_q(const Item &x, const Words<4> (&ahead)[MT][S::kQChunks]) {
     const float f = a.scale * kLog2e * (CACHE == DSDE_E4M3 ? a.cache.k_scale[x.h] : 1.0f);
-    // a negative scale turns the queries' signs, one of 0 makes them 0
     const bool flat = fabsf(f) < 0x1p-126f;
     const uint32_t flip = f < 0.0f ? (CACHE == DSDE_FP32 ? 0x80000000u : 0x80008000u) : 0u;
     c = flat ? 1.0f : fabsf(f);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const bool live = (x.block * MT + mt) * 16 + r < x.s.n * a.group;
+#pragma unroll
+      for (int i = 0; i < S::kQChunks; ++i) {
+        const bool there = live && !flat && S::q_dim(i, g) < a.cache.dim;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[mt][i].w[e] = there ? ahead[mt][i].w[e] ^ flip : 0u;
+      }
+    }
+  }
+  // What an item's rows see, and empty accumulators.
+  __device__ __forceinline__ void begin(const Item &x) {
     const int32_t newest = x.s.context - 1, oldest = x.s.context - x.s.n;
     hi_all = oldest, hi_any = newest;
     lo_all = a.window > 0 && newest >= a.window ? newest - a.window + 1 : 0;
@@ -280,15 +292,8 @@ struct Wave {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int32_t row = (x.block * MT + mt) * 16 + r;
-      const bool live = row < x.s.n * a.group;
-      hi[mt] = live ? oldest + row / a.group : -1;
+      hi[mt] = row < x.s.n * a.group ? oldest + row / a.group : -1;
       lo[mt] = a.window > 0 && hi[mt] >= a.window ? hi[mt] - a.window + 1 : 0;
-#pragma unroll
-      for (int i = 0; i < S::kQChunks; ++i) {
-        const bool there = live && !flat && S::q_dim(i, g) < a.cache.dim;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[mt][i].w[e] = there ? ahead[mt][i].w[e] ^ flip : 0u;
-      }
       m[mt] = -INFINITY, l[mt] = 0.0f;
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e)
@@ -590,7 +595,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
 #pragma unroll
   for (int t = 0; t < S::kSub; ++t) now[t] = w.locate(x, x.first, t, true);
   w.load_k(now);
-  w.load_v(now);
+  w.take_q(x, ahead);
   for (;;) {
     // what comes behind this item
     Item y = x;
@@ -608,14 +613,19 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
         } while (y.s.blocks == 0);
       }
     }
-    if (more) take(y, 0);
-    else y = x;
-    w.begin(x, ahead);
+    if (more)
+      take(y, 0);
+    else
+      y = x;
+    w.begin(x);
     if (kAhead) w.load_q(y, ahead);
-    // The next tile's keys are on their way while this one's values are weighed, and its values while the next scores
-    // are taken, into registers that have just been read; behind an item's last tile comes the next item's first.  No
-    // load stands behind a branch: waits could not be counted then.  A tile behind the last of all is none.
-    for (int32_t tile = x.first; tile < x.end; ++tile) {
+    // A tile's values are on their way while its scores are taken, and the next tile's keys while its values are
+    // weighed, into registers that have just been read; behind an item's last tile come the next item's first keys.
+    // No load stands behind a branch, and a loop has a tile at least: waits could not be counted otherwise.  A tile
+    // behind the last of all is none.
+    int32_t tile = x.first;
+    do {
+      w.load_v(now);
       const bool last = tile + 1 == x.end;
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) next[t] = w.locate(last ? y : x, last ? y.first : tile + 1, t, !last || more);
@@ -627,14 +637,14 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
       w.weigh(p, now);
       if (!clear) w.mask_values(p, tile, now, next);
       w.add(p);
-      w.load_v(next);
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) now[t] = next[t];
-    }
+    } while (++tile < x.end);
+    if (!kAhead) w.load_q(y, ahead);
+    w.take_q(y, ahead);  // before the stores, which its wait would count
     w.end(x, part_of(a, at.parts, worker, x.first > x.s.tile0 ? 0 : 1, kPart));
     if (!more) return;
     x = y;
-    if (!kAhead) w.load_q(x, ahead);
   }
 }
 
