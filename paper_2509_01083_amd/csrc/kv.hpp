@@ -81,7 +81,7 @@ struct AttendLayout {
 inline AttendLayout attend_layout(int32_t dim) {
   AttendLayout l;
   l.starts = 0;  // where each wavefront's share begins
-  l.parts = align_up(size_t(24) * kAttendWorkers);
+  l.parts = align_up(size_t(32) * kAttendWorkers);
   // two parts of a wavefront: for each of its rows the values, a reference and a sum
   l.total = l.parts + align_up(sizeof(float) * 2 * kAttendWorkers * kAttendRows * size_t(padded_dim(dim) + 2));
   return l;

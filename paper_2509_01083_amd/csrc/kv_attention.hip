@@ -13,8 +13,8 @@
 // Scores come out with a row's keys in the registers of four lanes, in the order that the second
 // product takes P in: its contraction runs over keys in whatever order both operands have, so the
 // probabilities never leave their lane.  V^T wants eight keys of one dimension in a lane:
-// lane (c, g) loads dimensions 8c .. 8c+7 of its eight keys, whole rows of 256 bytes per four
-// lanes' keys, and picks halves of registers with v_perm (one per two elements).
+// lane (c, g) loads eight dimensions of its eight keys, whole rows of 256 bytes in sixteen lanes,
+// and picks halves of registers with v_perm (one per two elements).
 #include "kv.hpp"
 
 namespace dsde {
@@ -139,38 +139,42 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, int32_t b, int32_t 
 // The work in one line: for every sequence, key head and row block an item of kStart units (what it costs to begin
 // and end one, in tiles) and a unit for each tile.  Every wavefront takes an equal share of the line, whatever the
 // lengths are, so that all end together; items that it has a part of leave that part to join_kernel.
-constexpr int32_t kStart = 4;
-constexpr int32_t kLeast = 4;  // units of a share at least: short calls do not end in joining many parts
+constexpr int32_t kStart = 2;
+constexpr int32_t kLeast = 2;  // units of a share at least: short calls do not end in joining many parts
 __device__ __forceinline__ int64_t units_of(const AttendArgs &a, const Seq &s) {
   return int64_t(s.tiles + kStart) * s.blocks * a.cache.heads;
 }
 // Where a wavefront's share begins inside an item (tile > 0), and the wavefronts that have parts of that item.
 struct Start {
-  int32_t b, h, block, tile, w0, w1;
+  int32_t h, block, tile, w0, w1, row0, rows, b;
 };
 // A wavefront has two places for parts: 0 for one that another began, 1 for one that it began and did not end.
 __device__ __forceinline__ float *part_of(const AttendArgs &a, size_t at, int64_t worker, int slot, size_t floats) {
   return reinterpret_cast<float *>(static_cast<char *>(a.workspace) + at) + size_t(2 * worker + slot) * floats;
 }
 
+// Finished values: stored past the cache (nt), where reads that fill it keep a write waiting for microseconds, and with
+// it, waits being counted in order, every load behind it.
+template <typename T>
+__device__ __forceinline__ void store_past(char *to, T x) {
+  __builtin_nontemporal_store(x, reinterpret_cast<T *>(to));
+}
 // kVec values of a finished row, from dimension d on.
 template <int CACHE, int VEC>
 __device__ __forceinline__ void store_row(char *row, int32_t d, const float (&x)[VEC]) {
-  if constexpr (CACHE == DSDE_FP32) {
-    *reinterpret_cast<f32x4 *>(row + d * 4) = f32x4{x[0], x[1], x[2], x[3]};
-  } else if constexpr (VEC == 8) {
-    *reinterpret_cast<u32x4 *>(row + d * 2) =
-        u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
-  } else {
-    *reinterpret_cast<u32x2 *>(row + d * 2) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-  }
+  if constexpr (CACHE == DSDE_FP32)
+    store_past(row + d * 4, f32x4{x[0], x[1], x[2], x[3]});
+  else if constexpr (VEC == 8)
+    store_past(row + d * 2, u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])});
+  else
+    store_past(row + d * 2, u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
 }
 // A finished row's place, its factor and its log-normaliser.
 template <int CACHE>
-__device__ __forceinline__ char *finished(const AttendArgs &a, const Seq &s, int32_t h, int32_t row, float m, float l, bool stats,
+__device__ __forceinline__ char *finished(const AttendArgs &a, int32_t row0, int32_t h, int32_t row, float m, float l, bool stats,
                                           float *factor) {
   const int32_t j = row / a.group, head = h * a.group + (row - j * a.group);
-  const int64_t t = int64_t(s.row0) + j;
+  const int64_t t = int64_t(row0) + j;
   if (stats && a.lse)
     a.lse[t * (int64_t(a.group) * a.cache.heads) + head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2f;
   float f = l == 0.0f ? 0.0f : 1.0f / l;
@@ -212,8 +216,12 @@ struct Wave {
 
   __device__ __forceinline__ explicit Wave(const AttendArgs &args, int lane) : a(args), r(lane & 15), g(lane >> 4) {
     k_off = uint32_t(r * a.cache.token_stride + 16 * g);
-    v_off = uint32_t(4 * g * a.cache.token_stride + S::kVecBytes * r);
+    v_off = uint32_t(4 * g * a.cache.token_stride + S::kVecBytes * piece(r));
   }
+
+  // Which kVec dimensions of a set lane r loads.  Its sums come out in register r % 4 of the lanes of g = r / 4: in
+  // this order the four lanes of a row hold 64 bytes in a row (bf16) in each register, and store them together.
+  __device__ static __forceinline__ int piece(int r) { return 4 * (r % 4) + r / 4; }
 
   // Subtile t of a tile; nothing is read of those that no row sees.
   __device__ __forceinline__ At locate(const Item &x, int32_t tile, int t, bool wanted) const {
@@ -245,7 +253,7 @@ struct Wave {
       const Buffer from = buffer(at[t].keys + (a.cache.v - a.cache.k), at[t].bytes);
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e) {
-        const uint32_t off = (16 * e + r) * S::kVec < a.cache.dim ? v_off + 16 * S::kVecBytes * e : kOutside;
+        const uint32_t off = (16 * e + piece(r)) * S::kVec < a.cache.dim ? v_off + 16 * S::kVecBytes * e : kOutside;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[4 * t + i][e] = load_words<S::kVecWords>(from, off, i * a.cache.token_stride);
       }
@@ -476,12 +484,12 @@ struct Wave {
       if (row < x.s.n * a.group) {
         float f = 1.0f;
         char *to = nullptr;
-        if (done) to = finished<CACHE>(a, x.s, x.h, row, m[mt], sum, g == 0, &f);
+        if (done) to = finished<CACHE>(a, x.s.row0, x.h, row, m[mt], sum, g == 0, &f);
 #pragma unroll
         for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int32_t d = (16 * e + 4 * g + i) * S::kVec;
+            const int32_t d = (16 * e + piece(4 * g + i)) * S::kVec;
             float y[S::kVec];
 #pragma unroll
             for (int j = 0; j < S::kVec; ++j) y[j] = o[mt][e][j][i] * f;
@@ -513,7 +521,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
   constexpr int kRows = 16 * MT;
   constexpr size_t kPart = kRows * (DP + 2);
   // the next item's rows are fetched early where registers allow
-  constexpr bool kAhead = MT * DP * S::kQElt <= 512;
+  constexpr bool kAhead = MT * DP * S::kQElt <= 768;
   struct Begin {
     Start at;
     int32_t used;  // units of its item's start that lie before the share
@@ -528,7 +536,11 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
   const int32_t per = (a.B + kAttendThreads - 1) / kAttendThreads;
   const int32_t b0 = tid * per < a.B ? tid * per : a.B, b1 = b0 + per < a.B ? b0 + per : a.B;
   int64_t own = 0;
-  for (int32_t b = b0; b < b1; ++b) own += units_of(a, sequence<S::kTile>(a, b, kRows));
+  Seq mine;  // a thread's last sequence, its only one in batches up to 256
+  for (int32_t b = b0; b < b1; ++b) {
+    mine = sequence<S::kTile>(a, b, kRows);
+    own += units_of(a, mine);
+  }
   int64_t upto = own;
   for (int n = 1; n < 64; n <<= 1) {
     const int64_t o = __shfl_up(upto, n);
@@ -550,15 +562,15 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
     int64_t before = upto - own;
     if (begin < before || begin >= upto) continue;
     for (int32_t b = b0; b < b1; ++b) {
-      const Seq s = sequence<S::kTile>(a, b, kRows);
+      const Seq s = per == 1 ? mine : sequence<S::kTile>(a, b, kRows);
       const int64_t n = units_of(a, s);
       if (begin < before + n) {
         const int64_t x = begin - before;
         const int32_t size = s.tiles + kStart, item = int32_t(quotient(x, size, small)), u = int32_t(x - int64_t(item) * size);
         const int64_t unit = before + int64_t(item) * size + kStart;  // of the item's first tile
         const int32_t h = item / s.blocks;
-        s_begin[i] = Begin{Start{b, h, item - h * s.blocks, u > kStart ? u - kStart : 0, int32_t(quotient(unit, share, small)),
-                                 int32_t(quotient(unit + s.tiles - 1, share, small))}, u < kStart ? u : kStart, s};
+        s_begin[i] = Begin{Start{h, item - h * s.blocks, u > kStart ? u - kStart : 0, int32_t(quotient(unit, share, small)),
+                                 int32_t(quotient(unit + s.tiles - 1, share, small)), s.row0, s.n * a.group, b}, u < kStart ? u : kStart, s};
         break;
       }
       before += n;
@@ -679,10 +691,35 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
   const int32_t worker = blockIdx.x;
   const Start x = reinterpret_cast<const Start *>(static_cast<const char *>(a.workspace) + at.starts)[worker];
   if (x.tile == 0) return;
-  const Seq s = sequence<S::kTile>(a, x.b, kRows);
-  const int32_t rows = s.n * a.group, row0 = x.block * kRows, live = rows - row0 < kRows ? rows - row0 : kRows;
+  const int32_t row0 = x.block * kRows, live = x.rows - row0 < kRows ? x.rows - row0 : kRows;
   // cells of four values; at least 16 cells (256 bytes) for each workgroup
   const int32_t cells = live * (DP / 4), parts = x.w1 - x.w0 + 1, sharers = parts - 1;
+  if (parts == 2) {  // most often: all loads at once
+    constexpr int kTimes = (kRows * DP / 4 + 255) / 256;
+    const float *p0 = part_of(a, at.parts, x.w0, 1, kPart), *p1 = part_of(a, at.parts, x.w1, 0, kPart);
+    float m0[kTimes], m1[kTimes], l0[kTimes], l1[kTimes];
+    f32x4 o0[kTimes], o1[kTimes];
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k) {
+      const int32_t c = tid + 256 * k < cells ? tid + 256 * k : 0, i = c / (DP / 4), d = c % (DP / 4) * 4;
+      m0[k] = p0[kRows * DP + i], m1[k] = p1[kRows * DP + i];
+      l0[k] = p0[kRows * (DP + 1) + i], l1[k] = p1[kRows * (DP + 1) + i];
+      o0[k] = *reinterpret_cast<const f32x4 *>(p0 + i * DP + d), o1[k] = *reinterpret_cast<const f32x4 *>(p1 + i * DP + d);
+    }
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k) {
+      const int32_t c = tid + 256 * k, i = c / (DP / 4), d = c % (DP / 4) * 4;
+      if (c >= cells) break;
+      const float m = fmaxf(m0[k], m1[k]), ref = m == -INFINITY ? 0.0f : m;
+      const float f0 = exp2_fast(m0[k] - ref), f1 = exp2_fast(m1[k] - ref);
+      float f;
+      char *to = finished<CACHE>(a, x.row0, x.h, row0 + i, m, l0[k] * f0 + l1[k] * f1, d == 0, &f);
+      const f32x4 o = (o0[k] * f0 + o1[k] * f1) * f;
+      const float y[4] = {o.x, o.y, o.z, o.w};
+      if (d < a.cache.dim) store_row<CACHE, 4>(to, d, y);
+    }
+    return;
+  }
   int32_t n = (cells + sharers - 1) / sharers;
   n = n < 16 ? 16 : n;
   const int32_t c0 = (worker - x.w0 - 1) * n, c1 = c0 + n < cells ? c0 + n : cells;
@@ -717,7 +754,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
     }
     if (mine && lane == 0) {
       float f;
-      char *to = finished<CACHE>(a, s, x.h, row0 + i, m, l, d == 0, &f);
+      char *to = finished<CACHE>(a, x.row0, x.h, row0 + i, m, l, d == 0, &f);
       const float y[4] = {o.x * f, o.y * f, o.z * f, o.w * f};
       if (d < a.cache.dim) store_row<CACHE, 4>(to, d, y);
     }
