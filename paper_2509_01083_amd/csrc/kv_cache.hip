@@ -12,6 +12,7 @@ namespace {
 constexpr int kMapThreads = 1024, kMapWaves = kMapThreads / 64;
 constexpr int kSmallSeqs = 1024;     // sequences whose prefix sums stay in LDS
 constexpr int64_t kSmallRows = 8192;  // rows that the planning workgroup maps itself
+constexpr int32_t kManyPages = 4096;  // more pages than it gives back itself where it can leave them
 
 struct Sums {
   int64_t rows, taken, back;
@@ -76,7 +77,7 @@ __device__ __forceinline__ Sums moved(const Want &x, bool fits) {
   return Sums{x.n, ok && x.to > x.from ? x.to - x.from : 0, ok && x.to < x.from ? x.from - x.to : 0};
 }
 
-// The sequence (smallest index) whose range of the prefix sums pre [B+1] holds i.
+// The sequence whose range of the prefix sums pre [B+1] holds i: pre[0] <= i < pre[B].
 __device__ __forceinline__ int32_t find(const int32_t *pre, int32_t B, int32_t i) {
   int32_t lo = 0, hi = B;  // pre[lo] <= i < pre[hi]
   while (hi - lo > 1) {
@@ -89,17 +90,19 @@ __device__ __forceinline__ int32_t find(const int32_t *pre, int32_t B, int32_t i
   return lo;
 }
 
-// Page c of a sequence, where its table has it or, taken in this call, on the stack.
-__device__ __forceinline__ void map_row(const MapArgs &a, const int32_t *cu, const int32_t *taken, int32_t top, int64_t t) {
-  const int32_t total = cu[a.B];
+// What the second half of the plan needs of every sequence: in LDS for batches up to kSmallSeqs.
+struct Plan {
+  const int32_t *cu, *taken, *from, *base, *context;
+};
+// A row's slot: its page is in the table or, taken in this call, on the stack.
+__device__ __forceinline__ void map_row(const MapArgs &a, const Plan &p, int32_t top, int64_t t) {
   int32_t slot = -1, pos = -1;
-  if (t < total) {
-    const int32_t b = find(cu, a.B, int32_t(t));
-    const int32_t context = a.context[b];
-    if (context > 0) {  // a sequence with rows that is not flagged
-      pos = a.base[b] + (int32_t(t) - cu[b]);
-      const int32_t c = pos >> a.shift, grown = c - a.from[b];
-      const int32_t page = grown >= 0 ? a.stack[top - 1 - (taken[b] + grown)] : a.table[int64_t(b) * a.width + c];
+  if (t < p.cu[a.B]) {
+    const int32_t b = find(p.cu, a.B, int32_t(t));
+    if (p.context[b] > 0) {  // a sequence with rows that is not flagged
+      pos = p.base[b] + (int32_t(t) - p.cu[b]);
+      const int32_t c = pos >> a.shift, grown = c - p.from[b];
+      const int32_t page = grown >= 0 ? a.stack[top - 1 - (p.taken[b] + grown)] : a.table[int64_t(b) * a.width + c];
       if (page >= 0 && page < a.pages)
         slot = (page << a.shift) | (pos & ((1 << a.shift) - 1));
       else
@@ -109,65 +112,76 @@ __device__ __forceinline__ void map_row(const MapArgs &a, const int32_t *cu, con
   a.slots[t] = slot;
   a.positions[t] = pos;
 }
-__device__ __forceinline__ void take_page(const MapArgs &a, const int32_t *taken, int32_t top, int32_t i) {
-  const int32_t b = find(taken, a.B, i);
-  const int32_t c = a.from[b] + (i - taken[b]);
-  if (c < a.held[b]) a.table[int64_t(b) * a.width + c] = a.stack[top - 1 - i];  // not of a sequence that went without
+// The i-th page taken, of those that there are.
+__device__ __forceinline__ void take_page(const MapArgs &a, const Plan &p, int32_t top, int32_t i) {
+  const int32_t b = find(p.taken, a.B, i);
+  // not of a sequence that went without
+  if (p.context[b] > 0) a.table[int64_t(b) * a.width + p.from[b] + (i - p.taken[b])] = a.stack[top - 1 - i];
+}
+// The i-th page of F given back onto a stack of `have`; those of the sequences behind come first.
+__device__ __forceinline__ void give_page(const MapArgs &a, const int32_t *back, const int32_t *from, int32_t have, int32_t F,
+                                          int32_t i) {
+  const int32_t b = find(back, a.B, i);
+  int32_t *entry = a.table + int64_t(b) * a.width + from[b] - (back[b + 1] - i);  // ascending pages, descending places
+  a.stack[have + (F - 1 - i)] = *entry;
+  *entry = -1;
 }
 
-// The plan, by one workgroup.  ALL: it also takes the pages and maps the rows, which
-// saves a launch (2 us) where they are few; with more rows one CU takes longer than that.
-template <bool ALL>
+// The plan, by one workgroup: a chain of round trips to memory (the sequences' numbers, the pages that move, the pages
+// of the rows) and prefix sums between them.  ALL: it also takes the pages and maps the rows, which saves a launch (2 us)
+// where they are few; with more rows one CU takes longer than that.  LOCAL: one sequence to a thread, kept in
+// registers and LDS.  SHARED: give_kernel runs behind it (37,000 pages took this workgroup 31 us).
+template <bool ALL, bool LOCAL, bool SHARED>
 __global__ __launch_bounds__(kMapThreads) void map_plan_kernel(MapArgs a) {
-  __shared__ int32_t s_cu[kSmallSeqs + 1], s_taken[kSmallSeqs + 1], s_back[kSmallSeqs + 1];
-  const bool local = a.B <= kSmallSeqs;
-  // rows as they are packed, then what moves for sequences whose rows fit
+  constexpr int kHeld = LOCAL ? kSmallSeqs : 1;
+  __shared__ int32_t s_cu[kHeld + 1], s_taken[kHeld + 1], s_back[kHeld + 1], s_from[kHeld], s_base[kHeld], s_context[kHeld];
+  const int32_t have = a.n_free[0];
+  int32_t *cu = LOCAL ? s_cu : a.cu_rows, *taken = LOCAL ? s_taken : a.taken, *back = LOCAL ? s_back : a.back;
+  // rows as they are packed, and what moves for sequences whose rows fit
   Sums before{0, 0, 0}, total;
+  Want x{0, 0, 0, 0, 0};
+  Sums own{0, 0, 0};
   for (int32_t b0 = 0; b0 < a.B; b0 += kMapThreads) {
     const int32_t b = b0 + threadIdx.x;
-    Want x{0, 0, 0, 0, 0};
+    x = Want{0, 0, 0, 0, 0};
     if (b < a.B) x = wanted(a, b);
-    const Sums rows = block_scan(Sums{x.n, 0, 0}, &total);
-    const bool fits = before.rows + rows.rows <= a.rows;
-    const Sums own = moved(x, fits);
-    Sums moves;
-    const Sums end = block_scan(Sums{0, own.taken, own.back}, &moves);
+    own = moved(x, true);
+    Sums end = block_scan(own, &total);
+    if (before.rows + total.rows > a.rows) {  // some do not fit: once more, without what they move
+      own = moved(x, before.rows + end.rows <= a.rows);
+      end = block_scan(own, &total);
+    }
     if (b < a.B) {
-      const Sums last = before + Sums{rows.rows, end.taken, end.back};
+      const Sums last = before + end;
       const auto store = [&](int32_t i, int64_t r, int64_t t, int64_t g) {
         a.cu_rows[i] = kept(r);
-        a.taken[i] = kept(t);
-        a.back[i] = kept(g);
-        if (local) s_cu[i] = kept(r), s_taken[i] = kept(t), s_back[i] = kept(g);
+        cu[i] = kept(r), taken[i] = kept(t), back[i] = kept(g);
+        if (LOCAL && !ALL) a.taken[i] = kept(t);
+        if (LOCAL && SHARED) a.back[i] = kept(g);
       };
       store(b, last.rows - x.n, last.taken - own.taken, last.back - own.back);
-      a.from[b] = x.from;
       if (b == a.B - 1) store(a.B, last.rows, last.taken, last.back);
+      if (LOCAL) s_from[b] = x.from;
+      if (!LOCAL || !ALL || SHARED) a.from[b] = x.from;
     }
-    before = before + Sums{total.rows, moves.taken, moves.back};
+    before = before + total;
   }
   __syncthreads();
-  const int32_t *cu = local ? s_cu : a.cu_rows, *taken = local ? s_taken : a.taken, *back = local ? s_back : a.back;
-  const int32_t have = a.n_free[0];
   const bool sound = have >= 0 && have <= a.pages && before.back <= a.pages - have;
   const int32_t F = sound ? int32_t(before.back) : 0, top = sound ? have + F : 0;
-  __syncthreads();  // everyone has read n_free
-  // pages given back; those of the sequences behind come first
-  for (int32_t i = threadIdx.x; i < F; i += kMapThreads) {
-    const int32_t b = find(back, a.B, i);
-    const int32_t c = a.from[b] - (back[b + 1] - i);  // ascending pages, descending places
-    int32_t *entry = a.table + int64_t(b) * a.width + c;
-    a.stack[have + (F - 1 - i)] = *entry;
-    *entry = -1;
-  }
+  const int32_t *from = LOCAL ? s_from : a.from;
+  // many pages given back by a call that takes none are left to the whole card
+  const bool leave = SHARED && before.taken == 0 && F > kManyPages;
+  if (!leave)
+    for (int32_t i = threadIdx.x; i < F; i += kMapThreads) give_page(a, back, from, have, F, i);
   // every sequence's outcome
   int32_t used = 0;
   for (int32_t b0 = 0; b0 < a.B; b0 += kMapThreads) {
     const int32_t b = b0 + threadIdx.x;
     if (b >= a.B) break;
-    Want x = wanted(a, b);
+    if (!LOCAL) x = wanted(a, b);
     const bool fits = int64_t(cu[b]) + x.n <= a.rows;
-    const Sums own = moved(x, fits);
+    if (!LOCAL) own = moved(x, fits);
     if (!fits) x.err |= DSDE_ERR_LAYOUT;
     if (own.taken + own.back > 0 && !sound) x.err |= DSDE_ERR_STATE;
     if (own.taken > 0 && sound && taken[b + 1] > top) x.err |= DSDE_ERR_PAGES;
@@ -175,9 +189,11 @@ __global__ __launch_bounds__(kMapThreads) void map_plan_kernel(MapArgs a) {
       if (own.taken > 0) used = taken[b + 1];
       if (x.to != x.from) a.held[b] = x.to;
     }
-    a.base[b] = kept(x.base);
-    a.context[b] = x.err ? 0 : int32_t(x.base + x.n);
+    const int32_t base = kept(x.base), context = x.err ? 0 : int32_t(x.base + x.n);
+    a.base[b] = base;
+    a.context[b] = context;
     a.seq_err[b] = x.err;
+    if (LOCAL) s_base[b] = base, s_context[b] = context;
   }
   __shared__ int32_t s_used;
   if (threadIdx.x == 0) s_used = 0;
@@ -187,19 +203,28 @@ __global__ __launch_bounds__(kMapThreads) void map_plan_kernel(MapArgs a) {
   if (threadIdx.x == 0) {
     if (sound) a.n_free[0] = top - s_used;
     a.top[0] = top;
+    a.top[1] = leave ? F : 0;
   }
   if (!ALL) return;
+  const Plan p{cu, taken, from, LOCAL ? s_base : a.base, LOCAL ? s_context : a.context};
   const int32_t n = s_used;
-  for (int32_t i = threadIdx.x; i < n; i += kMapThreads) take_page(a, taken, top, i);
-  for (int64_t t = threadIdx.x; t < a.rows; t += kMapThreads) map_row(a, cu, taken, top, t);
+  for (int32_t i = threadIdx.x; i < n; i += kMapThreads) take_page(a, p, top, i);
+  for (int64_t t = threadIdx.x; t < a.rows; t += kMapThreads) map_row(a, p, top, t);
 }
 
 // Pages taken and rows mapped by the whole card.
 __global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
   const int64_t stride = int64_t(gridDim.x) * 256, at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const Plan p{a.cu_rows, a.taken, a.from, a.base, a.context};
   const int32_t top = a.top[0], n = top > 0 ? top - a.n_free[0] : 0;
-  for (int64_t i = at; i < n; i += stride) take_page(a, a.taken, top, int32_t(i));
-  for (int64_t t = at; t < a.rows; t += stride) map_row(a, a.cu_rows, a.taken, top, t);
+  for (int64_t i = at; i < n; i += stride) take_page(a, p, top, int32_t(i));
+  for (int64_t t = at; t < a.rows; t += stride) map_row(a, p, top, t);
+}
+// Pages given back that the plan left.
+__global__ __launch_bounds__(256) void give_kernel(MapArgs a) {
+  const int32_t F = a.top[1];
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < F; i += int64_t(gridDim.x) * 256)
+    give_page(a, a.back, a.from, a.top[0] - F, F, int32_t(i));
 }
 
 // Rows into slots: 16 bytes of a row per lane, a wavefront per row of keys or values.
@@ -251,10 +276,19 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvWriteArgs a, int64_t fi
 }  // namespace
 
 int launch_kv_map(const MapArgs &a, hipStream_t stream) {
-  if (a.rows <= kSmallRows) {
-    map_plan_kernel<true><<<1, kMapThreads, 0, stream>>>(a);
+  const auto plan = [&](auto all, auto shared) {
+    if (a.B <= kSmallSeqs)
+      map_plan_kernel<all.value, true, shared.value><<<1, kMapThreads, 0, stream>>>(a);
+    else
+      map_plan_kernel<all.value, false, shared.value><<<1, kMapThreads, 0, stream>>>(a);
+  };
+  if (a.rows == 0 && int64_t(a.B) * a.width > 4 * kManyPages) {  // sequences that end: maybe many pages
+    plan(std::true_type{}, std::true_type{});
+    give_kernel<<<256, 256, 0, stream>>>(a);
+  } else if (a.rows <= kSmallRows) {
+    plan(std::true_type{}, std::false_type{});
   } else {
-    map_plan_kernel<false><<<1, kMapThreads, 0, stream>>>(a);
+    plan(std::false_type{}, std::false_type{});
     const int64_t blocks = (a.rows + 255) / 256;
     map_rows_kernel<<<uint32_t(blocks < 2048 ? blocks : 2048), 256, 0, stream>>>(a);
   }

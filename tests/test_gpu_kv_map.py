@@ -64,9 +64,9 @@ def test_steps_follow_the_loop(gpu_lib, B, page):
         accepted = [r.randrange(-1, s + 1) for s in sl]
 
 
-@pytest.mark.parametrize("B,most", [(3, 9000), (40, 1500), (1, 60000), (1100, 70)])
+@pytest.mark.parametrize("B,most", [(3, 9000), (40, 1500), (1, 60000), (1100, 70), (300, 1500), (1100, 400)])
 def test_prompts_and_their_end(gpu_lib, B, most):
-    """More rows than the planning workgroup maps itself; then every page goes back."""
+    """More rows than the planning workgroup maps itself; then every page goes back, by that workgroup or by all."""
     r = random.Random(B)
     page = 16
     W = -(-most // page)
