@@ -89,6 +89,21 @@ def test_e4m3_rows_and_layouts(gpu_lib):
         assert torch.equal(bits(kc), want[0]) and torch.equal(bits(vc), want[1]), (T, H, D)
 
 
+@pytest.mark.parametrize("dtype,T", [("bf16", 9000), ("e4m3", 17000)])
+def test_more_rows_than_the_caches_hold(gpu_lib, dtype, T):
+    H, D, S = 16, 128, 64
+    g = torch.Generator(device="cuda").manual_seed(T)
+    k, v = (torch.randn((T, H, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    scale = torch.full((H,), 0.25, device="cuda") if dtype == "e4m3" else None
+    P = -(-T // S)
+    slots = torch.randperm(P * S, generator=g, device="cuda")[:T].int()
+    kc, vc = cache(P, H, S, D, DT[dtype], False)
+    gpu_lib.kv_write(k, v, slots, kc, vc, k_scale=scale, v_scale=scale)
+    for x, c in ((k, kc), (v, vc)):
+        y = x if scale is None else (x.float() * 4.0).to(DT[dtype])  # a scale of a power of two
+        assert torch.equal(bits(c)[slots.long() // S, :, slots.long() % S], bits(y))
+
+
 def test_slots_out_of_range_are_flagged(gpu_lib):
     H, D, S, P = 2, 64, 16, 4
     buf = torch.full((P + 2, H, S, D), 7.0, device="cuda")  # the cache is its middle
