@@ -39,12 +39,13 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Elements of a cache type, DP the head size rounded up to 64, 128 or 256.  Lane (r, g) = (lane & 15, lane >> 4).
-template <int CACHE, int DP>
+template <int CACHE, int DP, int MT>
 struct Shape {
   static constexpr int kElt = CACHE == DSDE_FP32 ? 4 : CACHE == DSDE_BF16 ? 2 : 1;
   // subtiles of 16 keys: 16 KiB of keys and values at a time where registers allow
   static constexpr int kLeastSub = CACHE == DSDE_FP32 ? 1 : 2;
-  static constexpr int kSub = 512 / (DP * kElt) < kLeastSub ? kLeastSub : 512 / (DP * kElt) > 4 ? 4 : 512 / (DP * kElt);
+  static constexpr int kMostSub = MT > 2 ? 2 : 4;
+  static constexpr int kSub = 512 / (DP * kElt) < kLeastSub ? kLeastSub : 512 / (DP * kElt) > kMostSub ? kMostSub : 512 / (DP * kElt);
   static constexpr int kTile = 16 * kSub;                      // keys of a step
   static constexpr int kPer16 = 16 / kElt;                     // elements in 16 bytes
   static constexpr int kChunks = DP * kElt / 64;               // 16-byte chunks of a key per lane: chunk j at 16 (4 j + g)
@@ -55,6 +56,8 @@ struct Shape {
   static constexpr int kKeys = 4 * kSub;                       // keys of a tile in a lane: 16 t + 4 g + i
   static constexpr int kQElt = CACHE == DSDE_FP32 ? 4 : 2;
   static constexpr int kQChunks = DP * kQElt / 64;             // 16-byte chunks of a query row in a lane
+  // where rows and accumulators are many, the rows at hand are in LDS, and the next item's are not fetched early
+  static constexpr bool kAhead = MT * DP * kQElt <= 768;
   // first dimension of a chunk: those that the keys' chunks hold
   __device__ static __forceinline__ int32_t q_dim(int i, int g) {
     if constexpr (CACHE == DSDE_E4M3) return (4 * (i / 2) + g) * 16 + 8 * (i % 2);
@@ -63,7 +66,7 @@ struct Shape {
 };
 
 template <int WORDS>
-struct Words {
+struct alignas(4 * WORDS) Words {
   uint32_t w[WORDS];
 };
 // Memory that lanes read through one scalar descriptor and 32-bit offsets; what lies at or behind `bytes` reads as 0.
@@ -104,6 +107,21 @@ __device__ __forceinline__ bool not_finite(uint32_t x) {
   if constexpr (CACHE == DSDE_BF16) return (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
   const uint32_t y = ~x & 0x7f7f7f7fu;  // a byte of 0: NaN
   return ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+}
+
+// The same word with its values that are not finite at 0.
+template <int CACHE>
+__device__ __forceinline__ uint32_t finite_only(uint32_t x) {
+  if constexpr (CACHE == DSDE_FP32) return not_finite<CACHE>(x) ? 0u : x;
+  constexpr uint32_t part = CACHE == DSDE_BF16 ? 0xffffu : 0xffu;
+  uint32_t y = 0;
+#pragma unroll
+  for (int at = 0; at < 32; at += CACHE == DSDE_BF16 ? 16 : 8) {
+    const uint32_t one = x & (part << at);
+    // the rest of the word as 0 is finite
+    y |= not_finite<CACHE>(one) ? 0u : one;
+  }
+  return y;
 }
 
 // One sequence of a call.
@@ -197,7 +215,7 @@ struct At {
 
 template <int CACHE, int DP, int MT>
 struct Wave {
-  using S = Shape<CACHE, DP>;
+  using S = Shape<CACHE, DP, MT>;
   const AttendArgs &a;
   int r, g;
   uint32_t k_off, v_off;
@@ -207,14 +225,24 @@ struct Wave {
   int32_t hi_all, lo_all;  // seen by every row
   int32_t hi_any, lo_any;  // seen by any
   float c;                 // scale log2(e), with the keys' scale, positive
-  Words<4> q[MT][S::kQChunks];
+  Words<4> q[S::kAhead ? MT : 1][S::kAhead ? S::kQChunks : 1];
+  Words<4> (*q_lds)[64];   // [MT * kQChunks][64]: each lane its own
   f32x4 o[MT][S::kSets][S::kVec];
   float m[MT], l[MT];
+  // which of a lane's values have a NaN, +inf or -inf in their sum, a bit each (add_odd)
+  static constexpr int kBits = (DP + 127) / 128;
+  uint32_t special[3][MT][kBits];
   // keys and values of a tile
   Words<4> k[S::kSub][S::kChunks];
   Words<S::kVecWords> v[S::kKeys][S::kSets];
 
-  __device__ __forceinline__ explicit Wave(const AttendArgs &args, int lane) : a(args), r(lane & 15), g(lane >> 4) {
+  __device__ __forceinline__ Words<4> &row(int mt, int i) {
+    if constexpr (S::kAhead) return q[mt][i];
+    return q_lds[mt * S::kQChunks + i][16 * g + r];
+  }
+
+  __device__ __forceinline__ Wave(const AttendArgs &args, int lane, Words<4> (*lds)[64])
+      : a(args), r(lane & 15), g(lane >> 4), q_lds(lds) {
     k_off = uint32_t(r * a.cache.token_stride + 16 * g);
     v_off = uint32_t(4 * g * a.cache.token_stride + S::kVecBytes * piece(r));
   }
@@ -286,8 +314,10 @@ struct Wave {
 #pragma unroll
       for (int i = 0; i < S::kQChunks; ++i) {
         const bool there = live && !flat && S::q_dim(i, g) < a.cache.dim;
+        Words<4> x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[mt][i].w[e] = there ? ahead[mt][i].w[e] ^ flip : 0u;
+        for (int e = 0; e < 4; ++e) x.w[e] = there ? ahead[mt][i].w[e] ^ flip : 0u;
+        row(mt, i) = x;
       }
     }
   }
@@ -303,6 +333,8 @@ struct Wave {
       hi[mt] = row < x.s.n * a.group ? oldest + row / a.group : -1;
       lo[mt] = a.window > 0 && hi[mt] >= a.window ? hi[mt] - a.window + 1 : 0;
       m[mt] = -INFINITY, l[mt] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kBits; ++i) special[0][mt][i] = special[1][mt][i] = special[2][mt][i] = 0;
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
@@ -324,17 +356,17 @@ struct Wave {
           for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-              x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), __uint_as_float(q[mt][j].w[e]), x[mt][t], 0, 0, 0);
+              x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), __uint_as_float(row(mt, j).w[e]), x[mt][t], 0, 0, 0);
         } else if constexpr (CACHE == DSDE_BF16) {
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(w), operand(q[mt][j]), x[mt][t], 0, 0, 0);
+          for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(w), operand(row(mt, j)), x[mt][t], 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const bf16x8 kk = operand(Words<4>{{widen<false>(w.w[2 * e]), widen<true>(w.w[2 * e]), widen<false>(w.w[2 * e + 1]),
                                                 widen<true>(w.w[2 * e + 1])}});
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(q[mt][2 * j + e]), x[mt][t], 0, 0, 0);
+            for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(row(mt, 2 * j + e)), x[mt][t], 0, 0, 0);
           }
         }
       }
@@ -375,12 +407,28 @@ struct Wave {
     }
   }
 
-  // Adds the weights' values.  The weights are rounded to the type of the values for the matrix instruction: half a
-  // unit of the last place each, as the output's own rounding, and independent of each other.
-  // ONLY: to the rows of token `token` alone (a weight of 0 would not keep a NaN from the others).
-  template <bool ONLY = false>
-  __device__ __forceinline__ void add(const f32x4 (&p)[MT][S::kSub], int32_t token = 0) {
-    const auto put = [&](int mt, int e, int j, f32x4 x) { o[mt][e][j] = !ONLY || hi[mt] == token ? x : o[mt][e][j]; };
+  // Two dimensions, 2 j2 and 2 j2 + 1 of set e, of the eight keys of subtiles t and t + 1: one word of each key.
+  __device__ __forceinline__ void pick(int t, int e, int j2, Words<4> &even, Words<4> &odd) const {
+    uint32_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const Words<S::kVecWords> &y = v[4 * t + i][e];
+      if constexpr (CACHE == DSDE_BF16)
+        x[i] = y.w[j2];
+      else
+        x[i] = j2 & 1 ? widen<true>(y.w[j2 / 2]) : widen<false>(y.w[j2 / 2]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      even.w[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+      odd.w[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
+    }
+  }
+
+  // Adds the weights' values.  For 16-bit matrix instructions a weight is the sum of two bf16 numbers, good to 2^-17: one
+  // alone would be off by as much as the output's own rounding (2.2e-3 of the norm of random rows' outputs instead of
+  // 1.6e-3), and the second product takes no time that memory does not (0 to 1 % with up to 48 rows, 6 % with 64).
+  __device__ __forceinline__ void add(const f32x4 (&p)[MT][S::kSub]) {
     if constexpr (CACHE == DSDE_FP32) {
 #pragma unroll
       for (int i = 0; i < S::kKeys; ++i)
@@ -390,38 +438,36 @@ struct Wave {
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-              put(mt, e, j, __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e].w[j]), p[mt][i / 4][i % 4], o[mt][e][j], 0, 0, 0));
+              o[mt][e][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e].w[j]), p[mt][i / 4][i % 4], o[mt][e][j], 0, 0, 0);
     } else {
 #pragma unroll
       for (int t = 0; t < S::kSub; t += 2) {
-        bf16x8 w[MT];
+        bf16x8 w[MT], rest[MT];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          w[mt] = operand(Words<4>{{pack_bf16(p[mt][t].x, p[mt][t].y), pack_bf16(p[mt][t].z, p[mt][t].w),
-                                    pack_bf16(p[mt][t + 1].x, p[mt][t + 1].y), pack_bf16(p[mt][t + 1].z, p[mt][t + 1].w)}});
+        for (int mt = 0; mt < MT; ++mt) {
+          Words<4> hi, lo;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = p[mt][t + i / 2][2 * (i % 2)], y = p[mt][t + i / 2][2 * (i % 2) + 1];
+            hi.w[i] = pack_bf16(x, y);
+            lo.w[i] = pack_bf16(x - __uint_as_float(hi.w[i] << 16), y - __uint_as_float(hi.w[i] & 0xffff0000u));
+          }
+          w[mt] = operand(hi), rest[mt] = operand(lo);
+        }
 #pragma unroll
         for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
-          for (int j2 = 0; j2 < S::kVec / 2; ++j2) {  // two dimensions from one word of each key
-            uint32_t x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const Words<S::kVecWords> &y = v[4 * t + i][e];
-              if constexpr (CACHE == DSDE_BF16)
-                x[i] = y.w[j2];
-              else
-                x[i] = j2 & 1 ? widen<true>(y.w[j2 / 2]) : widen<false>(y.w[j2 / 2]);
-            }
+          for (int j2 = 0; j2 < S::kVec / 2; ++j2) {
             Words<4> even, odd;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              even.w[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
-              odd.w[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
-            }
+            pick(t, e, j2, even, odd);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-              put(mt, e, 2 * j2, __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(even), w[mt], o[mt][e][2 * j2], 0, 0, 0));
-              put(mt, e, 2 * j2 + 1, __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(odd), w[mt], o[mt][e][2 * j2 + 1], 0, 0, 0));
+              const auto both = [&](const Words<4> &v, f32x4 to) {
+                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(v), w[mt], to, 0, 0, 0);
+                return __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(v), rest[mt], to, 0, 0, 0);
+              };
+              o[mt][e][2 * j2] = both(even, o[mt][e][2 * j2]);
+              o[mt][e][2 * j2 + 1] = both(odd, o[mt][e][2 * j2 + 1]);
             }
           }
       }
@@ -439,13 +485,14 @@ struct Wave {
         for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= lo[mt] && key <= hi[mt] ? x[mt][t][i] : -INFINITY;
       }
   }
-  // Keeps the values of tokens from .. to, 0 for others; whether one of them is not finite.
-  __device__ __forceinline__ bool keep(int32_t tile, int32_t from, int32_t to) {
+  // The same for values, as a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0;
+  // others that are not finite (rare) too, once the rows that see them have them.
+  __device__ __forceinline__ void mask_values(int32_t tile) {
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < S::kKeys; ++i) {
       const int32_t key = tile * S::kTile + 16 * (i / 4) + 4 * g + i % 4;
-      const bool seen = key >= from && key <= to;
+      const bool seen = key >= lo_any && key <= hi_any;
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
@@ -454,20 +501,107 @@ struct Wave {
           odd |= not_finite<CACHE>(v[i][e].w[w]);
         }
     }
-    return __any(odd);
+    if (__any(odd)) add_odd(tile);
   }
-  // The same for values: a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0; where
-  // one that some rows see is not finite (rare), the tile's values are read again for each of the sequence's tokens,
-  // which adds what it sees, and then all become 0.
-  __device__ __forceinline__ void mask_values(const f32x4 (&p)[MT][S::kSub], int32_t tile, const At (&from)[S::kSub], const At (&next)[S::kSub]) {
-    if (!keep(tile, lo_any, hi_any)) return;
-    for (int32_t token = hi_all; token <= hi_any; ++token) {
-      load_v(from);
-      keep(tile, a.window > 0 && token >= a.window ? token - a.window + 1 : 0, token);
-      add<true>(p, token);
+  __device__ static constexpr int bit(int e, int j, int i) { return (e * S::kVec + j) * 4 + i; }
+  // For NaN, +inf and -inf in turn: how many such values of each dimension a row sees, a product of ones and zeros.  A
+  // sum with one of them is it, whatever the weights (NaN with both infinities), so a bit is enough until the end; the
+  // accumulators have no second place among the registers here.
+  __device__ __forceinline__ void add_odd(int32_t tile) {
+    const auto sees = [&](int mt, int t, int i) {
+      const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
+      return key >= lo[mt] && key <= hi[mt];
+    };
+#pragma unroll 1
+    for (int kind = 0; kind < 3; ++kind) {
+      // nothing is to be worked out before the loop and kept: registers are scarce on all ways to here
+#pragma unroll
+      for (int i = 0; i < S::kKeys; ++i)
+#pragma unroll
+        for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+          for (int w = 0; w < S::kVecWords; ++w) asm volatile("" : "+v"(v[i][e].w[w]));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(lo[mt]), "+v"(hi[mt]));
+      uint32_t bits[MT][kBits];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < kBits; ++i) bits[mt][i] = 0;
+      const auto put = [&](int mt, int e, int j, f32x4 count) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits[mt][bit(e, j, i) / 32] |= count[i] > 0.0f ? 1u << bit(e, j, i) % 32 : 0u;
+      };
+      if constexpr (CACHE == DSDE_FP32) {
+#pragma unroll
+        for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              f32x4 count{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int i = 0; i < S::kKeys; ++i) {
+                const float y = __uint_as_float(v[i][e].w[j]);
+                const bool is = kind == 0 ? y != y : y == (kind == 1 ? INFINITY : -INFINITY);
+                count = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.0f : 0.0f, sees(mt, i / 4, i % 4) ? 1.0f : 0.0f, count, 0, 0, 0);
+              }
+              put(mt, e, j, count);
+            }
+      } else {
+        // halves of a word that are of the kind, as ones
+        const auto ones = [&](Words<4> x) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const auto one = [&](uint32_t h) {
+              return (kind == 0 ? (h & 0x7fffu) > 0x7f80u : h == (kind == 1 ? 0x7f80u : 0xff80u)) ? 0x3f80u : 0u;
+            };
+            x.w[i] = one(x.w[i] & 0xffffu) | one(x.w[i] >> 16) << 16;
+          }
+          return x;
+        };
+#pragma unroll
+        for (int t = 0; t < S::kSub; t += 2) {
+          bf16x8 seen[MT];
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            Words<4> x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x.w[i] = (sees(mt, t + i / 2, 2 * (i % 2)) ? 0x3f80u : 0u) | (sees(mt, t + i / 2, 2 * (i % 2) + 1) ? 0x3f800000u : 0u);
+            seen[mt] = operand(x);
+          }
+#pragma unroll
+          for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+            for (int j2 = 0; j2 < S::kVec / 2; ++j2) {
+              Words<4> even, odd;
+              pick(t, e, j2, even, odd);
+              even = ones(even), odd = ones(odd);
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                const f32x4 none{0.0f, 0.0f, 0.0f, 0.0f};
+                put(mt, e, 2 * j2, __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(even), seen[mt], none, 0, 0, 0));
+                put(mt, e, 2 * j2 + 1, __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(odd), seen[mt], none, 0, 0, 0));
+              }
+            }
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < kBits; ++i) {
+          special[0][mt][i] |= kind == 0 ? bits[mt][i] : 0u;
+          special[1][mt][i] |= kind == 1 ? bits[mt][i] : 0u;
+          special[2][mt][i] |= kind == 2 ? bits[mt][i] : 0u;
+        }
     }
-    keep(tile, 0, -1);
-    load_k(next);  // again: this path has had their registers
+#pragma unroll
+    for (int i = 0; i < S::kKeys; ++i)
+#pragma unroll
+      for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+        for (int w = 0; w < S::kVecWords; ++w) v[i][e].w[w] = finite_only<CACHE>(v[i][e].w[w]);
   }
 
   // The item's rows, or its part of them.
@@ -481,6 +615,10 @@ struct Wave {
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       if (x.s.err) sum = NAN;  // a context that is none
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < kBits; ++i) any |= special[0][mt][i] | special[1][mt][i] | special[2][mt][i];
+      const bool odd = __any(any != 0);
       if (row < x.s.n * a.group) {
         float f = 1.0f;
         char *to = nullptr;
@@ -493,6 +631,15 @@ struct Wave {
             float y[S::kVec];
 #pragma unroll
             for (int j = 0; j < S::kVec; ++j) y[j] = o[mt][e][j][i] * f;
+            if (odd) {
+#pragma unroll
+              for (int j = 0; j < S::kVec; ++j) {
+                const int w = bit(e, j, i) / 32, at = bit(e, j, i) % 32;
+                y[j] += special[0][mt][w] >> at & 1 ? NAN : 0.0f;
+                y[j] += special[1][mt][w] >> at & 1 ? INFINITY : 0.0f;
+                y[j] -= special[2][mt][w] >> at & 1 ? INFINITY : 0.0f;
+              }
+            }
             if (done) {
               if (d < a.cache.dim) store_row<CACHE, S::kVec>(to, d, y);
             } else {
@@ -517,11 +664,9 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y, bool small) {
 
 template <int CACHE, int DP, int MT>
 __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a, AttendLayout at) {
-  using S = Shape<CACHE, DP>;
+  using S = Shape<CACHE, DP, MT>;
   constexpr int kRows = 16 * MT;
   constexpr size_t kPart = kRows * (DP + 2);
-  // the next item's rows are fetched early where registers allow
-  constexpr bool kAhead = MT * DP * S::kQElt <= 768;
   struct Begin {
     Start at;
     int32_t used;  // units of its item's start that lie before the share
@@ -600,7 +745,9 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
   };
   take(x, tile);
 
-  Wave<CACHE, DP, MT> w(a, lane);
+  constexpr int kLds = S::kAhead ? 1 : MT * S::kQChunks;
+  __shared__ Words<4> s_q[S::kAhead ? 1 : kAttendWaves][kLds][64];
+  Wave<CACHE, DP, MT> w(a, lane, s_q[S::kAhead ? 0 : wave]);
   At now[S::kSub], next[S::kSub];
   Words<4> ahead[MT][S::kQChunks];
   w.load_q(x, ahead);
@@ -630,13 +777,14 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
     else
       y = x;
     w.begin(x);
-    if (kAhead) w.load_q(y, ahead);
+    if (S::kAhead) w.load_q(y, ahead);
     // A tile's values are on their way while its scores are taken, and the next tile's keys while its values are
     // weighed, into registers that have just been read; behind an item's last tile come the next item's first keys.
     // No load stands behind a branch, and a loop has a tile at least: waits could not be counted otherwise.  A tile
     // behind the last of all is none.
     int32_t tile = x.first;
     do {
+      if (!S::kAhead) asm volatile("" : : : "memory");  // rows are read from LDS for every tile, not kept
       w.load_v(now);
       const bool last = tile + 1 == x.end;
 #pragma unroll
@@ -647,12 +795,12 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
       const bool clear = tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
       if (!clear) w.mask(p, tile);
       w.weigh(p, now);
-      if (!clear) w.mask_values(p, tile, now, next);
+      if (!clear) w.mask_values(tile);
       w.add(p);
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) now[t] = next[t];
     } while (++tile < x.end);
-    if (!kAhead) w.load_q(y, ahead);
+    if (!S::kAhead) w.load_q(y, ahead);
     w.take_q(y, ahead);  // before the stores, which its wait would count
     w.end(x, part_of(a, at.parts, worker, x.first > x.s.tile0 ? 0 : 1, kPart));
     if (!more) return;
@@ -665,7 +813,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
 // behind them check the sequences.
 template <int CACHE, int DP, int MT>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at, int32_t workers) {
-  using S = Shape<CACHE, DP>;
+  using S = Shape<CACHE, DP, MT>;
   constexpr int kRows = 16 * MT;
   constexpr size_t kPart = kRows * (DP + 2);
   const int tid = threadIdx.x;
