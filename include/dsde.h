@@ -599,7 +599,7 @@ size_t dsde_kv_map_workspace_bytes(int32_t B);
  * it took leaves the stack as it was.)
  *
  *   B, pages, width             sequences (1 to 2^20), pages in the cache, entries of a table row
- *                               (width * page_size < 2^31)
+ *                               (width * page_size <= 2^30)
  *   rows                        rows the slot arrays have room for (0 <= rows < 2^31)
  *   sl [B]             int32    rows to come, less extra
  *   kv_len [B]         int32    tokens in the cache before the last step
@@ -609,7 +609,8 @@ size_t dsde_kv_map_workspace_bytes(int32_t B);
  *   free_pages [pages] int32    in/out: the stack, n_free[0] entries; those above are left as they are
  *   n_free [1]         int32    in/out
  * Outputs:
- *   base [B], context [B]  int32   base_b, and base_b + n_b (base may be kv_len itself)
+ *   base [B], context [B]  int32   base_b (kv_len[b] where that or accepted[b] is out of range), and base_b + n_b; base
+ *                               may be kv_len itself
  *   cu_rows [B+1]      int32    exclusive prefix sums of n_b
  *   slots, positions [rows]  int32   of each row; -1 behind the last one
  *   seq_err [B]        uint32   DSDE_ERR_LAYOUT: a negative n_b, kv_len or base, accepted under -1, or rows that do
@@ -662,7 +663,8 @@ size_t dsde_kv_attention_workspace_bytes(int32_t B, int32_t heads, int32_t group
  *   q [T, q_heads, dim]   dtype   the cache's type, or DSDE_BF16 for DSDE_E4M3; q_heads a multiple of cache->heads:
  *                                 query head h reads key head h / (q_heads / heads)
  *   B, max_rows                   sequences (1 to 2^20), most rows of one (1 to DSDE_MAX_ROWS)
- *   table [B, width]      int32   as dsde_kv_map leaves it; entries behind a sequence's tokens are not read
+ *   table [B, width]      int32   as dsde_kv_map leaves it (width * page_size <= 2^30); entries behind a sequence's
+ *                                 tokens are not read
  *   context [B]           int32   tokens of each sequence, its new rows among them (fewer than n_b: the first rows see nothing)
  *   cu_rows [B+1]         int32   rows of each sequence, cu_rows[B] <= T; rows of no sequence are left as they are
  *   scale                         finite

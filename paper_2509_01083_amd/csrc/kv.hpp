@@ -6,6 +6,7 @@
 namespace dsde {
 
 constexpr int32_t kMaxKvSeqs = 1 << 20;
+constexpr int64_t kMaxTokens = int64_t(1) << 30;  // of one sequence: a tile behind the last stays below 2^31
 constexpr int32_t kMinPage = 16, kMaxPage = 1024;
 
 // dsde_kv_map's workspace: the stack's height behind the pages given back, then per

@@ -102,7 +102,7 @@ int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, 
   const int64_t limit = int64_t(1) << 31;
   if (B < 1 || B > dsde::kMaxKvSeqs || shift_of(page_size) < 0 || pages < 1 || int64_t(pages) * page_size >= limit)
     return DSDE_INVALID_ARG;
-  if (width < 1 || int64_t(width) * page_size >= limit || rows < 0 || rows >= limit) return DSDE_INVALID_ARG;
+  if (width < 1 || int64_t(width) * page_size > dsde::kMaxTokens || rows < 0 || rows >= limit) return DSDE_INVALID_ARG;
   if (!sl || !kv_len || !table || !held || !free_pages || !n_free || !base || !context || !cu_rows || !seq_err || !workspace)
     return DSDE_INVALID_ARG;
   if (rows > 0 && (!slots || !positions)) return DSDE_INVALID_ARG;
@@ -152,7 +152,7 @@ int32_t dsde_kv_attention(const dsde_kv_cache *cache, const void *q, int64_t q_t
   if (q_heads < 1 || q_heads % cache->heads != 0 ||
       !attend_sizes_ok(B, cache->heads, q_heads / cache->heads, max_rows, cache->dim))
     return DSDE_INVALID_ARG;
-  if (T < 0 || T >= (int64_t(1) << 31) || width < 1 || int64_t(width) * cache->page_size >= (int64_t(1) << 31))
+  if (T < 0 || T >= (int64_t(1) << 31) || width < 1 || int64_t(width) * cache->page_size > dsde::kMaxTokens)
     return DSDE_INVALID_ARG;
   if (!isfinite(scale) || window < 0) return DSDE_INVALID_ARG;
   if (!table || !context || !cu_rows || !seq_err || !workspace || (T > 0 && (!q || !out))) return DSDE_INVALID_ARG;
