@@ -56,7 +56,9 @@ struct Shape {
   static constexpr int kKeys = 4 * kSub;                       // keys of a tile in a lane: 16 t + 4 g + i
   static constexpr int kQElt = CACHE == DSDE_FP32 ? 4 : 2;
   static constexpr int kQChunks = DP * kQElt / 64;             // 16-byte chunks of a query row in a lane
-  // where rows and accumulators are many, the rows at hand are in LDS, and the next item's are not fetched early
+  // where rows and accumulators are many, the rows at hand are in LDS, or the next item's are not fetched early either:
+  // a spill of a few registers in the loop costs more (12 % with 48 rows of 128)
+  static constexpr bool kRowsInLds = MT * DP * kQElt > 512;
   static constexpr bool kAhead = MT * DP * kQElt <= 768;
   // first dimension of a chunk: those that the keys' chunks hold
   __device__ static __forceinline__ int32_t q_dim(int i, int g) {
@@ -225,19 +227,19 @@ struct Wave {
   int32_t hi_all, lo_all;  // seen by every row
   int32_t hi_any, lo_any;  // seen by any
   float c;                 // scale log2(e), with the keys' scale, positive
-  Words<4> q[S::kAhead ? MT : 1][S::kAhead ? S::kQChunks : 1];
+  Words<4> q[S::kRowsInLds ? 1 : MT][S::kRowsInLds ? 1 : S::kQChunks];
   Words<4> (*q_lds)[64];   // [MT * kQChunks][64]: each lane its own
   f32x4 o[MT][S::kSets][S::kVec];
   float m[MT], l[MT];
-  // which of a lane's values have a NaN, +inf or -inf in their sum, a bit each (add_odd)
+  // which of a lane's values have +inf, and which -inf in their sum, a bit each, NaN as both (add_odd)
   static constexpr int kBits = (DP + 127) / 128;
-  uint32_t special[3][MT][kBits];
+  uint32_t special[2][MT][kBits];
   // keys and values of a tile
   Words<4> k[S::kSub][S::kChunks];
   Words<S::kVecWords> v[S::kKeys][S::kSets];
 
   __device__ __forceinline__ Words<4> &row(int mt, int i) {
-    if constexpr (S::kAhead) return q[mt][i];
+    if constexpr (!S::kRowsInLds) return q[mt][i];
     return q_lds[mt * S::kQChunks + i][16 * g + r];
   }
 
@@ -287,37 +289,47 @@ struct Wave {
       }
     }
   }
-  // An item's rows; for rows and dimensions that are none, others that are, which begin() drops.
-  __device__ __forceinline__ void load_q(const Item &x, Words<4> (&ahead)[MT][S::kQChunks]) const {
+  // An item's rows: a lane's chunk of one, in memory; for rows and dimensions that are none, another one's.
+  __device__ __forceinline__ const u32x4 *q_chunk(const Item &x, int mt, int i) const {
     const char *base = a.q.data + x.s.row0 * a.q.token_stride + int64_t(x.h) * a.group * a.q.head_stride;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int32_t row = (x.block * MT + mt) * 16 + r, at = row < x.s.n * a.group ? row : 0, j = at / a.group;
-      const char *p = base + j * a.q.token_stride + (at - j * a.group) * a.q.head_stride;
-#pragma unroll
-      for (int i = 0; i < S::kQChunks; ++i) {
-        const int32_t d = S::q_dim(i, g);
-        const u32x4 y = *reinterpret_cast<const u32x4 *>(p + (d < a.cache.dim ? d : 0) * S::kQElt);
-        ahead[mt][i] = Words<4>{{y.x, y.y, y.z, y.w}};
-      }
-    }
+    const int32_t row = (x.block * MT + mt) * 16 + r, at = row < x.s.n * a.group ? row : 0, j = at / a.group, d = S::q_dim(i, g);
+    return reinterpret_cast<const u32x4 *>(base + j * a.q.token_stride + (at - j * a.group) * a.q.head_stride +
+                                           (d < a.cache.dim ? d : 0) * S::kQElt);
   }
-  // Takes over an item's loaded rows.  A negative scale turns their signs, one of 0 makes them 0.
+  __device__ __forceinline__ void load_q(const Item &x, Words<4> (&ahead)[MT][S::kQChunks]) const {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < S::kQChunks; ++i) ahead[mt][i] = __builtin_bit_cast(Words<4>, *q_chunk(x, mt, i));
+  }
+  // Takes over an item's rows, loaded or (kAhead false) from memory.  A negative scale turns their signs, one of 0 makes
+  // them 0.
   __device__ __forceinline__ void take_q(const Item &x, const Words<4> (&ahead)[MT][S::kQChunks]) {
     const float f = a.scale * kLog2e * (CACHE == DSDE_E4M3 ? a.cache.k_scale[x.h] : 1.0f);
     const bool flat = fabsf(f) < 0x1p-126f;
     const uint32_t flip = f < 0.0f ? (CACHE == DSDE_FP32 ? 0x80000000u : 0x80008000u) : 0u;
     c = flat ? 1.0f : fabsf(f);
+    const auto put = [&](int mt, int i, const Words<4> &y) {
+      const bool there = (x.block * MT + mt) * 16 + r < x.s.n * a.group && !flat && S::q_dim(i, g) < a.cache.dim;
+      Words<4> z;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const bool live = (x.block * MT + mt) * 16 + r < x.s.n * a.group;
+      for (int e = 0; e < 4; ++e) z.w[e] = there ? y.w[e] ^ flip : 0u;
+      row(mt, i) = z;
+    };
+    if constexpr (S::kAhead) {
 #pragma unroll
-      for (int i = 0; i < S::kQChunks; ++i) {
-        const bool there = live && !flat && S::q_dim(i, g) < a.cache.dim;
-        Words<4> x;
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x.w[e] = there ? ahead[mt][i].w[e] ^ flip : 0u;
-        row(mt, i) = x;
+        for (int i = 0; i < S::kQChunks; ++i) put(mt, i, ahead[mt][i]);
+    } else {  // eight chunks at a time
+      static_assert(S::kAhead || MT * S::kQChunks % 8 == 0, "whole turns");
+#pragma unroll 1
+      for (int k = 0; k < MT * S::kQChunks; k += 8) {
+        Words<4> y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = __builtin_bit_cast(Words<4>, *q_chunk(x, (k + i) / S::kQChunks, (k + i) % S::kQChunks));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put((k + i) / S::kQChunks, (k + i) % S::kQChunks, y[i]);
       }
     }
   }
@@ -334,7 +346,7 @@ struct Wave {
       lo[mt] = a.window > 0 && hi[mt] >= a.window ? hi[mt] - a.window + 1 : 0;
       m[mt] = -INFINITY, l[mt] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kBits; ++i) special[0][mt][i] = special[1][mt][i] = special[2][mt][i] = 0;
+      for (int i = 0; i < kBits; ++i) special[0][mt][i] = special[1][mt][i] = 0;
 #pragma unroll
       for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
@@ -373,9 +385,8 @@ struct Wave {
     }
   }
 
-  // Raises references (in the log2 domain) where scores pass them, and turns scores into weights; those of a bad page,
-  // whose keys read as 0, into NaN.
-  __device__ __forceinline__ void weigh(f32x4 (&x)[MT][S::kSub], const At (&at)[S::kSub]) {
+  // Raises references (in the log2 domain) where scores pass them, and turns scores into weights.
+  __device__ __forceinline__ void weigh(f32x4 (&x)[MT][S::kSub]) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float top = -INFINITY;
@@ -398,9 +409,8 @@ struct Wave {
       float sum = 0.0f;
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) {
-        const float f = at[t].bad ? NAN : c;
-        x[mt][t] = f32x4{exp2_fast(fmaf(x[mt][t].x, f, -ref)), exp2_fast(fmaf(x[mt][t].y, f, -ref)),
-                         exp2_fast(fmaf(x[mt][t].z, f, -ref)), exp2_fast(fmaf(x[mt][t].w, f, -ref))};
+        x[mt][t] = f32x4{exp2_fast(fmaf(x[mt][t].x, c, -ref)), exp2_fast(fmaf(x[mt][t].y, c, -ref)),
+                         exp2_fast(fmaf(x[mt][t].z, c, -ref)), exp2_fast(fmaf(x[mt][t].w, c, -ref))};
         sum += (x[mt][t].x + x[mt][t].y) + (x[mt][t].z + x[mt][t].w);
       }
       l[mt] += sum;
@@ -474,16 +484,18 @@ struct Wave {
     }
   }
 
-  // Scores that some row does not see.
-  __device__ __forceinline__ void mask(f32x4 (&x)[MT][S::kSub], int32_t tile) {
+  // Scores that some row does not see, or of a bad page.
+  __device__ __forceinline__ void mask(f32x4 (&x)[MT][S::kSub], int32_t tile, const At (&at)[S::kSub]) {
 #pragma unroll
-    for (int t = 0; t < S::kSub; ++t)
+    for (int t = 0; t < S::kSub; ++t) {
+      const float f = at[t].bad ? NAN : 1.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= lo[mt] && key <= hi[mt] ? x[mt][t][i] : -INFINITY;
+        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= lo[mt] && key <= hi[mt] ? x[mt][t][i] * f : -INFINITY;
       }
+    }
   }
   // The same for values, as a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0;
   // others that are not finite (rare) too, once the rows that see them have them.
@@ -504,16 +516,16 @@ struct Wave {
     if (__any(odd)) add_odd(tile);
   }
   __device__ static constexpr int bit(int e, int j, int i) { return (e * S::kVec + j) * 4 + i; }
-  // For NaN, +inf and -inf in turn: how many such values of each dimension a row sees, a product of ones and zeros.  A
-  // sum with one of them is it, whatever the weights (NaN with both infinities), so a bit is enough until the end; the
-  // accumulators have no second place among the registers here.
+  // For +inf and -inf in turn, NaN counting as either: how many such values of each dimension a row sees, a product of
+  // ones and zeros.  A sum with one of them is it, whatever the weights (NaN with both), so a bit is enough until the
+  // end; the accumulators have no second place among the registers here.
   __device__ __forceinline__ void add_odd(int32_t tile) {
     const auto sees = [&](int mt, int t, int i) {
       const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
       return key >= lo[mt] && key <= hi[mt];
     };
 #pragma unroll 1
-    for (int kind = 0; kind < 3; ++kind) {
+    for (int kind = 0; kind < 2; ++kind) {
       // nothing is to be worked out before the loop and kept: registers are scarce on all ways to here
 #pragma unroll
       for (int i = 0; i < S::kKeys; ++i)
@@ -543,7 +555,7 @@ struct Wave {
 #pragma unroll
               for (int i = 0; i < S::kKeys; ++i) {
                 const float y = __uint_as_float(v[i][e].w[j]);
-                const bool is = kind == 0 ? y != y : y == (kind == 1 ? INFINITY : -INFINITY);
+                const bool is = y != y || y == (kind == 0 ? INFINITY : -INFINITY);
                 count = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.0f : 0.0f, sees(mt, i / 4, i % 4) ? 1.0f : 0.0f, count, 0, 0, 0);
               }
               put(mt, e, j, count);
@@ -554,7 +566,7 @@ struct Wave {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const auto one = [&](uint32_t h) {
-              return (kind == 0 ? (h & 0x7fffu) > 0x7f80u : h == (kind == 1 ? 0x7f80u : 0xff80u)) ? 0x3f80u : 0u;
+              return (h & 0x7fffu) > 0x7f80u || h == (kind == 0 ? 0x7f80u : 0xff80u) ? 0x3f80u : 0u;
             };
             x.w[i] = one(x.w[i] & 0xffffu) | one(x.w[i] >> 16) << 16;
           }
@@ -593,7 +605,6 @@ struct Wave {
         for (int i = 0; i < kBits; ++i) {
           special[0][mt][i] |= kind == 0 ? bits[mt][i] : 0u;
           special[1][mt][i] |= kind == 1 ? bits[mt][i] : 0u;
-          special[2][mt][i] |= kind == 2 ? bits[mt][i] : 0u;
         }
     }
 #pragma unroll
@@ -617,7 +628,7 @@ struct Wave {
       if (x.s.err) sum = NAN;  // a context that is none
       uint32_t any = 0;
 #pragma unroll
-      for (int i = 0; i < kBits; ++i) any |= special[0][mt][i] | special[1][mt][i] | special[2][mt][i];
+      for (int i = 0; i < kBits; ++i) any |= special[0][mt][i] | special[1][mt][i];
       const bool odd = __any(any != 0);
       if (row < x.s.n * a.group) {
         float f = 1.0f;
@@ -635,9 +646,8 @@ struct Wave {
 #pragma unroll
               for (int j = 0; j < S::kVec; ++j) {
                 const int w = bit(e, j, i) / 32, at = bit(e, j, i) % 32;
-                y[j] += special[0][mt][w] >> at & 1 ? NAN : 0.0f;
-                y[j] += special[1][mt][w] >> at & 1 ? INFINITY : 0.0f;
-                y[j] -= special[2][mt][w] >> at & 1 ? INFINITY : 0.0f;
+                y[j] += special[0][mt][w] >> at & 1 ? INFINITY : 0.0f;
+                y[j] -= special[1][mt][w] >> at & 1 ? INFINITY : 0.0f;
               }
             }
             if (done) {
@@ -745,12 +755,12 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
   };
   take(x, tile);
 
-  constexpr int kLds = S::kAhead ? 1 : MT * S::kQChunks;
-  __shared__ Words<4> s_q[S::kAhead ? 1 : kAttendWaves][kLds][64];
-  Wave<CACHE, DP, MT> w(a, lane, s_q[S::kAhead ? 0 : wave]);
+  constexpr int kLds = S::kRowsInLds ? MT * S::kQChunks : 1;
+  __shared__ Words<4> s_q[S::kRowsInLds ? kAttendWaves : 1][kLds][64];
+  Wave<CACHE, DP, MT> w(a, lane, s_q[S::kRowsInLds ? wave : 0]);
   At now[S::kSub], next[S::kSub];
   Words<4> ahead[MT][S::kQChunks];
-  w.load_q(x, ahead);
+  if (S::kAhead) w.load_q(x, ahead);
 #pragma unroll
   for (int t = 0; t < S::kSub; ++t) now[t] = w.locate(x, x.first, t, true);
   w.load_k(now);
@@ -784,7 +794,7 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
     // behind the last of all is none.
     int32_t tile = x.first;
     do {
-      if (!S::kAhead) asm volatile("" : : : "memory");  // rows are read from LDS for every tile, not kept
+      if (S::kRowsInLds) asm volatile("" : : : "memory");  // rows are read from LDS for every tile, not kept
       w.load_v(now);
       const bool last = tile + 1 == x.end;
 #pragma unroll
@@ -792,15 +802,16 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
       f32x4 p[MT][S::kSub];
       w.scores(p);
       w.load_k(next);
-      const bool clear = tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
-      if (!clear) w.mask(p, tile);
-      w.weigh(p, now);
+      bool clear = tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
+#pragma unroll
+      for (int t = 0; t < S::kSub; ++t) clear &= !now[t].bad;
+      if (!clear) w.mask(p, tile, now);
+      w.weigh(p);
       if (!clear) w.mask_values(tile);
       w.add(p);
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) now[t] = next[t];
     } while (++tile < x.end);
-    if (!S::kAhead) w.load_q(y, ahead);
     w.take_q(y, ahead);  // before the stores, which its wait would count
     w.end(x, part_of(a, at.parts, worker, x.first > x.s.tile0 ? 0 : 1, kPart));
     if (!more) return;

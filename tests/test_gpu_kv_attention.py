@@ -252,6 +252,61 @@ def test_faults_are_flagged(gpu_lib, dtype):
     assert got["seq_err"].tolist() == [1, 0, 0, 0, 0, 0, 0]
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_before_a_bad_page_are_unharmed(gpu_lib, dtype):
+    """Rows of tokens 44 .. 52, the page of 48 on bad: those before it are as they were, in one head's item and in parts."""
+    for c, n, bad in ((53, 9, 3), (2003, 9, 125), (700, 33, 42)):
+        x = make([c], [n], H=1, G=2, D=64, dtype=dtype, junk=False)
+        y = to_gpu(x)
+        want = gpu_lib.kv_attention(**y, lse=True)
+        for page in (-1, x["k"].shape[0]):
+            y["table"][0, bad] = page
+            got = gpu_lib.kv_attention(**y, lse=True)
+            assert got["seq_err"].tolist() == [256]
+            for j in range(n):
+                if c - n + j >= 16 * bad:
+                    assert bool(torch.isnan(got["out"][j]).all()) and bool(torch.isnan(got["lse"][j]).all()), j
+                else:
+                    assert torch.equal(got["out"][j], want["out"][j]) and torch.equal(got["lse"][j], want["lse"][j]), j
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_infinite_values_of_both_signs(gpu_lib, dtype):
+    """+inf, then -inf in one dimension: inf, then NaN; alone in others; in the last tile of a long cache too."""
+    for c in (64, 1500):
+        x = make([c], [4], H=2, G=3, D=128, dtype=dtype, junk=False)
+        for at, d, value in ((c - 3, 5, math.inf), (c - 2, 5, -math.inf), (c - 2, 100, -math.inf), (c - 1, 64, math.inf)):
+            x["v"][int(x["table"][0, at // 16]), 1, at % 16, d] = value
+        o = gpu_lib.kv_attention(**to_gpu(x))["out"][:, 3:].float().cpu()  # the second key head's
+        assert bool(torch.isfinite(o[0]).all())
+        assert bool((o[1, :, 5] == math.inf).all()) and bool(torch.isnan(o[2:, :, 5]).all())
+        assert bool((o[2:, :, 100] == -math.inf).all()) and bool((o[3, :, 64] == math.inf).all())
+        o[:, :, [5, 64, 100]] = 0
+        assert bool(torch.isfinite(o).all())
+
+
+def test_one_page_for_many(gpu_lib):
+    """Sequences that share pages, and one whose table is the same page throughout: 2^20 tokens of a cache of 64."""
+    g = torch.Generator().manual_seed(4)
+    k, v = (torch.randn(4, 1, 16, 16, generator=g) for _ in range(2))
+    n = 1 << 16
+    table = torch.zeros(2, n, dtype=torch.int32)
+    table[1] = torch.arange(n) % 4
+    q = torch.randn(2, 1, 16, generator=g)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    got = gpu_lib.kv_attention(q.cuda(), k.cuda(), v.cuda(), table.cuda(), torch.tensor([16 * n, 16 * n], **i32),
+                               torch.tensor([0, 1, 2], **i32), 1, lse=True)
+    for b, (kk, vv, times) in enumerate(((k[0, 0], v[0, 0], n), (k[:, 0].reshape(64, 16), v[:, 0].reshape(64, 16), n // 4))):
+        z = kk.double() @ q[b, 0].double() / 4
+        want = torch.softmax(z, 0) @ vv.double()
+        # sums of 2^20 weights: 2^20 / 64 of a lane in a row at most 2^14 2^-24 off, of values of size sum p |v|
+        A = torch.softmax(z, 0) @ vv.double().abs()
+        assert bool(((got["out"][b, 0].cpu().double() - want).abs() <= 2.0 ** -10 * A).all())
+        lse = torch.logsumexp(z, 0) + math.log(times)
+        assert abs(float(got["lse"][b, 0]) - float(lse)) <= 2.0 ** -10
+    assert not got["seq_err"].any()
+
+
 def test_calls_repeat_bit_for_bit(gpu_lib):
     g = torch.Generator().manual_seed(1)
     lens = torch.randint(1, 900, (50,), generator=g).tolist()
