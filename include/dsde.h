@@ -667,7 +667,7 @@ size_t dsde_kv_attention_workspace_bytes(int32_t B, int32_t heads, int32_t group
  *                                 tokens are not read
  *   context [B]           int32   tokens of each sequence, its new rows among them (fewer than n_b: the first rows see nothing)
  *   cu_rows [B+1]         int32   rows of each sequence, cu_rows[B] <= T; rows of no sequence are left as they are
- *   scale                         finite
+ *   scale                         finite, and 1.45 times it too
  *   window                        >= 0
  * Outputs:
  *   out [T, q_heads, dim] dtype   each value rounded once, from fp32

@@ -81,7 +81,7 @@ def test_write_refuses(dsde):
 def test_attention_refuses(dsde):
     bad = [dict(dtype=0), dict(dtype=2), dict(q_heads=0), dict(q_heads=12), dict(q_heads=1032), dict(T=-1), dict(T=1 << 31),
            dict(B=0), dict(B=(1 << 20) + 1), dict(max_rows=0), dict(max_rows=65), dict(width=0), dict(width=1 << 27),
-           dict(width=(1 << 26) + 1), dict(scale=float("nan")), dict(scale=float("inf")), dict(window=-1), dict(q=ODD), dict(out=ODD), dict(ws=ODD),
+           dict(width=(1 << 26) + 1), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(scale=-2.4e38), dict(window=-1), dict(q=ODD), dict(out=ODD), dict(ws=ODD),
            dict(q_token=4097), dict(q_head=-128), dict(out_token=4100), dict(out_token=2048), dict(out_head=64), dict(out_head=0)]
     bad += [{k: None} for k, v in ATTEND.items() if isinstance(v, ctypes.c_void_p)]
     for over in bad:
