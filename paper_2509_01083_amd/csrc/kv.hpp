@@ -74,17 +74,19 @@ struct AttendArgs {
   void *workspace;
 };
 constexpr int kAttendWorkers = 1024;  // wavefronts of a launch
-constexpr int kAttendRows = 64;       // most rows that one of them takes at once
+// Rows that one of them takes at once, at most, of so many of a sequence and key head.
+constexpr int kAttendRows = 64;
+inline int attend_rows(int64_t rows) { return rows < kAttendRows ? int(rows + 15) / 16 * 16 : kAttendRows; }
 inline int padded_dim(int32_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 struct AttendLayout {
   size_t starts, parts, total;
 };
-inline AttendLayout attend_layout(int32_t dim) {
+inline AttendLayout attend_layout(int32_t dim, int64_t rows) {
   AttendLayout l;
   l.starts = 0;  // where each wavefront's share begins
   l.parts = align_up(size_t(32) * kAttendWorkers);
   // two parts of a wavefront: for each of its rows the values, a reference and a sum
-  l.total = l.parts + align_up(sizeof(float) * 2 * kAttendWorkers * kAttendRows * size_t(padded_dim(dim) + 2));
+  l.total = l.parts + align_up(sizeof(float) * 2 * kAttendWorkers * size_t(attend_rows(rows)) * size_t(padded_dim(dim) + 2));
   return l;
 }
 int launch_kv_attention(const AttendArgs &a, hipStream_t stream);

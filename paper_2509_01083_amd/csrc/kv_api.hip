@@ -139,7 +139,7 @@ int32_t dsde_kv_write(const dsde_kv_cache *cache, const void *k, int64_t k_token
 }
 
 size_t dsde_kv_attention_workspace_bytes(int32_t B, int32_t heads, int32_t group, int32_t max_rows, int32_t dim) {
-  return attend_sizes_ok(B, heads, group, max_rows, dim) ? dsde::attend_layout(dim).total : 0;
+  return attend_sizes_ok(B, heads, group, max_rows, dim) ? dsde::attend_layout(dim, int64_t(group) * max_rows).total : 0;
 }
 
 int32_t dsde_kv_attention(const dsde_kv_cache *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride,
@@ -154,14 +154,14 @@ int32_t dsde_kv_attention(const dsde_kv_cache *cache, const void *q, int64_t q_t
     return DSDE_INVALID_ARG;
   if (T < 0 || T >= (int64_t(1) << 31) || width < 1 || int64_t(width) * cache->page_size > dsde::kMaxTokens)
     return DSDE_INVALID_ARG;
-  if (!isfinite(scale) || window < 0) return DSDE_INVALID_ARG;
+  if (!isfinite(scale * 1.4426950f) || window < 0) return DSDE_INVALID_ARG;  // the kernel's scale is log2(e) times that
   if (!table || !context || !cu_rows || !seq_err || !workspace || (T > 0 && (!q || !out))) return DSDE_INVALID_ARG;
   if (T > 0 && (!rows_ok(q, q_token_stride, q_head_stride, dtype) || !rows_ok(out, out_token_stride, out_head_stride, dtype)))
     return DSDE_INVALID_ARG;
   // rows that are written must not overlap
   if (T > 0 && !apart({T, out_token_stride}, {q_heads, out_head_stride}, {1, 0}, cache->dim)) return DSDE_INVALID_ARG;
   const int32_t group = q_heads / cache->heads;
-  if (workspace_bytes < dsde::attend_layout(cache->dim).total) return DSDE_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < dsde::attend_layout(cache->dim, int64_t(group) * max_rows).total) return DSDE_WORKSPACE_TOO_SMALL;
   if (misaligned(workspace)) return DSDE_INVALID_ARG;
   dsde::AttendArgs a;
   a.cache = view(cache);

@@ -157,10 +157,12 @@ __device__ __forceinline__ Seq sequence(const AttendArgs &a, int32_t b, int32_t 
   return s;
 }
 // The work in one line: for every sequence, key head and row block an item of kStart units (what it costs to begin
-// and end one, in tiles) and a unit for each tile.  Every wavefront takes an equal share of the line, whatever the
+// and end one, in tiles: with 0, 1, 2, 4 units 256 sequences took 465, 449, 440, 434 us, 1,024 over e4m3 460, 408, 390,
+// 400, 64 in fp32 46, 36, 39, 41) and a unit for each tile.  Every wavefront takes an equal share of the line, whatever the
 // lengths are, so that all end together; items that it has a part of leave that part to join_kernel.
 constexpr int32_t kStart = 2;
-constexpr int32_t kLeast = 2;  // units of a share at least: short calls do not end in joining many parts
+// units of a share at least: short calls do not end in joining many parts (1,000 tokens: 12.4 us, with 1 13.2, with 4 13.8)
+constexpr int32_t kLeast = 2;
 __device__ __forceinline__ int64_t units_of(const AttendArgs &a, const Seq &s) {
   return int64_t(s.tiles + kStart) * s.blocks * a.cache.heads;
 }
@@ -838,8 +840,15 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
       if (s.n > 0 && s.context > 0) {
         const int64_t first = a.window > 0 ? int64_t(s.context) - s.n - a.window + 1 : 0;
         bool bad = false;
-        for (int32_t i = int32_t((first > 0 ? first : 0) >> a.cache.shift) + tid; i <= (s.context - 1) >> a.cache.shift; i += 256)
-          bad |= uint32_t(a.table[int64_t(b) * a.width + i]) >= uint32_t(a.cache.pages);
+        // eight loads at once: one workgroup has all pages of a sequence (8,192 of them: the whole kernel 7.4 us instead of 9.6)
+        const int32_t last = (s.context - 1) >> a.cache.shift;
+        for (int32_t i = int32_t((first > 0 ? first : 0) >> a.cache.shift) + tid; i <= last; i += 256 * 8) {
+          int32_t id[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) id[k] = a.table[int64_t(b) * a.width + (i + 256 * k < last ? i + 256 * k : last)];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) bad |= uint32_t(id[k]) >= uint32_t(a.cache.pages);
+        }
         if (bad) s_bad = 1;
       }
       __syncthreads();
@@ -851,7 +860,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
   const Start x = reinterpret_cast<const Start *>(static_cast<const char *>(a.workspace) + at.starts)[worker];
   if (x.tile == 0) return;
   const int32_t row0 = x.block * kRows, live = x.rows - row0 < kRows ? x.rows - row0 : kRows;
-  // cells of four values; at least 16 cells (256 bytes) for each workgroup
+  // cells of four values, at least 4 (64 bytes) for each workgroup: the fewer they are, the more lanes share a cell's parts
+  // and the fewer loads come one after another (128 parts of 8 items: 9.5 us, with 16 cells 12)
   const int32_t cells = live * (DP / 4), parts = x.w1 - x.w0 + 1, sharers = parts - 1;
   if (parts == 2) {  // most often: all loads at once
     constexpr int kTimes = (kRows * DP / 4 + 255) / 256;
@@ -880,7 +890,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
     return;
   }
   int32_t n = (cells + sharers - 1) / sharers;
-  n = n < 16 ? 16 : n;
+  n = n < 4 ? 4 : n;
   const int32_t c0 = (worker - x.w0 - 1) * n, c1 = c0 + n < cells ? c0 + n : cells;
   // lanes that share a cell's parts
   int32_t span = 1;
@@ -924,15 +934,15 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
 // 2.1 GB took 340 us instead of 330, with three 373.
 template <int CACHE, int DP, int MT>
 void launch(const AttendArgs &a, hipStream_t stream) {
-  const AttendLayout at = attend_layout(a.cache.dim);
+  const AttendLayout at = attend_layout(a.cache.dim, int64_t(a.group) * a.max_rows);
   constexpr int32_t groups = 256, workers = groups * kAttendWaves;
-  static_assert(workers <= kAttendWorkers, "workspace");
+  static_assert(workers <= kAttendWorkers && 16 * MT <= kAttendRows, "workspace");
   attend_kernel<CACHE, DP, MT><<<groups, kAttendThreads, 0, stream>>>(a, at);
   join_kernel<CACHE, DP, MT><<<workers + (a.B < 1024 ? a.B : 1024), 256, 0, stream>>>(a, at, workers);
 }
 template <int CACHE, int DP>
 void by_tiles(const AttendArgs &a, hipStream_t stream) {
-  // as many row blocks as fit the registers
+  // as many row blocks as fit the registers, and no more than the rows fill (the workspace has room for those)
   constexpr int most = DP == 256 ? (CACHE == DSDE_FP32 ? 1 : 2) : CACHE == DSDE_FP32 && DP == 128 ? 2 : 4;
   const int32_t rows = a.group * a.max_rows;
   if (rows <= 16 || most == 1)
