@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kMapThreads = 1024, kMapWaves = kMapThreads / 64;
 constexpr int kSmallSeqs = 1024;     // sequences whose prefix sums stay in LDS
-constexpr int64_t kSmallRows = 8192;  // rows that the planning workgroup maps itself
+constexpr int64_t kSmallRows = 4096;  // rows that the planning workgroup maps itself
 constexpr int32_t kManyPages = 4096;  // more pages than it gives back itself where it can leave them
 
 struct Sums {
@@ -128,8 +128,9 @@ __device__ __forceinline__ void give_page(const MapArgs &a, const int32_t *back,
 }
 
 // The plan, by one workgroup: a chain of round trips to memory (the sequences' numbers, the pages that move, the pages
-// of the rows) and prefix sums between them.  ALL: it also takes the pages and maps the rows, which saves a launch (2 us)
-// where they are few; with more rows one CU takes longer than that.  LOCAL: one sequence to a thread, kept in
+// of the rows) and prefix sums between them.  ALL: it also takes the pages and maps the rows, which saves a launch
+// where they are few (512 rows: 6.1 us instead of 8.9, 4,096 of 1,024 sequences: 10.1 instead of 10.8); more take one CU
+// longer (8,192: 14.4 instead of 10.5).  LOCAL: one sequence to a thread, kept in
 // registers and LDS.  SHARED: give_kernel runs behind it (37,000 pages took this workgroup 31 us).
 template <bool ALL, bool LOCAL, bool SHARED>
 __global__ __launch_bounds__(kMapThreads) void map_plan_kernel(MapArgs a) {
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(256) void give_kernel(MapArgs a) {
 
 // Rows into slots, a wavefront per row of keys or values: 16 bytes of the cache per lane.  Bound by HBM: 81,000 rows of
 // 4 KiB take 140 to 148 us, 4.5 to 4.75 TB/s, the rate of a large copy.  PAST: stores past the L2s (nt), 2 to 7 % faster
-// where the rows are more than those hold (32 MiB); fewer rows are read sooner than they would leave them (a reader of
+// for more than twice what those hold (32 MiB); fewer rows are read sooner than they would leave them (a reader of
 // 17 MiB right behind took 10 us longer).
 using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
 __device__ __forceinline__ u32x4 load16(const char *from) { return *reinterpret_cast<const u32x4 *>(from); }
