@@ -42,9 +42,10 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 template <int CACHE, int DP, int MT>
 struct Shape {
   static constexpr int kElt = CACHE == DSDE_FP32 ? 4 : CACHE == DSDE_BF16 ? 2 : 1;
-  // subtiles of 16 keys: 16 KiB of keys and values at a time where registers allow
+  // subtiles of 16 keys: 16 KiB of keys and values at a time where registers allow (heads of 64 with 48 rows and more: 433
+  // and 488 us with four subtiles, 446 and 512 with two)
   static constexpr int kLeastSub = CACHE == DSDE_FP32 ? 1 : 2;
-  static constexpr int kMostSub = MT > 2 ? 2 : 4;
+  static constexpr int kMostSub = MT > 2 && DP > 64 ? 2 : 4;
   static constexpr int kSub = 512 / (DP * kElt) < kLeastSub ? kLeastSub : 512 / (DP * kElt) > kMostSub ? kMostSub : 512 / (DP * kElt);
   static constexpr int kTile = 16 * kSub;                      // keys of a step
   static constexpr int kPer16 = 16 / kElt;                     // elements in 16 bytes
