@@ -229,6 +229,7 @@ struct Wave {
   int32_t hi[MT], lo[MT];  // tokens that lane r's row of each block sees: lo .. hi
   int32_t hi_all, lo_all;  // seen by every row
   int32_t hi_any, lo_any;  // seen by any
+  int32_t live;            // blocks of 16 that have rows, the first ones
   float c;                 // scale log2(e), with the keys' scale, positive
   Words<4> q[S::kRowsInLds ? 1 : MT][S::kRowsInLds ? 1 : S::kQChunks];
   Words<4> (*q_lds)[64];   // [MT * kQChunks][64]: each lane its own
@@ -340,6 +341,8 @@ struct Wave {
   __device__ __forceinline__ void begin(const Item &x) {
     const int32_t newest = x.s.context - 1, oldest = x.s.context - x.s.n;
     hi_all = oldest, hi_any = newest;
+    const int32_t blocks = (x.s.n * a.group + 15) / 16 - x.block * MT;
+    live = blocks < MT ? blocks : MT;
     lo_all = a.window > 0 && newest >= a.window ? newest - a.window + 1 : 0;
     lo_any = a.window > 0 && oldest >= a.window ? oldest - a.window + 1 : 0;
 #pragma unroll
@@ -357,7 +360,18 @@ struct Wave {
     }
   }
 
+  // f for the blocks of 16 that have rows.  The fp32 instructions take eight times as long as bf16's, so that an empty
+  // second block is left out: 4 to 32 rows of 64 take 371 us instead of 439, of 128 404 instead of 502 (always 32 rows: 474 and
+  // 479 instead of 467 and 457).  With three or four blocks, or 16-bit products, the branches cost more than they save (3 to
+  // 6 %, or spills).
+  template <typename F>
+  __device__ __forceinline__ void of_live(F f) const {
+    if constexpr (CACHE == DSDE_FP32 && MT == 2)
+      if (live == 1) return f(std::integral_constant<int, 1>{});
+    f(std::integral_constant<int, MT>{});
+  }
   // Scores of a tile, without their scale.
+  template <int L>
   __device__ __forceinline__ void scores(f32x4 (&x)[MT][S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t) {
@@ -370,18 +384,18 @@ struct Wave {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < L; ++mt)
               x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), __uint_as_float(row(mt, j).w[e]), x[mt][t], 0, 0, 0);
         } else if constexpr (CACHE == DSDE_BF16) {
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(w), operand(row(mt, j)), x[mt][t], 0, 0, 0);
+          for (int mt = 0; mt < L; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(w), operand(row(mt, j)), x[mt][t], 0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const bf16x8 kk = operand(Words<4>{{widen<false>(w.w[2 * e]), widen<true>(w.w[2 * e]), widen<false>(w.w[2 * e + 1]),
                                                 widen<true>(w.w[2 * e + 1])}});
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(row(mt, 2 * j + e)), x[mt][t], 0, 0, 0);
+            for (int mt = 0; mt < L; ++mt) x[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, operand(row(mt, 2 * j + e)), x[mt][t], 0, 0, 0);
           }
         }
       }
@@ -389,9 +403,10 @@ struct Wave {
   }
 
   // Raises references (in the log2 domain) where scores pass them, and turns scores into weights.
+  template <int L>
   __device__ __forceinline__ void weigh(f32x4 (&x)[MT][S::kSub]) {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int mt = 0; mt < L; ++mt) {
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) top = fmaxf(fmaxf(fmaxf(x[mt][t].x, x[mt][t].y), fmaxf(x[mt][t].z, x[mt][t].w)), top);
@@ -441,6 +456,7 @@ struct Wave {
   // Adds the weights' values.  For 16-bit matrix instructions a weight is the sum of two bf16 numbers, good to 2^-17: one
   // alone would be off by as much as the output's own rounding (2.2e-3 of the norm of random rows' outputs instead of
   // 1.6e-3), and the second product takes no time that memory does not (0 to 1 % with up to 48 rows, 6 % with 64).
+  template <int L>
   __device__ __forceinline__ void add(const f32x4 (&p)[MT][S::kSub]) {
     if constexpr (CACHE == DSDE_FP32) {
 #pragma unroll
@@ -450,14 +466,14 @@ struct Wave {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int mt = 0; mt < L; ++mt)
               o[mt][e][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[i][e].w[j]), p[mt][i / 4][i % 4], o[mt][e][j], 0, 0, 0);
     } else {
 #pragma unroll
       for (int t = 0; t < S::kSub; t += 2) {
-        bf16x8 w[MT], rest[MT];
+        bf16x8 w[L], rest[L];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int mt = 0; mt < L; ++mt) {
           Words<4> hi, lo;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -474,7 +490,7 @@ struct Wave {
             Words<4> even, odd;
             pick(t, e, j2, even, odd);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            for (int mt = 0; mt < L; ++mt) {
               const auto both = [&](const Words<4> &v, f32x4 to) {
                 to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(v), w[mt], to, 0, 0, 0);
                 return __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(v), rest[mt], to, 0, 0, 0);
@@ -803,15 +819,15 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) next[t] = w.locate(last ? y : x, last ? y.first : tile + 1, t, !last || more);
       f32x4 p[MT][S::kSub];
-      w.scores(p);
+      w.of_live([&](auto n) { w.template scores<n.value>(p); });
       w.load_k(next);
       bool clear = tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) clear &= !now[t].bad;
       if (!clear) w.mask(p, tile, now);
-      w.weigh(p);
+      w.of_live([&](auto n) { w.template weigh<n.value>(p); });
       if (!clear) w.mask_values(tile);
-      w.add(p);
+      w.of_live([&](auto n) { w.template add<n.value>(p); });
 #pragma unroll
       for (int t = 0; t < S::kSub; ++t) now[t] = next[t];
     } while (++tile < x.end);

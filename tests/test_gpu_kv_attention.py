@@ -106,6 +106,16 @@ def test_rows_of_a_step(gpu_lib, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,G,most", [(64, 4, 8), (128, 4, 8), (64, 5, 9), (64, 7, 9)])
+def test_row_blocks_that_come_and_go(gpu_lib, D, G, most, dtype):
+    """Wavefronts that go from items with few rows to items with many, and back."""
+    g = torch.Generator().manual_seed(G * D)
+    lens = torch.randint(1, 120, (280,), generator=g).tolist()
+    n = torch.randint(0, most + 1, (280,), generator=g).tolist()
+    check(gpu_lib, make(lens, n, H=3, G=G, D=D, dtype=dtype, seed=G * D))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 31, 33, 64, 100, 1000])
 def test_windows(gpu_lib, window, dtype):
     check(gpu_lib, make([1, 16, 33, 150, 400], [1, 4, 9, 3, 5], dtype=dtype, seed=window), window=window)
