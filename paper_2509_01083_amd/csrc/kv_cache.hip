@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kMapThreads = 1024, kMapWaves = kMapThreads / 64;
 constexpr int kSmallSeqs = 1024;     // sequences whose prefix sums stay in LDS
-constexpr int64_t kSmallRows = 4096;  // rows that the planning workgroup maps itself
+constexpr int64_t kSmallRows = 6144;  // rows that the planning workgroup maps itself
 constexpr int32_t kManyPages = 4096;  // more pages than it gives back itself where it can leave them
 
 struct Sums {
@@ -129,8 +129,8 @@ __device__ __forceinline__ void give_page(const MapArgs &a, const int32_t *back,
 
 // The plan, by one workgroup: a chain of round trips to memory (the sequences' numbers, the pages that move, the pages
 // of the rows) and prefix sums between them.  ALL: it also takes the pages and maps the rows, which saves a launch
-// where they are few (512 rows: 6.1 us instead of 8.9, 4,096 of 1,024 sequences: 10.1 instead of 10.8); more take one CU
-// longer (8,192: 14.4 instead of 10.5).  LOCAL: one sequence to a thread, kept in
+// where they are few (512 rows: 6.1 us instead of 8.9, 4,096 of 1,024 sequences 10.1 instead of 10.8, and where many take a
+// page 1.5 less); more take one CU longer (8,192: 14.4 instead of 10.5, with pages 2 more; the two meet at 4,600 and 7,000).  LOCAL: one sequence to a thread, kept in
 // registers and LDS.  SHARED: give_kernel runs behind it (37,000 pages took this workgroup 31 us).
 template <bool ALL, bool LOCAL, bool SHARED>
 __global__ __launch_bounds__(kMapThreads) void map_plan_kernel(MapArgs a) {
