@@ -155,6 +155,36 @@ def test_page_ids_out_of_range(gpu_lib):
     assert got["seq_err"].tolist() == [256, 256, 0]  # the third takes page 5
 
 
+@pytest.mark.parametrize("B", [130, 1500])
+@pytest.mark.parametrize("fault", ["spare 0", "spare 60", "n_free", "held", "ids", "sl"])
+def test_faults_with_much_room(gpu_lib, B, fault):
+    """The same outcomes where the whole card maps the rows."""
+    r = random.Random(B)
+    W, page = 9, 16
+    P = B * W
+    lens, pool = state(r, B, W, page, P, 80, int(fault[6:]) if fault.startswith("spare") else None)
+    sl = [r.randrange(0, 40) for _ in range(B)]
+    if fault == "n_free":
+        pool["n_free"] = [P + 1]
+    elif fault == "held":
+        pool["held"][:2], pool["held"][-1] = [-1, W + 1], 2 ** 31 - 1
+    elif fault == "ids":
+        for b in range(0, B, 3):
+            pool["table"][b] = [x if x < 0 or r.random() < 0.5 else r.choice([P, -1, -2 ** 31, 2 ** 31 - 1]) for x in pool["table"][b]]
+    elif fault == "sl":
+        sl[:3], sl[-1] = [-2, 2 ** 31 - 2, 2 ** 31 - 2], -5
+    gpu = to_gpu(pool)
+    got = gpu_lib.kv_map(torch.tensor(sl, **I32), torch.tensor(lens, **I32), gpu, page, 100_000)
+    torch.cuda.synchronize()
+    new, want = R.kv_map(sl, 1, lens, [-1] * B, pool["table"], pool["held"], pool["free"], pool["n_free"][0], page, P, 100_000)
+    want["cu_rows"] = [min(x, 2 ** 31 - 1) for x in want["cu_rows"]]
+    for k, v in want.items():
+        assert got[k].tolist() == v, k
+    for k, v in new.items():
+        assert gpu[k].tolist() == v, k
+    assert any(want["seq_err"]) or (fault, B) == ("spare 60", 130)  # where 60 pages are enough
+
+
 def test_lengths_advance_in_place(gpu_lib):
     lens = torch.tensor([5, 0, 77], **I32)
     pool = gpu_lib.new_kv_pool(3, 8, 24)
