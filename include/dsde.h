@@ -639,7 +639,7 @@ typedef struct {
 } dsde_kv_cache;
 
 /*
- * Keys and values into their slots.
+ * Keys and values into their slots; the two must not lie in the same memory (which attention alone allows).
  *   k, v [T, heads, dim]  dtype   row t, head h at t * token_stride + h * head_stride (of each)
  *   dtype                         the cache's type, or DSDE_BF16 for a DSDE_E4M3 cache, which then takes
  *                                 x / scale (in fp32) rounded to the nearest, ties to even, at most +-448; NaN stays NaN

@@ -120,7 +120,7 @@ int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, 
 int32_t dsde_kv_write(const dsde_kv_cache *cache, const void *k, int64_t k_token_stride, int64_t k_head_stride,
                       const void *v, int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, int64_t T,
                       const int32_t *slots, uint32_t *row_err, void *stream) {
-  if (!cache_ok(cache) || (dtype != DSDE_FP32 && dtype != DSDE_BF16) || !types_match(cache, dtype))
+  if (!cache_ok(cache) || cache->k == cache->v || (dtype != DSDE_FP32 && dtype != DSDE_BF16) || !types_match(cache, dtype))
     return DSDE_INVALID_ARG;
   if (T < 0 || T >= (int64_t(1) << 31)) return DSDE_INVALID_ARG;
   if (T == 0) return DSDE_OK;

@@ -74,6 +74,7 @@ def test_write_refuses(dsde):
         assert rc(dsde, "dsde_kv_write", dict(WRITE, **over)) == 1, over
     e4m3 = dict(dtype=2, k_scale=0x1000, v_scale=0x1000)
     assert rc(dsde, "dsde_kv_write", dict(WRITE, dtype=0), e4m3) == 1
+    assert rc(dsde, "dsde_kv_write", WRITE, dict(v=GOOD["k"])) == 1  # keys and values in one place
     none = dict(WRITE, T=0, k=None, v=None, slots=None, err=None)
     assert rc(dsde, "dsde_kv_write", none) == 0 and rc(dsde, "dsde_kv_write", none, e4m3) == 0
 
