@@ -659,6 +659,10 @@ size_t dsde_kv_attention_workspace_bytes(int32_t B, int32_t heads, int32_t group
  * p = context[b] - n_b + j and sees the tokens t <= p of the sequence, with a window > 0 those with t > p - window:
  *   s_t = scale * q . k_t,  lse = log sum_t exp s_t,  out = sum_t exp(s_t - lse) v_t
  * A row that sees nothing has out 0 and lse -inf.  Nothing that a row does not see has an effect on it, whatever it holds.
+ * Of a value that it sees and that is not finite, out is that value in the dimension, whatever its weight (one that
+ * underflows to 0 too): inf or -inf, NaN with both or with a NaN; no other dimension is affected.  A score that is NaN or
+ * +inf makes the row NaN, one of -inf is a weight of 0.  The sums are fp32, of weights up to 2^8 times the largest: where
+ * the sizes of a dimension's finite values add up to 2^120 and more, out may be inf or NaN there.
  *
  *   q [T, q_heads, dim]   dtype   the cache's type, or DSDE_BF16 for DSDE_E4M3; q_heads a multiple of cache->heads:
  *                                 query head h reads key head h / (q_heads / heads)

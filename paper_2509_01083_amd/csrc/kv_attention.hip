@@ -104,27 +104,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, p);
 }
 __device__ __forceinline__ bf16x8 operand(const Words<4> &x) { return __builtin_bit_cast(bf16x8, x); }
+// The values of a word that are not finite: the highest bit of each.  Their exponent (e4m3: all but the sign) is all ones.
 template <int CACHE>
-__device__ __forceinline__ bool not_finite(uint32_t x) {
-  if constexpr (CACHE == DSDE_FP32) return (x & 0x7f800000u) == 0x7f800000u;
-  if constexpr (CACHE == DSDE_BF16) return (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
-  const uint32_t y = ~x & 0x7f7f7f7fu;  // a byte of 0: NaN
-  return ((y - 0x01010101u) & ~y & 0x80808080u) != 0;
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+  if constexpr (CACHE == DSDE_FP32) return ((x & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+  if constexpr (CACHE == DSDE_BF16) return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
-
-// The same word with its values that are not finite at 0.
+// The same word with those values at 0.
 template <int CACHE>
 __device__ __forceinline__ uint32_t finite_only(uint32_t x) {
-  if constexpr (CACHE == DSDE_FP32) return not_finite<CACHE>(x) ? 0u : x;
-  constexpr uint32_t part = CACHE == DSDE_BF16 ? 0xffffu : 0xffu;
-  uint32_t y = 0;
-#pragma unroll
-  for (int at = 0; at < 32; at += CACHE == DSDE_BF16 ? 16 : 8) {
-    const uint32_t one = x & (part << at);
-    // the rest of the word as 0 is finite
-    y |= not_finite<CACHE>(one) ? 0u : one;
-  }
-  return y;
+  constexpr int kTop = CACHE == DSDE_FP32 ? 31 : CACHE == DSDE_BF16 ? 15 : 7;
+  return x & ~((not_finite<CACHE>(x) >> kTop) * ((2u << kTop) - 1));
 }
 
 // One sequence of a call.
@@ -206,6 +197,12 @@ __device__ __forceinline__ char *finished(const AttendArgs &a, int32_t row0, int
   return a.out + t * a.out_token_stride + int64_t(head) * a.out_head_stride;
 }
 
+// A sum that is not finite stays what it is, whatever part of the whole it has (NaN: none is known).
+__device__ __forceinline__ float carried(float o, float f) { return fabsf(o) < INFINITY || f != f ? o * f : o; }
+__device__ __forceinline__ f32x4 carried(f32x4 o, float f) {
+  return f32x4{carried(o.x, f), carried(o.y, f), carried(o.z, f), carried(o.w, f)};
+}
+
 // One item of a wavefront's share: tiles first .. end - 1 of a sequence, key head and row block.
 struct Item {
   int32_t b, h, block, first, end;
@@ -235,9 +232,8 @@ struct Wave {
   Words<4> (*q_lds)[64];   // [MT * kQChunks][64]: each lane its own
   f32x4 o[MT][S::kSets][S::kVec];
   float m[MT], l[MT];
-  // which of a lane's values have +inf, and which -inf in their sum, a bit each, NaN as both (add_odd)
-  static constexpr int kBits = (DP + 127) / 128;
-  uint32_t special[2][MT][kBits];
+  bool odd;                // mask_values left values out that are not finite
+  static constexpr int kBits = (DP + 127) / 128;  // words with a bit for each of a lane's values
   // keys and values of a tile
   Words<4> k[S::kSub][S::kChunks];
   Words<S::kVecWords> v[S::kKeys][S::kSets];
@@ -352,12 +348,11 @@ struct Wave {
       lo[mt] = a.window > 0 && hi[mt] >= a.window ? hi[mt] - a.window + 1 : 0;
       m[mt] = -INFINITY, l[mt] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kBits; ++i) special[0][mt][i] = special[1][mt][i] = 0;
-#pragma unroll
       for (int e = 0; e < S::kSets; ++e)
 #pragma unroll
         for (int j = 0; j < S::kVec; ++j) o[mt][e][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+    odd = false;
   }
 
   // f for the blocks of 16 that have rows.  The fp32 instructions take eight times as long as bf16's, so that an empty
@@ -517,9 +512,9 @@ struct Wave {
     }
   }
   // The same for values, as a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0;
-  // others that are not finite (rare) too, once the rows that see them have them.
+  // others that are not finite (rare) too, for find_odd.
   __device__ __forceinline__ void mask_values(int32_t tile) {
-    bool odd = false;
+    uint32_t any = 0;
 #pragma unroll
     for (int i = 0; i < S::kKeys; ++i) {
       const int32_t key = tile * S::kTile + 16 * (i / 4) + 4 * g + i % 4;
@@ -529,23 +524,70 @@ struct Wave {
 #pragma unroll
         for (int w = 0; w < S::kVecWords; ++w) {
           v[i][e].w[w] = seen ? v[i][e].w[w] : 0;
-          odd |= not_finite<CACHE>(v[i][e].w[w]);
+          any |= not_finite<CACHE>(v[i][e].w[w]);
         }
     }
-    if (__any(odd)) add_odd(tile);
+    if (__any(any != 0)) {
+      odd = true;
+#pragma unroll
+      for (int i = 0; i < S::kKeys; ++i)
+#pragma unroll
+        for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+          for (int w = 0; w < S::kVecWords; ++w) v[i][e].w[w] = finite_only<CACHE>(v[i][e].w[w]);
+    }
+  }
+  // Whether some row may see a value that is not finite: one was left out, or reached an accumulator (which is inf
+  // or NaN ever after, whatever it is multiplied by or added to).
+  __device__ __forceinline__ bool maybe_odd() const {
+    f32x4 t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+        for (int j = 0; j < S::kVec; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t[i] = fmaf(o[mt][e][j][i], 0.0f, t[i]);
+    const float u = (t.x + t.y) + (t.z + t.w);
+    return __any(odd || u != u);
   }
   __device__ static constexpr int bit(int e, int j, int i) { return (e * S::kVec + j) * 4 + i; }
-  // For +inf and -inf in turn, NaN counting as either: how many such values of each dimension a row sees, a product of
-  // ones and zeros.  A sum with one of them is it, whatever the weights (NaN with both), so a bit is enough until the
-  // end; the accumulators have no second place among the registers here.
-  __device__ __forceinline__ void add_odd(int32_t tile) {
+  // Which of a lane's values have +inf (bits[0]), and which -inf (bits[1]) among what their row sees of the item, NaN as
+  // both: a sum with one of them is it, whatever the weights (NaN with both).  The accumulators cannot tell: the sum of two
+  // bf16 numbers that a weight is makes inf NaN where the second is not positive, as do weights and factors that underflow
+  // to 0.  So the values are read once more, and what each row sees of either kind is counted: a product of ones and zeros.
+  __device__ __forceinline__ void find_odd(const Item &x, uint32_t (&bits)[2][MT][kBits]) {
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < kBits; ++i) bits[kind][mt][i] = 0;
+#pragma unroll 1
+    for (int32_t tile = x.first; tile < x.end; ++tile) {
+      At at[S::kSub];
+#pragma unroll
+      for (int t = 0; t < S::kSub; ++t) at[t] = locate(x, tile, t, true);
+      load_v(at);
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < S::kKeys; ++i)
+#pragma unroll
+        for (int e = 0; e < S::kSets; ++e)
+#pragma unroll
+          for (int w = 0; w < S::kVecWords; ++w) any |= not_finite<CACHE>(v[i][e].w[w]);
+      if (__any(any != 0)) count_odd(tile, bits);
+    }
+  }
+  __device__ __forceinline__ void count_odd(int32_t tile, uint32_t (&bits)[2][MT][kBits]) {
     const auto sees = [&](int mt, int t, int i) {
       const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
       return key >= lo[mt] && key <= hi[mt];
     };
 #pragma unroll 1
     for (int kind = 0; kind < 2; ++kind) {
-      // nothing is to be worked out before the loop and kept: registers are scarce on all ways to here
+      // nothing is to be worked out before the loop and kept: registers are scarce
 #pragma unroll
       for (int i = 0; i < S::kKeys; ++i)
 #pragma unroll
@@ -554,14 +596,13 @@ struct Wave {
           for (int w = 0; w < S::kVecWords; ++w) asm volatile("" : "+v"(v[i][e].w[w]));
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(lo[mt]), "+v"(hi[mt]));
-      uint32_t bits[MT][kBits];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < kBits; ++i) bits[mt][i] = 0;
       const auto put = [&](int mt, int e, int j, f32x4 count) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bits[mt][bit(e, j, i) / 32] |= count[i] > 0.0f ? 1u << bit(e, j, i) % 32 : 0u;
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t one = count[i] > 0.0f ? 1u << bit(e, j, i) % 32 : 0u;
+          bits[0][mt][bit(e, j, i) / 32] |= kind == 0 ? one : 0u;
+          bits[1][mt][bit(e, j, i) / 32] |= kind == 1 ? one : 0u;
+        }
       };
       if constexpr (CACHE == DSDE_FP32) {
 #pragma unroll
@@ -618,26 +659,16 @@ struct Wave {
             }
         }
       }
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < kBits; ++i) {
-          special[0][mt][i] |= kind == 0 ? bits[mt][i] : 0u;
-          special[1][mt][i] |= kind == 1 ? bits[mt][i] : 0u;
-        }
     }
-#pragma unroll
-    for (int i = 0; i < S::kKeys; ++i)
-#pragma unroll
-      for (int e = 0; e < S::kSets; ++e)
-#pragma unroll
-        for (int w = 0; w < S::kVecWords; ++w) v[i][e].w[w] = finite_only<CACHE>(v[i][e].w[w]);
   }
 
   // The item's rows, or its part of them.
   __device__ __forceinline__ void end(const Item &x, float *part) {
     constexpr int kRows = 16 * MT;
     const bool done = x.end - x.first == x.s.tiles;
+    uint32_t bits[2][MT][kBits];
+    const bool some = maybe_odd();
+    if (some) find_odd(x, bits);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int32_t row = x.block * kRows + 16 * mt + r;
@@ -645,10 +676,6 @@ struct Wave {
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       if (x.s.err) sum = NAN;  // a context that is none
-      uint32_t any = 0;
-#pragma unroll
-      for (int i = 0; i < kBits; ++i) any |= special[0][mt][i] | special[1][mt][i];
-      const bool odd = __any(any != 0);
       if (row < x.s.n * a.group) {
         float f = 1.0f;
         char *to = nullptr;
@@ -661,12 +688,12 @@ struct Wave {
             float y[S::kVec];
 #pragma unroll
             for (int j = 0; j < S::kVec; ++j) y[j] = o[mt][e][j][i] * f;
-            if (odd) {
+            if (some) {
 #pragma unroll
               for (int j = 0; j < S::kVec; ++j) {
                 const int w = bit(e, j, i) / 32, at = bit(e, j, i) % 32;
-                y[j] += special[0][mt][w] >> at & 1 ? INFINITY : 0.0f;
-                y[j] -= special[1][mt][w] >> at & 1 ? INFINITY : 0.0f;
+                const bool plus = bits[0][mt][w] >> at & 1, minus = bits[1][mt][w] >> at & 1;
+                if (plus || minus) y[j] = sum != sum || (plus && minus) ? NAN : plus ? INFINITY : -INFINITY;
               }
             }
             if (done) {
@@ -900,7 +927,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
       const float f0 = exp2_fast(m0[k] - ref), f1 = exp2_fast(m1[k] - ref);
       float f;
       char *to = finished<CACHE>(a, x.row0, x.h, row0 + i, m, l0[k] * f0 + l1[k] * f1, d == 0, &f);
-      const f32x4 o = (o0[k] * f0 + o1[k] * f1) * f;
+      const f32x4 o = carried(carried(o0[k], f0) + carried(o1[k], f1), f);
       const float y[4] = {o.x, o.y, o.z, o.w};
       if (d < a.cache.dim) store_row<CACHE, 4>(to, d, y);
     }
@@ -927,7 +954,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
       const float f0 = exp2_fast(m - ref), f1 = exp2_fast(pm - ref);
       m = now;
       l = l * f0 + pl * f1;
-      o = o * f0 + po * f1;
+      o = carried(o, f0) + carried(po, f1);
     }
     for (int32_t step = 1; step < span; step *= 2) {
       const float pm = __shfl_xor(m, step), pl = __shfl_xor(l, step);
@@ -936,12 +963,13 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, AttendLayout at
       const float f0 = exp2_fast(m - ref), f1 = exp2_fast(pm - ref);
       m = now;
       l = l * f0 + pl * f1;
-      o = o * f0 + po * f1;
+      o = carried(o, f0) + carried(po, f1);
     }
     if (mine && lane == 0) {
       float f;
       char *to = finished<CACHE>(a, x.row0, x.h, row0 + i, m, l, d == 0, &f);
-      const float y[4] = {o.x * f, o.y * f, o.z * f, o.w * f};
+      o = carried(o, f);
+      const float y[4] = {o.x, o.y, o.z, o.w};
       if (d < a.cache.dim) store_row<CACHE, 4>(to, d, y);
     }
   }
