@@ -570,7 +570,7 @@ int32_t dsde_distill_step(const void *logits, int64_t row_stride, int32_t dtype,
  * SL_b + 1 rows per sequence, pages mapped and given back as the SLs change), and
  * the rows' attention over the cache.  A step of a serving loop:
  *
- *   1. dsde_kv_map        from the accepted counts of the last step and the SLs of the coming one:
+ *   1. dsde_kv_map_next   from the accepted counts of the last step and the SLs of the coming one:
  *                         how many tokens stay, pages for the new rows, each row's slot
  *   2. dsde_kv_write      per layer: the rows' keys and values into their slots
  *   3. dsde_kv_attention  per layer: the rows' queries over each sequence's cache
@@ -620,12 +620,28 @@ size_t dsde_kv_map_workspace_bytes(int32_t B);
  *                               sequences that need any too), or a page id outside [0, pages) at one of its rows.
  *                               A flagged sequence keeps its pages (except after such a page id, whose rows alone have slot -1),
  *                               has context 0, and slots -1 for its rows, which still count (0 if n_b is negative).
+ *
+ * A flagged sequence's rows are not written (slots -1), attention gives 0 for them, and what dsde_step makes of
+ * them means nothing: no token of that step was accepted, and its last token is to be scored again.  So its count from
+ * that step must not be added by the next call, which otherwise takes tokens for its own that were never written:
+ * dsde_kv_map_next, or -1 in accepted.  base_b counts the step before and holds.  Where base is kv_len, a call has
+ * advanced it, for the sequences that it flags too: a call that is repeated after a fault takes no counts again (accepted NULL).
  */
 int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, int64_t rows, const int32_t *sl,
                     int32_t extra, const int32_t *kv_len, const int32_t *accepted, int32_t *table, int32_t *held,
                     int32_t *free_pages, int32_t *n_free, int32_t *base, int32_t *context, int32_t *cu_rows,
                     int32_t *slots, int32_t *positions, uint32_t *seq_err, void *workspace, size_t workspace_bytes,
                     void *stream);
+
+/*
+ * dsde_kv_map behind a call that may have flagged sequences: accepted[b] is not read where last_err[b] is not 0.
+ *   last_err [B]       uint32   optional (NULL: as dsde_kv_map); the last call's seq_err, also in the place of this one's
+ */
+int32_t dsde_kv_map_next(int32_t B, int32_t page_size, int32_t pages, int32_t width, int64_t rows, const int32_t *sl,
+                         int32_t extra, const int32_t *kv_len, const int32_t *accepted, const uint32_t *last_err,
+                         int32_t *table, int32_t *held, int32_t *free_pages, int32_t *n_free, int32_t *base,
+                         int32_t *context, int32_t *cu_rows, int32_t *slots, int32_t *positions, uint32_t *seq_err,
+                         void *workspace, size_t workspace_bytes, void *stream);
 
 /* A cache (passed by pointer, read during the call only).  Element (p, h, i, d) of the keys is
  * k[p * page_stride + h * head_stride + i * token_stride + d], so a page may hold heads of tokens or tokens of

@@ -31,7 +31,7 @@ EXPORTS = ("dsde_abi_version", "dsde_status_string", "dsde_verify_workspace_byte
            "dsde_shard_accept", "dsde_shard_accept_step", "dsde_shard_draw_mass", "dsde_shard_draw_pick",
            "dsde_sample_workspace_bytes", "dsde_sample", "dsde_top_logits", "dsde_distill_workspace_bytes",
            "dsde_distill_loss", "dsde_distill_grad", "dsde_distill_step", "dsde_kv_map_workspace_bytes", "dsde_kv_map",
-           "dsde_kv_write", "dsde_kv_attention_workspace_bytes", "dsde_kv_attention")
+           "dsde_kv_map_next", "dsde_kv_write", "dsde_kv_attention_workspace_bytes", "dsde_kv_attention")
 # sizes of the records the vocabulary-shard calls exchange (dsde_shard_partial,
 # dsde_draw_job, dsde_shard_mass); kept as raw bytes on the Python side
 SHARD_PARTIAL_BYTES, DRAW_JOB_BYTES, SHARD_MASS_BYTES = 64, 44, 32
@@ -115,6 +115,8 @@ def load(path: str = LIB_PATH):
     lib.dsde_kv_map_workspace_bytes.argtypes = [i32]
     lib.dsde_kv_map.restype = i32
     lib.dsde_kv_map.argtypes = [i32, i32, i32, i32, i64, P, i32, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
+    lib.dsde_kv_map_next.restype = i32
+    lib.dsde_kv_map_next.argtypes = [i32, i32, i32, i32, i64, P, i32, P, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
     lib.dsde_kv_write.restype = i32
     lib.dsde_kv_write.argtypes = [P, P, i64, i64, P, i64, i64, i32, i64, P, P, P]
     lib.dsde_kv_attention_workspace_bytes.restype = sz
@@ -565,12 +567,13 @@ def new_kv_map_out(B, rows, device="cuda"):
     return out
 
 
-def kv_map(sl, kv_len, pool, page_size, rows, extra=1, accepted=None, out=None, workspace=None, stream=None):
-    """``dsde_kv_map``: pages for the coming ``sl + extra`` rows of every sequence (those
+def kv_map(sl, kv_len, pool, page_size, rows, extra=1, accepted=None, out=None, workspace=None, stream=None, last_err=None):
+    """``dsde_kv_map_next``: pages for the coming ``sl + extra`` rows of every sequence (those
     no longer needed go back first) and the slot of each row.  ``kv_len`` [B] int32 are the tokens in
     the cache before the last step, ``accepted`` [B] int32 that step's counts (``verify``'s; -1 or
-    None: nothing to add), ``pool`` the state of ``new_kv_pool``, updated in place, ``rows`` the room
-    for rows.  Returns a dict with base, context [B], cu_rows [B + 1], slots, positions [rows]
+    None: nothing to add), ``last_err`` [B] int32 the last call's seq_err (which may be ``out``'s): sequences flagged
+    there had no rows in that step, and what it accepted of them is not added; without it their counts must be -1.
+    ``pool`` is the state of ``new_kv_pool``, updated in place, ``rows`` the room for rows.  Returns a dict with base, context [B], cu_rows [B + 1], slots, positions [rows]
     (-1 behind the last row; not with rows = 0) and seq_err."""
     native = _native or _bind()
     if out is None or workspace is None:
@@ -580,7 +583,7 @@ def kv_map(sl, kv_len, pool, page_size, rows, extra=1, accepted=None, out=None, 
                 out = new_kv_map_out(B, int(rows), dev)
             if workspace is None:
                 workspace = new_kv_map_workspace(B, dev)
-    native.kv_map(sl, int(extra), kv_len, accepted, pool, int(page_size), int(rows), out, workspace, _handle(stream))
+    native.kv_map(sl, int(extra), kv_len, accepted, last_err, pool, int(page_size), int(rows), out, workspace, _handle(stream))
     return out
 
 

@@ -26,7 +26,7 @@ PyObject *g_error = nullptr;  // paper_2509_01083_amd.DsdeError
   X(dsde_status_string)                                                                                         \
   X(dsde_verify) X(dsde_step) X(dsde_step_static) X(dsde_kld_signal) X(dsde_next_sl) X(dsde_calibration_update) \
   X(dsde_sample) X(dsde_top_logits) X(dsde_distill_loss) X(dsde_distill_grad) X(dsde_distill_step)              \
-  X(dsde_kv_map) X(dsde_kv_write) X(dsde_kv_attention)                                                          \
+  X(dsde_kv_map_next) X(dsde_kv_write) X(dsde_kv_attention)                                                          \
   X(dsde_shard_stats) X(dsde_shard_accept) X(dsde_shard_accept_step) X(dsde_shard_draw_mass) X(dsde_shard_draw_pick)
 struct Library {
 #define X(name) decltype(&::name) name;
@@ -831,7 +831,7 @@ void check_rows(const dsde_kv_cache &c, const HeadRows &r, const char *name) {
     fail(std::string(name) + " must be of the cache's type, or bfloat16 for a cache of float8_e4m3fn");
 }
 
-// kv_map(sl, extra, kv_len, accepted, pool, page_size, rows, out, workspace, stream)
+// kv_map(sl, extra, kv_len, accepted, last_err, pool, page_size, rows, out, workspace, stream)
 PyObject *py_kv_map(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return guarded(args, n, [&](Args &a) {
     OneDevice dev;
@@ -840,6 +840,7 @@ PyObject *py_kv_map(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const auto *sl = take_on<int32_t>(a, dev, kI32, B, "sl");
     const int32_t extra = a.int32();
     const auto *kv_len = take_on<int32_t>(a, dev, kI32, B, "kv_len"), *accepted = take_on<int32_t>(a, dev, kI32, B, "accepted");
+    const auto *last_err = take_on<uint32_t>(a, dev, kErr, B, "last_err");
     PyObject *pool = a.next();
     const int64_t page = a.integer(), rows = a.integer();
     PyObject *table_o = dev.item(pool, "table"), *free_o = dev.item(pool, "free");
@@ -860,8 +861,9 @@ PyObject *py_kv_map(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void *ws = take_workspace(a, &bytes), *stream = a.stream();
     a.done();
     call([&] {
-      return g_lib.dsde_kv_map(int32_t(B), int32_t(page), int32_t(pages), int32_t(width), rows, sl, extra, kv_len, accepted,
-                               table, held, stack, n_free, base, context, cu, slots, positions, err, ws, bytes, stream);
+      return g_lib.dsde_kv_map_next(int32_t(B), int32_t(page), int32_t(pages), int32_t(width), rows, sl, extra, kv_len,
+                                    accepted, last_err, table, held, stack, n_free, base, context, cu, slots, positions, err,
+                                    ws, bytes, stream);
     });
   });
 }

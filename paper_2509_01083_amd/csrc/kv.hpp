@@ -29,6 +29,7 @@ struct MapArgs {
   const int32_t *sl;
   int32_t extra;
   const int32_t *kv_len, *accepted;  // accepted may be null
+  const uint32_t *last_err;          // may be null, may be seq_err
   int32_t *table, *held, *stack, *n_free, *base, *context, *cu_rows, *slots, *positions;
   uint32_t *seq_err;
   int32_t *top, *from, *taken, *back;  // workspace

@@ -99,6 +99,15 @@ int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, 
                     int32_t *free_pages, int32_t *n_free, int32_t *base, int32_t *context, int32_t *cu_rows,
                     int32_t *slots, int32_t *positions, uint32_t *seq_err, void *workspace, size_t workspace_bytes,
                     void *stream) {
+  return dsde_kv_map_next(B, page_size, pages, width, rows, sl, extra, kv_len, accepted, nullptr, table, held, free_pages,
+                          n_free, base, context, cu_rows, slots, positions, seq_err, workspace, workspace_bytes, stream);
+}
+
+int32_t dsde_kv_map_next(int32_t B, int32_t page_size, int32_t pages, int32_t width, int64_t rows, const int32_t *sl,
+                         int32_t extra, const int32_t *kv_len, const int32_t *accepted, const uint32_t *last_err,
+                         int32_t *table, int32_t *held, int32_t *free_pages, int32_t *n_free, int32_t *base,
+                         int32_t *context, int32_t *cu_rows, int32_t *slots, int32_t *positions, uint32_t *seq_err,
+                         void *workspace, size_t workspace_bytes, void *stream) {
   const int64_t limit = int64_t(1) << 31;
   if (B < 1 || B > dsde::kMaxKvSeqs || shift_of(page_size) < 0 || pages < 1 || int64_t(pages) * page_size >= limit)
     return DSDE_INVALID_ARG;
@@ -111,8 +120,8 @@ int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, 
   if (misaligned(workspace)) return DSDE_INVALID_ARG;
   char *ws = static_cast<char *>(workspace);
   const auto part = [&](size_t at) { return reinterpret_cast<int32_t *>(ws + at); };
-  const dsde::MapArgs a{B, shift_of(page_size), pages, width, rows, sl, extra, kv_len, accepted, table, held,
-                        free_pages, n_free, base, context, cu_rows, slots, positions, seq_err, part(l.top),
+  const dsde::MapArgs a{B, shift_of(page_size), pages, width, rows, sl, extra, kv_len, accepted, last_err, table,
+                        held, free_pages, n_free, base, context, cu_rows, slots, positions, seq_err, part(l.top),
                         part(l.from), part(l.taken), part(l.back)};
   return dsde::launch_kv_map(a, static_cast<hipStream_t>(stream));
 }

@@ -52,7 +52,9 @@ struct Want {
 };
 __device__ __forceinline__ Want wanted(const MapArgs &a, int32_t b) {
   Want x;
-  const int64_t len = a.kv_len[b], acc = a.accepted ? a.accepted[b] : -1;
+  // a sequence without rows in the last step has none to keep; last_err may be seq_err, of which a thread reads what
+  // it writes later
+  const int64_t len = a.kv_len[b], acc = a.accepted && !(a.last_err && a.last_err[b]) ? a.accepted[b] : -1;
   x.n = int64_t(a.sl[b]) + a.extra;
   x.base = len + acc + 1;
   x.from = a.held[b];
