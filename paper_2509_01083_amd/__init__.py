@@ -590,7 +590,8 @@ def kv_map(sl, kv_len, pool, page_size, rows, extra=1, accepted=None, out=None, 
 def kv_write(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, row_err=None, stream=None):
     """``dsde_kv_write``: rows ``k``, ``v`` [T, heads, dim] (any strides of whole 16 bytes) into
     the ``slots`` [T] int32 of a cache (-1: left out).  A float8_e4m3fn cache takes bfloat16 rows
-    divided by ``k_scale``, ``v_scale`` [heads] float32.  Returns row_err [T]."""
+    divided by ``k_scale``, ``v_scale`` [heads] float32.  Returns row_err [T].  Like ``kv_attention`` it goes forward only: a
+    tensor that requires a gradient is refused while gradients are recorded."""
     native = _native or _bind()
     if row_err is None:
         _gpu_tensor(k, "k")
@@ -615,7 +616,9 @@ def kv_attention(q, k_cache, v_cache, table, context, cu_rows, max_rows, scale=N
     [B + 1] int32, at most ``max_rows`` each, the newest of ``context`` [B] int32 tokens) over the cache
     through ``table`` [B, width] int32.  ``scale`` defaults to dim ** -0.5; ``window`` > 0: a row sees
     that many tokens, itself the last.  Returns a dict with out [T, q_heads, dim], seq_err (and lse
-    [T, q_heads] float32 when asked for); pass ``out`` to reuse its buffers (lse is computed where it has one)."""
+    [T, q_heads] float32 when asked for); pass ``out`` to reuse its buffers (lse is computed where it has one; one that
+    is asked for and missing is put there).  It goes forward only: a tensor that requires a gradient is refused while gradients
+    are recorded (under ``torch.no_grad()`` they are not)."""
     native = _native or _bind()
     if out is None or workspace is None or (lse and "lse" not in out):
         if _gpu_tensor(q, "q").dim() != 3 or _gpu_tensor(k_cache, "k_cache").dim() != 4:

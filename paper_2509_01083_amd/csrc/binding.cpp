@@ -7,6 +7,7 @@
 // step's kernels take in small batches.
 #include <Python.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -757,6 +758,12 @@ T *out_on(PyObject *dict, OneDevice &dev, const char *key, int type, int64_t n) 
   return p;
 }
 
+// The cache's calls go forward only: where a gradient is being recorded, a tensor that wants one would lose it unsaid.
+void forward_only(PyObject *o, const char *name) {
+  if (o != Py_None && THPVariable_Check(o) && c10::GradMode::is_enabled() && THPVariable_Unpack(o).requires_grad())
+    fail(std::string(name) + " requires a gradient, which the cache's calls do not give: call them under torch.no_grad()");
+}
+
 // Rows [T, heads, dim] with dense heads.
 struct HeadRows {
   void *data;
@@ -767,6 +774,7 @@ HeadRows head_rows(PyObject *o, OneDevice &dev, const char *name) {
   size_of(o, 2, name);
   const at::Tensor &t = THPVariable_Unpack(o);
   if (t.dim() != 3) fail(std::string(name) + " must be [rows, heads, dim]");
+  forward_only(o, name);
   if (t.scalar_type() != at::ScalarType::BFloat16 && t.scalar_type() != at::ScalarType::Float)
     fail(std::string(name) + " must be bfloat16 or float32");
   if (!t.is_cuda()) fail(std::string(name) + " must be a GPU tensor");
@@ -790,6 +798,7 @@ dsde_kv_cache take_cache(Args &a, OneDevice &dev, bool write) {
     size_of(o[i], 3, names[i]);
     const at::Tensor &t = THPVariable_Unpack(o[i]);
     if (t.dim() != 4) fail(std::string(names[i]) + " must be [pages, heads, page_size, dim]");
+    forward_only(o[i], names[i]);
     const at::ScalarType is = t.scalar_type();
     if (is != at::ScalarType::BFloat16 && is != at::ScalarType::Float && is != at::ScalarType::Float8_e4m3fn)
       fail(std::string(names[i]) + " must be bfloat16, float32 or float8_e4m3fn");
@@ -819,8 +828,12 @@ dsde_kv_cache take_cache(Args &a, OneDevice &dev, bool write) {
     }
     if (write) written(o[i]);
   }
-  c.k_scale = take_on<float>(a, dev, kF32, c.heads, "k_scale");
-  c.v_scale = take_on<float>(a, dev, kF32, c.heads, "v_scale");
+  const auto scale = [&](const char *name) {
+    if (a.at != a.end) forward_only(*a.at, name);
+    return take_on<float>(a, dev, kF32, c.heads, name);
+  };
+  c.k_scale = scale("k_scale");
+  c.v_scale = scale("v_scale");
   if ((c.dtype == DSDE_E4M3) != (c.k_scale != nullptr) || (c.dtype == DSDE_E4M3) != (c.v_scale != nullptr))
     fail("k_scale and v_scale belong to a cache of float8_e4m3fn, and both to each");
   return c;
