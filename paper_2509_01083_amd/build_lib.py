@@ -13,7 +13,8 @@ beside this file:
 
 After linking, the device code in the library is disassembled and the build
 fails if any packed FP32 arithmetic instruction is found
-(``packed_fp32_instructions``; a CPU test runs the same check).
+(``packed_fp32_instructions``), or a copy of a vector register that the compiler
+has placed where lanes are still off (``partial_copies``).  CPU tests run the same checks.
 
 ``build`` then compiles the Python binding's marshalling code
 (csrc/binding.cpp, host code only) against torch's headers; it takes its entry
@@ -66,10 +67,12 @@ def build(verbose: bool = False) -> str:
         objs.append(obj)
     tmp = LIB + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
-    bad = packed_fp32_instructions(tmp)
-    if bad:
-        os.remove(tmp)
-        raise RuntimeError("packed FP32 instructions in the device code: " + "; ".join(bad[:5]))
+    text = device_disassembly(tmp)
+    for bad, what in ((packed_fp32_instructions(text=text), "packed FP32 instructions in the device code"),
+                      (partial_copies(text=text), "vector registers copied while lanes are off")):
+        if bad:
+            os.remove(tmp)
+            raise RuntimeError(f"{what}: " + "; ".join(bad[:5]))
     os.replace(tmp, LIB)
     build_binding(verbose)
     return LIB
@@ -121,9 +124,61 @@ def device_disassembly(path: str = LIB) -> str:
     return "\n".join(text)
 
 
-def packed_fp32_instructions(path: str = LIB):
+def packed_fp32_instructions(path: str = LIB, text: str = None):
     """Lines of the library's device code that use packed FP32 arithmetic."""
-    return [ln.strip() for ln in device_disassembly(path).splitlines() if PACKED_FP32.search(ln)]
+    text = device_disassembly(path) if text is None else text
+    return [ln.strip() for ln in text.splitlines() if PACKED_FP32.search(ln)]
+
+
+_SYMBOL = re.compile(r"^([0-9a-f]+) <(\S+)>:$")
+_LINE = re.compile(r"^\s+(\S.*?)\s*// ([0-9A-F]+): [0-9A-F ]+(?:<(\S+?)(?:\+0x([0-9a-f]+))?>)?$")
+_MOVE = re.compile(r"v_mov_b(32|64)_e32 |v_accvgpr_(read|write|mov)_b32 |scratch_(load|store)_dword")
+_LANES_ON = re.compile(r"s_or_b64 exec, exec, |s_(or|andn2)_saveexec_b64 ")
+
+
+def partial_copies(path: str = LIB, text: str = None):
+    """Moves of vector registers ahead of the instruction that turns lanes back on, at the place where the two ways of
+    a divergent branch meet or a divergent loop ends: "symbol: instruction" each.
+
+    The register allocator, when it gives a value another register or a place in memory from such a point on, puts the
+    copy behind the instructions that begin the block; a scalar copy that it has put there before hides the
+    restore of the lane mask from it (ROCm 7.2, seen in kernels with many spilled scalar registers).  The copy then
+    leaves out the lanes that were off, and what they hold in the new place is whatever was there: in an attention
+    kernel a row's number, so that its query was loaded from an address that is none.  Only a block's head
+    is looked at, scalar instructions and moves alone; a program's own moves lie behind other work."""
+    text = device_disassembly(path) if text is None else text
+    bodies, base = [], {}  # (symbol, [(address, instruction)]); symbol -> address
+    targets = set()
+    for ln in text.splitlines():
+        m = _SYMBOL.match(ln)
+        if m:
+            bodies.append((m.group(2), []))
+            base = {m.group(2): int(m.group(1), 16)}
+            continue
+        m = _LINE.match(ln)
+        if not m or not bodies:
+            continue
+        bodies[-1][1].append((int(m.group(2), 16), m.group(1)))
+        if m.group(1).startswith("s_cbranch_execz") and m.group(3) in base:
+            targets.add((m.group(3), base[m.group(3)] + int(m.group(4) or "0", 16)))
+    found = []
+    for name, body in bodies:
+        moves = None  # those of the head at hand; None outside of one
+        for at, ins in body:
+            if (name, at) in targets:
+                moves = []
+            if ins.startswith("s_cbranch_execnz"):
+                moves = []
+            elif moves is None:
+                continue
+            elif _LANES_ON.match(ins):
+                found += [f"{name}: {x}" for x in moves]
+                moves = None
+            elif _MOVE.match(ins):
+                moves.append(ins)
+            elif not re.match(r"s_(?!cbranch|branch|endpgm|setpc|\w+ exec|\w+_saveexec)|v_(read|write)lane|v_readfirstlane", ins):
+                moves = None
+    return found
 
 
 if __name__ == "__main__":

@@ -343,8 +343,12 @@ struct Wave {
     lo_any = a.window > 0 && oldest >= a.window ? oldest - a.window + 1 : 0;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
+      // the quotient of every lane, no branch around it: where lanes without a row leave one, the compiler has saved
+      // other values with those lanes still off (build_lib.py, partial_copies), and a later load went astray
       const int32_t row = (x.block * MT + mt) * 16 + r;
-      hi[mt] = row < x.s.n * a.group ? oldest + row / a.group : -1;
+      const bool there = row < x.s.n * a.group;
+      const int32_t j = (there ? row : 0) / a.group;
+      hi[mt] = there ? oldest + j : -1;
       lo[mt] = a.window > 0 && hi[mt] >= a.window ? hi[mt] - a.window + 1 : 0;
       m[mt] = -INFINITY, l[mt] = 0.0f;
 #pragma unroll
