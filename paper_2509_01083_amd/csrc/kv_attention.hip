@@ -502,18 +502,26 @@ struct Wave {
     }
   }
 
-  // Scores that some row does not see, or of a bad page.
-  __device__ __forceinline__ void mask(f32x4 (&x)[MT][S::kSub], int32_t tile, const At (&at)[S::kSub]) {
+  // Scores that some row does not see.
+  __device__ __forceinline__ void mask(f32x4 (&x)[MT][S::kSub], int32_t tile) {
 #pragma unroll
-    for (int t = 0; t < S::kSub; ++t) {
-      const float f = at[t].bad ? NAN : 1.0f;
+    for (int t = 0; t < S::kSub; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int32_t key = tile * S::kTile + 16 * t + 4 * g + i;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= lo[mt] && key <= hi[mt] ? x[mt][t][i] * f : -INFINITY;
+        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = key >= lo[mt] && key <= hi[mt] ? x[mt][t][i] : -INFINITY;
       }
-    }
+  }
+  // Scores of a bad page: NaN where mask has left any, to rows that see them.  Apart from mask, where a factor for every
+  // score kept registers that the loop needs (36 rows of 256 571 us, 64 over e4m3 423, behind a branch of their own 547 and 378).
+  __device__ __forceinline__ void spoil(f32x4 (&x)[MT][S::kSub], const At (&at)[S::kSub]) {
+#pragma unroll
+    for (int t = 0; t < S::kSub; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = at[t].bad && x[mt][t][i] != -INFINITY ? NAN : x[mt][t][i];
   }
   // The same for values, as a weight of 0 takes no part only beside finite ones.  Values that no row sees become 0;
   // others that are not finite (rare) too, for find_odd.
@@ -852,10 +860,12 @@ __global__ __launch_bounds__(kAttendThreads, 1) void attend_kernel(AttendArgs a,
       f32x4 p[MT][S::kSub];
       w.of_live([&](auto n) { w.template scores<n.value>(p); });
       w.load_k(next);
-      bool clear = tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
+      bool bad = false;
 #pragma unroll
-      for (int t = 0; t < S::kSub; ++t) clear &= !now[t].bad;
-      if (!clear) w.mask(p, tile, now);
+      for (int t = 0; t < S::kSub; ++t) bad |= now[t].bad;
+      const bool clear = !bad && tile * S::kTile >= w.lo_all && tile * S::kTile + S::kTile - 1 <= w.hi_all;
+      if (!clear) w.mask(p, tile);
+      if (bad) w.spoil(p, now);
       w.of_live([&](auto n) { w.template weigh<n.value>(p); });
       if (!clear) w.mask_values(tile);
       w.of_live([&](auto n) { w.template add<n.value>(p); });
