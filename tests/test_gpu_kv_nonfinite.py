@@ -134,3 +134,13 @@ def test_many_sequences_each_with_its_own(gpu_lib):
             if c - n + j >= 0:
                 want[x["cu"][b] + j, 2:, b] = INF if b % 2 else -INF
     assert torch.equal(o, want) and torch.equal(got["lse"], clean["lse"])
+
+
+@pytest.mark.parametrize("c", [40, 700, 5000])
+def test_a_scale_past_the_types_range(gpu_lib, c):
+    """Values that pass the largest number once they are scaled are infinite with their sign, in one wavefront and in parts."""
+    x = make([c], [1], H=1, G=2, D=64, dtype="e4m3", junk=False)
+    x["v"] = torch.where(torch.arange(64) % 2 == 0, 256.0, -256.0).expand(x["v"].shape).to(DT["e4m3"])
+    x["v_scale"] = torch.full((1,), 2.0 ** 121)  # 2^129
+    o = gpu_lib.kv_attention(**to_gpu(x))["out"].float().cpu()
+    assert bool((o[..., 0::2] == INF).all()) and bool((o[..., 1::2] == -INF).all())
