@@ -6,8 +6,10 @@
 // o likewise.  So a wavefront goes over its share of the tokens once, with its keys, values and
 // accumulators in registers; what is joined is (m, l, o).
 //
-// Bound by HBM: every key and value is read once, and the rows of all query heads of a key head
-// (and of all its newest tokens) share that read.  The matrix instructions hold 16 rows at a time:
+// Bound by HBM: every key and value is read once for a block of rows, in which the query heads of a key head and
+// their newest tokens share that read.  A block is as many rows as registers hold: 64 of heads up to 128 (32 in fp32 above
+// 64), of larger ones 32 (16 in fp32).  A key head with more rows has several blocks, each of which reads all it sees: 72
+// rows of 128 in bf16 (256 sequences, 2.4 GB) take 883 us, 64 take 513.  The matrix instructions hold 16 rows at a time:
 //   scores^T (16 keys x 16 rows)  = K (16 x d) Q^T (d x 16)
 //   out^T    (16 dims x 16 rows) += V^T (16 x 32 keys) P^T (32 x 16)
 // Scores come out with a row's keys in the registers of four lanes, in the order that the second
@@ -524,7 +526,8 @@ struct Wave {
       }
   }
   // Scores of a bad page: NaN where mask has left any, to rows that see them.  Apart from mask, where a factor for every
-  // score kept registers that the loop needs (36 rows of 256 571 us, 64 over e4m3 423, behind a branch of their own 547 and 378).
+  // score kept registers that the loop needs (256 sequences of 32 rows of 256 542 us, of 64 over e4m3 464; behind a branch of
+  // their own 517 and 425).
   __device__ __forceinline__ void spoil(f32x4 (&x)[MT][S::kSub], const At (&at)[S::kSub]) {
 #pragma unroll
     for (int t = 0; t < S::kSub; ++t)
@@ -578,7 +581,8 @@ struct Wave {
   // Which of a lane's values have +inf (bits[0]), and which -inf (bits[1]) among what their row sees of the item, NaN as
   // both: a sum with one of them is it, whatever the weights (NaN with both).  The accumulators cannot tell: the sum of two
   // bf16 numbers that a weight is makes inf NaN where the second is not positive, as do weights and factors that underflow
-  // to 0.  So the values are read once more, and what each row sees of either kind is counted: a product of ones and zeros.
+  // to 0.  So the values are read once more, and what each row sees of either kind is counted: a product of ones and zeros
+  // (256 sequences of 256 to 8,192 tokens, up to 36 rows: an infinity in each 610 us, in one 541, in none 428 to 455).
   __device__ __forceinline__ void find_odd(const Item &x, uint32_t (&bits)[2][MT][kBits]) {
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind)
