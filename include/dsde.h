@@ -635,7 +635,8 @@ int32_t dsde_kv_map(int32_t B, int32_t page_size, int32_t pages, int32_t width, 
 
 /*
  * dsde_kv_map behind a call that may have flagged sequences: accepted[b] is not read where last_err[b] is not 0.
- *   last_err [B]       uint32   optional (NULL: as dsde_kv_map); the last call's seq_err, also in the place of this one's
+ *   last_err [B]       uint32   optional (NULL: as dsde_kv_map); the last call's seq_err, also in the place of this one's;
+ *                               zeros before the first call
  */
 int32_t dsde_kv_map_next(int32_t B, int32_t page_size, int32_t pages, int32_t width, int64_t rows, const int32_t *sl,
                          int32_t extra, const int32_t *kv_len, const int32_t *accepted, const uint32_t *last_err,

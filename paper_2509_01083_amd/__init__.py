@@ -571,7 +571,7 @@ def kv_map(sl, kv_len, pool, page_size, rows, extra=1, accepted=None, out=None, 
     """``dsde_kv_map_next``: pages for the coming ``sl + extra`` rows of every sequence (those
     no longer needed go back first) and the slot of each row.  ``kv_len`` [B] int32 are the tokens in
     the cache before the last step, ``accepted`` [B] int32 that step's counts (``verify``'s; -1 or
-    None: nothing to add), ``last_err`` [B] int32 the last call's seq_err (which may be ``out``'s): sequences flagged
+    None: nothing to add), ``last_err`` [B] int32 the last call's seq_err (which may be ``out``'s; zeros before the first call): sequences flagged
     there had no rows in that step, and what it accepted of them is not added; without it their counts must be -1.
     ``pool`` is the state of ``new_kv_pool``, updated in place, ``rows`` the room for rows.  Returns a dict with base, context [B], cu_rows [B + 1], slots, positions [rows]
     (-1 behind the last row; not with rows = 0) and seq_err."""

@@ -95,3 +95,57 @@ def test_a_shortage_ends_and_nothing_unwritten_is_seen(gpu_lib):
         accepted.copy_(torch.tensor([s for s in sl], **I32))
         lens = [n if e else n + s + 1 for n, s, e in zip(lens, sl, err)]
     assert seen[1] == [0, 0, 256] and not any(sum(seen[2:], []))
+
+
+def test_a_captured_map_remembers_whom_it_flagged(gpu_lib):
+    """One graph that reads the flags it wrote in the replay before, with eager work between replays, through shortages."""
+    r = random.Random(21)
+    B, W, page, room = 70, 9, 16, 70 * 41
+    P = B * W
+    lens, pool = state(r, B, W, page, P, 80, spare=2)
+    gpu = to_gpu(pool)
+    keep = {k: v.clone() for k, v in gpu.items()}
+    sl, acc, kv_len = (torch.zeros(B, **I32) for _ in range(3))
+    out, ws = gpu_lib.new_kv_map_out(B, room), gpu_lib.new_kv_map_workspace(B)
+    out["base"] = kv_len
+
+    def step():
+        gpu_lib.kv_map(sl, kv_len, gpu, page, room, accepted=acc, last_err=out["seq_err"], out=out, workspace=ws)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k, v in keep.items():
+        gpu[k].copy_(v)
+    out["seq_err"].zero_()
+    kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+    accepted, flagged, ever, again = [-1] * B, [0] * B, 0, 0
+    for i in range(6):
+        drafts = [r.randrange(0, 40) for _ in range(B)]
+        sl.copy_(torch.tensor(drafts, dtype=torch.int32))
+        acc.copy_(torch.tensor(accepted, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        pool, want = R.kv_map(drafts, 1, lens, [-1 if f else a for f, a in zip(flagged, accepted)], pool["table"], pool["held"], pool["free"],
+                              pool["n_free"][0], page, P, room)
+        for k, v in want.items():
+            assert out[k].tolist() == v, (i, k)
+        for k, v in pool.items():
+            assert gpu[k].tolist() == v, (i, k)
+        again += sum(bool(a) and not b for a, b in zip(flagged, want["seq_err"]))
+        lens, flagged = want["base"], want["seq_err"]
+        ever += sum(map(bool, flagged))
+        accepted = [r.randrange(-9, 40) if f else r.randrange(0, d + 1) for f, d in zip(flagged, drafts)]
+    assert ever and again
+
+
+def test_flags_that_are_refused(gpu_lib):
+    sl, n = torch.ones(3, **I32), torch.zeros(3, **I32)
+    for bad, text in ((torch.zeros(3, dtype=torch.int64, device="cuda"), "last_err must be torch.int32, got torch.int64"),
+                      (torch.zeros(2, **I32), "last_err has 2 elements, needs 3"), (torch.zeros(3, dtype=torch.int32), "must be a GPU tensor"),
+                      (torch.zeros(6, **I32)[::2], "last_err must be contiguous")):
+        with pytest.raises(gpu_lib.DsdeError, match=text):
+            gpu_lib.kv_map(sl, n, gpu_lib.new_kv_pool(3, 4, 12), 16, 6, last_err=bad)
+    out = gpu_lib.kv_map(sl, n, gpu_lib.new_kv_pool(3, 4, 12), 16, 6, last_err=torch.zeros(3, dtype=torch.uint32, device="cuda"))
+    assert not out["seq_err"].any() and out["base"].tolist() == [0, 0, 0]
